@@ -20,7 +20,10 @@
  *     matrix cores (the same kernel with an uncompacted matrix is the dense
  *     baseline);
  *   - for non-structured (element-wise) pruning, the CSR form of the layer
- *     and its CONV as a sparse product (Section 5's comparison).
+ *     and its CONV as a sparse product (Section 5's comparison);
+ *   - for fully connected layers, the operators of a feed-forward block over
+ *     pruned or dense weight matrices: layer norm, the linear layer and the
+ *     gated pair of projections, each with its gradient.
  *
  * Conventions shared by every entry point
  *   - Every tensor argument is DEVICE memory owned by the caller.  The
@@ -452,6 +455,230 @@ typedef struct sa_sparse_conv_desc {
 size_t structadmm_conv_sparse_workspace(const sa_sparse_conv_desc *desc);
 
 int structadmm_conv_sparse_fwd(const sa_sparse_conv_desc *desc, hipStream_t stream);
+
+/* ---- feed-forward operators ------------------------------------------ */
+/*
+ * What stands around a pruned weight matrix in a feed-forward block: the layer
+ * norm before it, the matrix product with bias, activation and residual, and the
+ * gated pair of products, each with its gradient.  A layer whose W is [A, B, 1, 1]
+ * (a fully connected layer) is pruned by structadmm_project and compacted by
+ * structadmm_compact; the compacted matrix (row pitch ldk) is the W of these
+ * calls, and their weight gradients are the Gf of structadmm_sgd_step.
+ *
+ * Matrices are row-major with a row pitch in elements (ld >= columns, below
+ * 2^21); rows may start anywhere an element can (matrices whose rows start on
+ * 16-byte boundaries and have a whole number of 8-element vectors, or padding up
+ * to one, take the fastest kernels; others are first copied to such a layout in
+ * the workspace).  Padding between rows is neither read into a result nor
+ * written.  Products are summed in binary32 on the matrix cores; every other
+ * step is binary32 and the result is rounded once (nearest even) to its type.
+ * Sizes may be 0: an empty output is not written (its pointer may be NULL) and
+ * an empty sum is 0.  Infinities and NaN of the inputs reach the outputs that
+ * depend on them and no others.  Outputs may not overlap inputs or each other,
+ * except where stated.
+ */
+typedef enum {
+    SA_BF16 = 0, /* bfloat16 */
+    SA_F16 = 1,  /* binary16 */
+    SA_F32 = 2   /* binary32 */
+} sa_type;
+
+typedef enum {
+    SA_ACT_NONE = 0,
+    SA_ACT_RELU = 1,      /* max(z, 0), derivative 0 at 0; NaN stays NaN           */
+    SA_ACT_SIGMOID = 2,   /* 1 / (1 + exp(-z))                                    */
+    SA_ACT_SILU = 3,      /* z / (1 + exp(-z))                                    */
+    SA_ACT_GELU = 4,      /* z/2 (1 + erf(z / sqrt 2))                            */
+    SA_ACT_GELU_TANH = 5  /* z/2 (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3)))        */
+} sa_act;
+
+/* Largest row pitch of the matrices below, in elements. */
+#define SA_MAX_LD (1 << 21)
+
+/* ---- layer norm: structadmm_layer_norm_fwd / _bwd -------------------- */
+/*
+ * Y[r][c] = (X[r][c] - mean[r]) * rstd[r] * gamma[c] + beta[c],
+ * mean[r] = sum_c X[r][c] / cols, rstd[r] = 1 / sqrt(sum_c (X[r][c] - mean[r])^2 / cols + eps).
+ * gamma NULL stands for ones, beta NULL for zeros.  mean and rstd may be NULL
+ * (a forward pass without a backward one).  Y may be X itself with the same
+ * pitch.  A row of equal values gives rstd = 1 / sqrt(eps) and Y = beta.
+ */
+typedef struct sa_layer_norm_desc {
+    int64_t rows, cols;   /* rows >= 0, cols >= 1 */
+    int32_t type;         /* sa_type of X and Y */
+    float eps;            /* >= 0 */
+    const void *X;
+    int64_t ldx;
+    const float *gamma;   /* [cols] or NULL */
+    const float *beta;    /* [cols] or NULL */
+    void *Y;              /* out */
+    int64_t ldy;
+    float *mean;          /* out [rows] or NULL */
+    float *rstd;          /* out [rows] or NULL */
+} sa_layer_norm_desc;
+
+int structadmm_layer_norm_fwd(const sa_layer_norm_desc *desc, hipStream_t stream);
+
+/*
+ * With xn = (X - mean) * rstd and t = dY * gamma:
+ *   dX     = rstd * (t - sum_c(t) / cols - xn * sum_c(t * xn) / cols) + dR
+ *   dgamma = sum over rows of dY * xn,  dbeta = sum over rows of dY.
+ * dR is the gradient that reaches X past the norm (the residual path of a
+ * pre-norm block), NULL for none; dX may be dR or dY itself with the same pitch.
+ * dX, dgamma and dbeta may each be NULL (at least one is given).
+ */
+typedef struct sa_layer_norm_bwd_desc {
+    int64_t rows, cols;
+    int32_t type;         /* sa_type of dY, X, dR and dX */
+    const void *dY;
+    int64_t lddy;
+    const void *X;
+    int64_t ldx;
+    const float *mean;    /* [rows], as the forward pass wrote them */
+    const float *rstd;
+    const float *gamma;   /* [cols] or NULL */
+    const void *dR;       /* or NULL */
+    int64_t lddr;
+    void *dX;             /* out or NULL */
+    int64_t lddx;
+    float *dgamma;        /* out [cols] or NULL */
+    float *dbeta;         /* out [cols] or NULL */
+    void *ws;             /* structadmm_layer_norm_bwd_workspace() bytes, 256-byte aligned */
+    size_t ws_bytes;
+} sa_layer_norm_bwd_desc;
+
+/* Workspace bytes (0 if none, and for an invalid descriptor; the pointers are not read). */
+size_t structadmm_layer_norm_bwd_workspace(const sa_layer_norm_bwd_desc *desc);
+int structadmm_layer_norm_bwd(const sa_layer_norm_bwd_desc *desc, hipStream_t stream);
+
+/* ---- linear layer: structadmm_linear_fwd / _bwd ---------------------- */
+/*
+ * z = X W^T + bias, Y = act(z) + R: X [M, K], W [N, K], bias [N], R and Y [M, N].
+ * Z, when given, receives z for the backward pass.  Y may be R itself with the
+ * same pitch.
+ */
+typedef struct sa_linear_desc {
+    int64_t M, N, K;
+    int32_t type;        /* SA_BF16 or SA_F16: X, W and Z */
+    int32_t out_type;    /* type or SA_F32: R and Y       */
+    int32_t act;         /* sa_act */
+    const void *X;
+    int64_t ldx;
+    const void *W;
+    int64_t ldw;
+    const float *bias;   /* [N] or NULL */
+    const void *R;       /* [M, N] or NULL */
+    int64_t ldr;
+    void *Y;             /* out [M, N] */
+    int64_t ldy;
+    void *Z;             /* out [M, N] or NULL */
+    int64_t ldz;
+    void *ws;            /* structadmm_linear_workspace() bytes, 256-byte aligned */
+    size_t ws_bytes;
+} sa_linear_desc;
+
+size_t structadmm_linear_workspace(const sa_linear_desc *desc);
+int structadmm_linear_fwd(const sa_linear_desc *desc, hipStream_t stream);
+
+/*
+ * dz = dY * act'(Z) (dY where act is SA_ACT_NONE), rounded to type;
+ * dX = dz W, dW = dz^T X, dbias[n] = sum_m dz[m][n] (of the unrounded dz).
+ * The gradient of R is dY itself.  dX, dW and dbias may each be NULL (at least
+ * one is given); W is needed for dX, X for dW, Z for an activation.
+ */
+typedef struct sa_linear_bwd_desc {
+    int64_t M, N, K;
+    int32_t type;        /* SA_BF16 or SA_F16: dY, Z, X, W and dX */
+    int32_t dw_type;     /* type or SA_F32: dW */
+    int32_t act;
+    const void *dY;      /* [M, N] */
+    int64_t lddy;
+    const void *Z;       /* [M, N]; not read when act is SA_ACT_NONE */
+    int64_t ldz;
+    const void *X;       /* [M, K] */
+    int64_t ldx;
+    const void *W;       /* [N, K] */
+    int64_t ldw;
+    void *dX;            /* out [M, K] or NULL */
+    int64_t lddx;
+    void *dW;            /* out [N, K] or NULL */
+    int64_t lddw;
+    float *dbias;        /* out [N] or NULL */
+    void *ws;            /* structadmm_linear_bwd_workspace() bytes, 256-byte aligned */
+    size_t ws_bytes;
+} sa_linear_bwd_desc;
+
+size_t structadmm_linear_bwd_workspace(const sa_linear_bwd_desc *desc);
+int structadmm_linear_bwd(const sa_linear_bwd_desc *desc, hipStream_t stream);
+
+/* ---- gated pair of projections: structadmm_glu_fwd / _bwd ------------ */
+/*
+ * g = X Wg^T + bg, u = X Wu^T + bu, H = act(g) * u: X [M, K], Wg and Wu [N, K],
+ * H [M, N].  G and U, when given (both or neither), receive g and u for the
+ * backward pass.  H is computed from the unrounded g and u.
+ * Wg and Wu share one pitch; a neuron's two rows may lie side by side in one
+ * matrix [N, 2K] (Wu = Wg + K, ldw >= 2K), so that filter-wise pruning of that
+ * matrix keeps or drops whole neurons.
+ */
+typedef struct sa_glu_desc {
+    int64_t M, N, K;
+    int32_t type;        /* SA_BF16 or SA_F16: every matrix */
+    int32_t act;         /* sa_act */
+    const void *X;
+    int64_t ldx;
+    const void *Wg;
+    const void *Wu;
+    int64_t ldw;
+    const float *bg;     /* [N] or NULL */
+    const float *bu;     /* [N] or NULL */
+    void *H;             /* out */
+    int64_t ldh;
+    void *G;             /* out or NULL */
+    void *U;             /* out or NULL */
+    int64_t ldgu;        /* pitch of G and U */
+    void *ws;            /* structadmm_glu_workspace() bytes, 256-byte aligned */
+    size_t ws_bytes;
+} sa_glu_desc;
+
+size_t structadmm_glu_workspace(const sa_glu_desc *desc);
+int structadmm_glu_fwd(const sa_glu_desc *desc, hipStream_t stream);
+
+/*
+ * dg = dH * U * act'(G), du = dH * act(G), each rounded to type;
+ * dX = dg Wg + du Wu (one binary32 sum), dWg = dg^T X, dWu = du^T X,
+ * dbg[n] = sum_m dg[m][n], dbu[n] = sum_m du[m][n] (of the unrounded dg, du).
+ * dX, the pair dWg and dWu, and the biases may each be NULL (at least one output
+ * is given); Wg and Wu are needed for dX, X for dWg and dWu.  dWg and dWu share
+ * one pitch, as Wg and Wu do.
+ */
+typedef struct sa_glu_bwd_desc {
+    int64_t M, N, K;
+    int32_t type;        /* SA_BF16 or SA_F16: dH, G, U, X, Wg, Wu and dX */
+    int32_t dw_type;     /* type or SA_F32: dWg and dWu */
+    int32_t act;
+    const void *dH;      /* [M, N] */
+    int64_t lddh;
+    const void *G;       /* [M, N] */
+    const void *U;       /* [M, N] */
+    int64_t ldgu;
+    const void *X;       /* [M, K] */
+    int64_t ldx;
+    const void *Wg;      /* [N, K] */
+    const void *Wu;
+    int64_t ldw;
+    void *dX;            /* out [M, K] or NULL */
+    int64_t lddx;
+    void *dWg;           /* out [N, K] or NULL (both or neither) */
+    void *dWu;
+    int64_t lddw;
+    float *dbg;          /* out [N] or NULL */
+    float *dbu;          /* out [N] or NULL */
+    void *ws;            /* structadmm_glu_bwd_workspace() bytes, 256-byte aligned */
+    size_t ws_bytes;
+} sa_glu_bwd_desc;
+
+size_t structadmm_glu_bwd_workspace(const sa_glu_bwd_desc *desc);
+int structadmm_glu_bwd(const sa_glu_bwd_desc *desc, hipStream_t stream);
 
 /* Message describing the last error on the calling thread ("" if none). */
 const char *structadmm_last_error(void);

@@ -17,6 +17,13 @@ Entry points (same names as the C ABI):
   csr(Z, kept_idx, row_ptr=None, col=None, val=None, stream=None) -> (row_ptr, col, val)
   conv_sparse_workspace(Xp, shape, groups, stride, pad, nnz)
   conv_sparse_fwd(Xp, row_ptr, col, val, shape, groups, stride, pad, Y=None, ws=None, stream=None)
+  layer_norm_fwd(X, gamma=None, beta=None, eps=1e-5, ...) -> (Y, mean, rstd)
+  layer_norm_bwd(dY, X, mean, rstd, gamma=None, dR=None, ...) -> (dX, dgamma, dbeta)
+  linear_fwd(X, W, bias=None, R=None, act=ACT_NONE, ...) -> Y
+  linear_bwd(dY, X, W, Z=None, act=ACT_NONE, ...) -> (dX, dW, dbias)
+  glu_fwd(X, Wg, Wu, bg=None, bu=None, act=ACT_SILU, ...) -> H
+  glu_bwd(dH, X, Wg, Wu, G, U, act=ACT_SILU, ...) -> (dX, dWg, dWu, dbg, dbu)
+  compacted_matrix(Wc, sizes, group=0) -> the [M, K] matrix of a compacted layer
 """
 from __future__ import annotations
 
@@ -118,6 +125,53 @@ class SparseConvDesc(ctypes.Structure):
                 ("Y", _vp), ("ws", _vp), ("ws_bytes", ctypes.c_size_t), ("reuse_ws", ctypes.c_int32)]
 
 
+# element types and activations of the feed-forward operators
+BF16, F16, F32 = 0, 1, 2
+ACT_NONE, ACT_RELU, ACT_SIGMOID, ACT_SILU, ACT_GELU, ACT_GELU_TANH = range(6)
+ACTS = {"none": ACT_NONE, "relu": ACT_RELU, "sigmoid": ACT_SIGMOID, "silu": ACT_SILU, "gelu": ACT_GELU,
+        "gelu_tanh": ACT_GELU_TANH}
+MAX_LD = 1 << 21
+
+_i32, _i64, _sz = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
+
+
+class LayerNormDesc(ctypes.Structure):
+    _fields_ = [("rows", _i64), ("cols", _i64), ("type", _i32), ("eps", ctypes.c_float), ("X", _vp), ("ldx", _i64),
+                ("gamma", _vp), ("beta", _vp), ("Y", _vp), ("ldy", _i64), ("mean", _vp), ("rstd", _vp)]
+
+
+class LayerNormBwdDesc(ctypes.Structure):
+    _fields_ = [("rows", _i64), ("cols", _i64), ("type", _i32), ("dY", _vp), ("lddy", _i64), ("X", _vp), ("ldx", _i64),
+                ("mean", _vp), ("rstd", _vp), ("gamma", _vp), ("dR", _vp), ("lddr", _i64), ("dX", _vp),
+                ("lddx", _i64), ("dgamma", _vp), ("dbeta", _vp), ("ws", _vp), ("ws_bytes", _sz)]
+
+
+class LinearDesc(ctypes.Structure):
+    _fields_ = [("M", _i64), ("N", _i64), ("K", _i64), ("type", _i32), ("out_type", _i32), ("act", _i32), ("X", _vp),
+                ("ldx", _i64), ("W", _vp), ("ldw", _i64), ("bias", _vp), ("R", _vp), ("ldr", _i64), ("Y", _vp),
+                ("ldy", _i64), ("Z", _vp), ("ldz", _i64), ("ws", _vp), ("ws_bytes", _sz)]
+
+
+class LinearBwdDesc(ctypes.Structure):
+    _fields_ = [("M", _i64), ("N", _i64), ("K", _i64), ("type", _i32), ("dw_type", _i32), ("act", _i32), ("dY", _vp),
+                ("lddy", _i64), ("Z", _vp), ("ldz", _i64), ("X", _vp), ("ldx", _i64), ("W", _vp), ("ldw", _i64),
+                ("dX", _vp), ("lddx", _i64), ("dW", _vp), ("lddw", _i64), ("dbias", _vp), ("ws", _vp),
+                ("ws_bytes", _sz)]
+
+
+class GluDesc(ctypes.Structure):
+    _fields_ = [("M", _i64), ("N", _i64), ("K", _i64), ("type", _i32), ("act", _i32), ("X", _vp), ("ldx", _i64),
+                ("Wg", _vp), ("Wu", _vp), ("ldw", _i64), ("bg", _vp), ("bu", _vp), ("H", _vp), ("ldh", _i64),
+                ("G", _vp), ("U", _vp), ("ldgu", _i64), ("ws", _vp), ("ws_bytes", _sz)]
+
+
+class GluBwdDesc(ctypes.Structure):
+    _fields_ = [("M", _i64), ("N", _i64), ("K", _i64), ("type", _i32), ("dw_type", _i32), ("act", _i32), ("dH", _vp),
+                ("lddh", _i64), ("G", _vp), ("U", _vp), ("ldgu", _i64), ("X", _vp), ("ldx", _i64), ("Wg", _vp),
+                ("Wu", _vp), ("ldw", _i64), ("dX", _vp), ("lddx", _i64), ("dWg", _vp), ("dWu", _vp), ("lddw", _i64),
+                ("dbg", _vp), ("dbu", _vp), ("ws", _vp), ("ws_bytes", _sz)]
+
+
 class StructAdmmError(RuntimeError):
     pass
 
@@ -164,6 +218,17 @@ def lib():
         L.structadmm_conv_sparse_workspace.restype = ctypes.c_size_t
         L.structadmm_conv_sparse_fwd.argtypes = [ctypes.POINTER(SparseConvDesc), _vp]
         L.structadmm_conv_sparse_fwd.restype = ctypes.c_int
+        for name, cls in (("layer_norm_fwd", LayerNormDesc), ("layer_norm_bwd", LayerNormBwdDesc),
+                          ("linear_fwd", LinearDesc), ("linear_bwd", LinearBwdDesc), ("glu_fwd", GluDesc),
+                          ("glu_bwd", GluBwdDesc)):
+            f = getattr(L, f"structadmm_{name}")
+            f.argtypes = [ctypes.POINTER(cls), _vp]
+            f.restype = ctypes.c_int
+        for name, cls in (("layer_norm_bwd", LayerNormBwdDesc), ("linear", LinearDesc), ("linear_bwd", LinearBwdDesc),
+                          ("glu", GluDesc), ("glu_bwd", GluBwdDesc)):
+            f = getattr(L, f"structadmm_{name}_workspace")
+            f.argtypes = [ctypes.POINTER(cls)]
+            f.restype = ctypes.c_size_t
         L.structadmm_last_error.argtypes = []
         L.structadmm_last_error.restype = ctypes.c_char_p
         L.structadmm_version.argtypes = []
@@ -502,6 +567,263 @@ def conv_sparse_fwd(Xp, row_ptr, col, val, shape, groups: int, stride: int, pad:
     _check(lib().structadmm_conv_sparse_fwd(ctypes.byref(desc), _stream(stream)), "structadmm_conv_sparse_fwd")
     _keep_for_stream(stream, *temps)
     return Y
+
+
+# ------------------------------------------------------ feed-forward operators
+_type_codes = {}
+
+
+def _type_code(t, what: str) -> int:
+    """sa_type of a tensor: bfloat16 (or its bits as uint16, as compact writes them), float16 or float32."""
+    if not _type_codes:
+        import torch
+        _type_codes.update({torch.bfloat16: BF16, torch.uint16: BF16, torch.float16: F16, torch.float32: F32})
+    code = _type_codes.get(t.dtype)
+    if code is None:
+        raise StructAdmmError(f"{what}: unsupported type {t.dtype}")
+    return code
+
+
+def _matrix(t, rows: int, cols: int, code: int, dev, what: str) -> int:
+    """Checks a [rows, cols] matrix argument with unit column stride; its row pitch."""
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+        raise StructAdmmError(f"{what} must be [{rows}, {cols}], got {tuple(t.shape)}")
+    if t.device != dev:
+        raise StructAdmmError(f"{what} is on {t.device}, not {dev}")
+    if _type_code(t, what) != code:
+        raise StructAdmmError(f"{what} has type {t.dtype}, not the operands'")
+    ld, step = t.stride()
+    if step != 1 and cols > 1 and rows > 0:
+        raise StructAdmmError(f"{what} must have unit column stride")
+    if rows <= 1:
+        return max(ld, cols) if ld <= MAX_LD else cols  # a single row has no pitch
+    return ld
+
+
+def _vector(t, n: int, dev, what: str):
+    """Checks an optional float32 vector of n entries; its pointer."""
+    if t is None:
+        return None
+    if t.numel() != n or t.dim() != 1 or (n > 1 and t.stride(0) != 1) or t.device != dev \
+            or _type_code(t, what) != F32:
+        raise StructAdmmError(f"{what} must be float32 [{n}] on {dev}, contiguous")
+    return t.data_ptr()
+
+
+def _rows_of(X, what: str):
+    if X.dim() != 2 or not X.is_cuda:
+        raise StructAdmmError(f"{what} must be a matrix in GPU memory, got {tuple(X.shape)} on {X.device}")
+    return X.shape
+
+
+def _optional(t, rows, cols, code, dev, what):
+    """(pointer, pitch) of a matrix that may be None."""
+    return (None, cols) if t is None else (t.data_ptr(), _matrix(t, rows, cols, code, dev, what))
+
+
+def _new(like, rows: int, cols: int, dtype=None):
+    import torch
+    dtype = dtype or like.dtype
+    return torch.empty((rows, cols), dtype=torch.bfloat16 if dtype == torch.uint16 else dtype, device=like.device)
+
+
+def _run(desc, name: str, ws_fn, ws, like, stream, made):
+    """Gives the descriptor its workspace and makes the call."""
+    if ws_fn is not None:
+        if ws is None:
+            need = ws_fn(ctypes.byref(desc))
+            if need:
+                import torch
+                ws = torch.empty(need, dtype=torch.uint8, device=like.device)
+                made.append(ws)
+        if ws is not None:
+            desc.ws, desc.ws_bytes = ws.data_ptr(), ws.numel() * ws.element_size()
+    _check(getattr(lib(), name)(ctypes.byref(desc), _stream(stream)), name)
+    _keep_for_stream(stream, *made)
+
+
+def compacted_matrix(Wc, sizes: CompactSizes, group: int = 0):
+    """The compacted matrix of a conv group as a bfloat16 [M, K] view of Wc with
+    row pitch ldk: the W of linear_fwd and the Wg / Wu of glu_fwd."""
+    import torch
+    if not 0 <= group < sizes.groups:
+        raise StructAdmmError(f"compacted_matrix: group {group} outside [0, {sizes.groups})")
+    M, K, ldk, at = sizes.M[group], sizes.K[group], sizes.ldk[group], sizes.wc_offset[group]
+    return Wc.view(torch.bfloat16)[at:at + M * ldk].view(M, ldk)[:, :K]
+
+
+def layer_norm_fwd(X, gamma=None, beta=None, eps: float = 1e-5, Y=None, mean=None, rstd=None, stats: bool = True,
+                   stream=None):
+    """structadmm_layer_norm_fwd over the rows of X [rows, cols] (bfloat16, float16
+    or float32); returns (Y, mean, rstd).  mean and rstd, which the backward pass
+    reads, are None with stats=False."""
+    import torch
+    rows, cols = _rows_of(X, "layer_norm_fwd: X")
+    dev, code, made = X.device, _type_code(X, "layer_norm_fwd: X"), []
+    ldx = _matrix(X, rows, cols, code, dev, "layer_norm_fwd: X")
+    if Y is None:
+        Y = _new(X, rows, cols)
+        made.append(Y)
+    if stats and mean is None:
+        mean = torch.empty(rows, dtype=torch.float32, device=dev)
+        made.append(mean)
+    if stats and rstd is None:
+        rstd = torch.empty(rows, dtype=torch.float32, device=dev)
+        made.append(rstd)
+    d = LayerNormDesc(rows, cols, code, eps, X.data_ptr(), ldx, _vector(gamma, cols, dev, "layer_norm_fwd: gamma"),
+                      _vector(beta, cols, dev, "layer_norm_fwd: beta"), Y.data_ptr(),
+                      _matrix(Y, rows, cols, code, dev, "layer_norm_fwd: Y"),
+                      _vector(mean, rows, dev, "layer_norm_fwd: mean"),
+                      _vector(rstd, rows, dev, "layer_norm_fwd: rstd"))
+    _run(d, "structadmm_layer_norm_fwd", None, None, X, stream, made)
+    return Y, mean, rstd
+
+
+def layer_norm_bwd(dY, X, mean, rstd, gamma=None, dR=None, dX=None, dgamma=None, dbeta=None, params: bool = True,
+                   ws=None, stream=None):
+    """structadmm_layer_norm_bwd; returns (dX, dgamma, dbeta).  dR: the gradient
+    that reaches X past the norm, added to dX.  dgamma and dbeta are None with
+    params=False (unless given)."""
+    import torch
+    rows, cols = _rows_of(X, "layer_norm_bwd: X")
+    dev, code, made, w = X.device, _type_code(X, "layer_norm_bwd: X"), [], "layer_norm_bwd: "
+    if mean is None or rstd is None:
+        raise StructAdmmError(w + "mean and rstd of the forward pass are required")
+    if dX is None:
+        dX = _new(X, rows, cols)
+        made.append(dX)
+    if params and dgamma is None:
+        dgamma = torch.empty(cols, dtype=torch.float32, device=dev)
+        made.append(dgamma)
+    if params and dbeta is None:
+        dbeta = torch.empty(cols, dtype=torch.float32, device=dev)
+        made.append(dbeta)
+    r, ldr = _optional(dR, rows, cols, code, dev, w + "dR")
+    d = LayerNormBwdDesc(rows, cols, code, dY.data_ptr(), _matrix(dY, rows, cols, code, dev, w + "dY"), X.data_ptr(),
+                         _matrix(X, rows, cols, code, dev, w + "X"), _vector(mean, rows, dev, w + "mean"),
+                         _vector(rstd, rows, dev, w + "rstd"), _vector(gamma, cols, dev, w + "gamma"), r, ldr,
+                         dX.data_ptr(), _matrix(dX, rows, cols, code, dev, w + "dX"),
+                         _vector(dgamma, cols, dev, w + "dgamma"), _vector(dbeta, cols, dev, w + "dbeta"), None, 0)
+    _run(d, "structadmm_layer_norm_bwd", lib().structadmm_layer_norm_bwd_workspace, ws, X, stream, made)
+    return dX, dgamma, dbeta
+
+
+def linear_fwd(X, W, bias=None, R=None, act: int = ACT_NONE, Y=None, Z=None, out_dtype=None, ws=None, stream=None):
+    """structadmm_linear_fwd: Y = act(X W^T + bias) + R for X [M, K] and W [N, K]
+    (bfloat16 or float16); returns Y [M, N] (the operands' type, or float32 with
+    out_dtype=torch.float32 or a float32 Y; R has Y's type).  Z: receives the
+    pre-activations, which linear_bwd reads."""
+    M, K = _rows_of(X, "linear_fwd: X")
+    N, _ = _rows_of(W, "linear_fwd: W")
+    dev, code, made, w = X.device, _type_code(X, "linear_fwd: X"), [], "linear_fwd: "
+    if Y is None:
+        Y = _new(X, M, N, out_dtype)
+        made.append(Y)
+    out = _type_code(Y, w + "Y")
+    r, ldr = _optional(R, M, N, out, dev, w + "R")
+    z, ldz = _optional(Z, M, N, code, dev, w + "Z")
+    d = LinearDesc(M, N, K, code, out, act, X.data_ptr(), _matrix(X, M, K, code, dev, w + "X"), W.data_ptr(),
+                   _matrix(W, N, K, code, dev, w + "W"), _vector(bias, N, dev, w + "bias"), r, ldr, Y.data_ptr(),
+                   _matrix(Y, M, N, out, dev, w + "Y"), z, ldz, None, 0)
+    _run(d, "structadmm_linear_fwd", lib().structadmm_linear_workspace, ws, X, stream, made)
+    return Y
+
+
+def linear_bwd(dY, X, W, Z=None, act: int = ACT_NONE, dX=None, dW=None, dbias=None, grads: str = "xw", dw_dtype=None,
+               ws=None, stream=None):
+    """structadmm_linear_bwd; returns (dX, dW, dbias).  grads names the gradients to
+    make besides the buffers given: "x", "w" and "b" (the others are None).  dW is
+    float32 (the Gf of sgd_step) unless dw_dtype or a dW buffer says otherwise.
+    Z: the pre-activations (not needed for ACT_NONE)."""
+    import torch
+    M, K = _rows_of(X, "linear_bwd: X")
+    N, _ = _rows_of(W, "linear_bwd: W")
+    dev, code, made, w = X.device, _type_code(X, "linear_bwd: X"), [], "linear_bwd: "
+    if dX is None and "x" in grads:
+        dX = _new(X, M, K)
+        made.append(dX)
+    if dW is None and "w" in grads:
+        dW = _new(X, N, K, dw_dtype or torch.float32)
+        made.append(dW)
+    if dbias is None and "b" in grads:
+        dbias = torch.empty(N, dtype=torch.float32, device=dev)
+        made.append(dbias)
+    wcode = code if dW is None else _type_code(dW, w + "dW")
+    z, ldz = _optional(Z, M, N, code, dev, w + "Z")
+    dx, lddx = _optional(dX, M, K, code, dev, w + "dX")
+    dw, lddw = _optional(dW, N, K, wcode, dev, w + "dW")
+    d = LinearBwdDesc(M, N, K, code, wcode, act, dY.data_ptr(), _matrix(dY, M, N, code, dev, w + "dY"), z, ldz,
+                      X.data_ptr(), _matrix(X, M, K, code, dev, w + "X"), W.data_ptr(),
+                      _matrix(W, N, K, code, dev, w + "W"), dx, lddx, dw, lddw, _vector(dbias, N, dev, w + "dbias"),
+                      None, 0)
+    _run(d, "structadmm_linear_bwd", lib().structadmm_linear_bwd_workspace, ws, X, stream, made)
+    return dX, dW, dbias
+
+
+def _pair(A, B, rows, cols, code, dev, what):
+    """The one pitch of two matrices."""
+    a, b = _matrix(A, rows, cols, code, dev, what[0]), _matrix(B, rows, cols, code, dev, what[1])
+    if a != b and rows > 1:
+        raise StructAdmmError(f"{what[0]} and {what[1]} must have the same row pitch")
+    return a
+
+
+def glu_fwd(X, Wg, Wu, bg=None, bu=None, act: int = ACT_SILU, H=None, G=None, U=None, ws=None, stream=None):
+    """structadmm_glu_fwd: H = act(X Wg^T + bg) * (X Wu^T + bu) for X [M, K], Wg and
+    Wu [N, K] of one row pitch (bfloat16 or float16); returns H [M, N].  G and U
+    (both or neither) receive the two projections, which glu_bwd reads."""
+    M, K = _rows_of(X, "glu_fwd: X")
+    N, _ = _rows_of(Wg, "glu_fwd: Wg")
+    dev, code, made, w = X.device, _type_code(X, "glu_fwd: X"), [], "glu_fwd: "
+    if (G is None) != (U is None):
+        raise StructAdmmError(w + "give both G and U or neither")
+    if H is None:
+        H = _new(X, M, N)
+        made.append(H)
+    ldgu = N if G is None else _pair(G, U, M, N, code, dev, (w + "G", w + "U"))
+    d = GluDesc(M, N, K, code, act, X.data_ptr(), _matrix(X, M, K, code, dev, w + "X"), Wg.data_ptr(), Wu.data_ptr(),
+                _pair(Wg, Wu, N, K, code, dev, (w + "Wg", w + "Wu")), _vector(bg, N, dev, w + "bg"),
+                _vector(bu, N, dev, w + "bu"), H.data_ptr(), _matrix(H, M, N, code, dev, w + "H"), _ptr(G), _ptr(U),
+                ldgu, None, 0)
+    _run(d, "structadmm_glu_fwd", lib().structadmm_glu_workspace, ws, X, stream, made)
+    return H
+
+
+def glu_bwd(dH, X, Wg, Wu, G, U, act: int = ACT_SILU, dX=None, dWg=None, dWu=None, dbg=None, dbu=None,
+            grads: str = "xw", dw_dtype=None, ws=None, stream=None):
+    """structadmm_glu_bwd; returns (dX, dWg, dWu, dbg, dbu).  grads names the
+    gradients to make besides the buffers given: "x", "w" (dWg and dWu) and "b"
+    (dbg and dbu).  dWg and dWu are float32 views of one [N, 2K] matrix, neuron by
+    neuron, unless dw_dtype or buffers say otherwise."""
+    import torch
+    M, K = _rows_of(X, "glu_bwd: X")
+    N, _ = _rows_of(Wg, "glu_bwd: Wg")
+    dev, code, made, w = X.device, _type_code(X, "glu_bwd: X"), [], "glu_bwd: "
+    if (dWg is None) != (dWu is None):
+        raise StructAdmmError(w + "give both dWg and dWu or neither")
+    if dX is None and "x" in grads:
+        dX = _new(X, M, K)
+        made.append(dX)
+    if dWg is None and "w" in grads:
+        dW = _new(X, N, 2 * K, dw_dtype or torch.float32)
+        made.append(dW)
+        dWg, dWu = dW[:, :K], dW[:, K:]
+    if dbg is None and "b" in grads:
+        dbg = torch.empty(N, dtype=torch.float32, device=dev)
+        made.append(dbg)
+    if dbu is None and "b" in grads:
+        dbu = torch.empty(N, dtype=torch.float32, device=dev)
+        made.append(dbu)
+    wcode = code if dWg is None else _type_code(dWg, w + "dWg")
+    dx, lddx = _optional(dX, M, K, code, dev, w + "dX")
+    lddw = K if dWg is None else _pair(dWg, dWu, N, K, wcode, dev, (w + "dWg", w + "dWu"))
+    d = GluBwdDesc(M, N, K, code, wcode, act, dH.data_ptr(), _matrix(dH, M, N, code, dev, w + "dH"), G.data_ptr(),
+                   U.data_ptr(), _pair(G, U, M, N, code, dev, (w + "G", w + "U")), X.data_ptr(),
+                   _matrix(X, M, K, code, dev, w + "X"), Wg.data_ptr(), Wu.data_ptr(),
+                   _pair(Wg, Wu, N, K, code, dev, (w + "Wg", w + "Wu")), dx, lddx, _ptr(dWg), _ptr(dWu), lddw,
+                   _vector(dbg, N, dev, w + "dbg"), _vector(dbu, N, dev, w + "dbu"), None, 0)
+    _run(d, "structadmm_glu_bwd", lib().structadmm_glu_bwd_workspace, ws, X, stream, made)
+    return dX, dWg, dWu, dbg, dbu
 
 
 def version() -> str:

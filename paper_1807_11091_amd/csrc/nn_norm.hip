@@ -1,0 +1,457 @@
+// Layer norm over the rows of a matrix and its gradient.
+//
+//   forward   mean = sum x / n, rstd = (sum (x - mean)^2 / n + eps)^-1/2,
+//             y = (x - mean) rstd gamma + beta
+//   backward  with xn = (x - mean) rstd and t = dy gamma:
+//             dx = rstd (t - sum t / n - xn sum(t xn) / n) + dr,
+//             dgamma = sum over rows of dy xn, dbeta = sum over rows of dy
+//
+// Both are bound by HBM: the forward pass reads x and writes y, the backward pass
+// reads dy, x (and dr) and writes dx, each once.
+//
+// TPR threads hold one row in registers (CH vectors of 8 elements each), so the
+// row is read once and the variance is summed over x - mean, not as a difference
+// of two large sums.  Sums run in binary32 over at most 32 elements a thread and
+// then over the threads in a fixed tree.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+
+#include "nn_types.h"
+#include "sa_host.h"
+
+namespace sa {
+namespace {
+
+constexpr int kV = 8;  // elements per vector
+
+// Two sums over the TPR threads of a row, in a fixed order; every thread of the
+// row receives them.  Holds barriers when a row has several wavefronts.
+template <int TPR>
+__device__ inline void row_sums(float &a, float &b, float2 *tmp) {
+    a = wave_sum_f32(a);
+    b = wave_sum_f32(b);
+    if constexpr (TPR > 64) {
+        const int wave = threadIdx.x >> 6;
+        __syncthreads();  // the sums of the call before have been read
+        if ((threadIdx.x & 63) == 0) tmp[wave] = make_float2(a, b);
+        __syncthreads();
+        a = b = 0.0f;
+#pragma unroll
+        for (int w = 0; w < TPR / 64; ++w) {
+            const float2 t = tmp[w];
+            a += t.x;
+            b += t.y;
+        }
+    }
+}
+
+template <typename T>
+__device__ inline void load_chunk(const T *row, int c, int cols, float (&v)[kV]) {
+    if (c + kV <= cols) load_vec<T, kV>(row + c, v);
+    else load_part<T, kV>(row + c, cols - c, v);
+}
+
+template <typename T>
+__device__ inline void store_chunk(T *row, int c, int cols, const float (&v)[kV]) {
+    if (c + kV <= cols) store_vec<T, kV>(row + c, v);
+    else store_part<T, kV>(row + c, cols - c, v);
+}
+
+// gamma or beta of a chunk (`other` where the pointer is NULL or past the row)
+__device__ inline void load_param(const float *p, int c, int cols, float other, float (&v)[kV]) {
+#pragma unroll
+    for (int i = 0; i < kV; ++i) v[i] = other;
+    if (p && c < cols) load_chunk<float>(p, c, cols, v);
+}
+
+struct FwdArgs {
+    int64_t rows, ldx, ldy;
+    int cols;
+    float eps;
+    const void *X;
+    const float *gamma, *beta;
+    void *Y;
+    float *mean, *rstd;
+};
+
+template <typename T, int TPR, int CH>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_ln_fwd(FwdArgs a) {
+    constexpr int NT = TPR < 256 ? 256 : TPR, RPB = NT / TPR;
+    __shared__ float2 tmp[NT / 64];
+    const int t = threadIdx.x % TPR;
+    const int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
+    if (row >= a.rows) return;  // whole wavefronts, and whole workgroups where TPR >= 256
+    const T *x = reinterpret_cast<const T *>(a.X) + row * a.ldx;
+    const float n = (float)a.cols;
+    float v[CH][kV];
+    float s = 0.0f, q = 0.0f;
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+        const int c = (k * TPR + t) * kV;
+        if (c < a.cols) load_chunk<T>(x, c, a.cols, v[k]);
+        else
+#pragma unroll
+            for (int i = 0; i < kV; ++i) v[k][i] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kV; ++i) s += v[k][i];
+    }
+    row_sums<TPR>(s, q, tmp);
+    const float mean = s / n;
+    s = q = 0.0f;
+#pragma unroll
+    for (int k = 0; k < CH; ++k)
+#pragma unroll
+        for (int i = 0; i < kV; ++i) {
+            const float d = (k * TPR + t) * kV + i < a.cols ? v[k][i] - mean : 0.0f;
+            v[k][i] = d;
+            s = fmaf(d, d, s);
+        }
+    row_sums<TPR>(s, q, tmp);
+    const float rstd = 1.0f / sqrtf(s / n + a.eps);
+    if (t == 0) {
+        if (a.mean) a.mean[row] = mean;
+        if (a.rstd) a.rstd[row] = rstd;
+    }
+    T *y = reinterpret_cast<T *>(a.Y) + row * a.ldy;
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+        const int c = (k * TPR + t) * kV;
+        if (c >= a.cols) continue;
+        float g[kV], b[kV];
+        load_param(a.gamma, c, a.cols, 1.0f, g);
+        load_param(a.beta, c, a.cols, 0.0f, b);
+#pragma unroll
+        for (int i = 0; i < kV; ++i) g[i] = fmaf(v[k][i] * rstd, g[i], b[i]);
+        store_chunk<T>(y, c, a.cols, g);
+    }
+}
+
+// Rows longer than the registers hold: the row is read three times.
+template <typename T>
+__global__ __launch_bounds__(1024) void k_ln_fwd_long(FwdArgs a) {
+    constexpr int NT = 1024;
+    __shared__ float2 tmp[NT / 64];
+    const int64_t row = blockIdx.x;
+    const T *x = reinterpret_cast<const T *>(a.X) + row * a.ldx;
+    T *y = reinterpret_cast<T *>(a.Y) + row * a.ldy;
+    const float n = (float)a.cols;
+    float s = 0.0f, q = 0.0f, v[kV];
+    for (int c = threadIdx.x * kV; c < a.cols; c += NT * kV) {
+        load_chunk<T>(x, c, a.cols, v);
+#pragma unroll
+        for (int i = 0; i < kV; ++i) s += v[i];
+    }
+    row_sums<NT>(s, q, tmp);
+    const float mean = s / n;
+    s = q = 0.0f;
+    for (int c = threadIdx.x * kV; c < a.cols; c += NT * kV) {
+        load_chunk<T>(x, c, a.cols, v);
+#pragma unroll
+        for (int i = 0; i < kV; ++i) {
+            const float d = c + i < a.cols ? v[i] - mean : 0.0f;
+            s = fmaf(d, d, s);
+        }
+    }
+    row_sums<NT>(s, q, tmp);
+    const float rstd = 1.0f / sqrtf(s / n + a.eps);
+    if (threadIdx.x == 0) {
+        if (a.mean) a.mean[row] = mean;
+        if (a.rstd) a.rstd[row] = rstd;
+    }
+    for (int c = threadIdx.x * kV; c < a.cols; c += NT * kV) {
+        float g[kV], b[kV];
+        load_chunk<T>(x, c, a.cols, v);
+        load_param(a.gamma, c, a.cols, 1.0f, g);
+        load_param(a.beta, c, a.cols, 0.0f, b);
+#pragma unroll
+        for (int i = 0; i < kV; ++i) g[i] = fmaf((v[i] - mean) * rstd, g[i], b[i]);
+        store_chunk<T>(y, c, a.cols, g);
+    }
+}
+
+struct BwdArgs {
+    int64_t rows, lddy, ldx, lddr, lddx;
+    int cols;
+    const void *dY, *X;
+    const float *mean, *rstd, *gamma;
+    const void *dR;
+    void *dX;
+    float *part;  // [workgroups][2][cols]: sums of dy xn and of dy, or NULL
+};
+
+// Workgroup b takes the rows b * RPB + i, then those gridDim.x * RPB further on,
+// and keeps its columns' sums of dy xn and dy in registers.
+template <typename T, int TPR, int CH>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_ln_bwd(BwdArgs a) {
+    constexpr int NT = TPR < 256 ? 256 : TPR, RPB = NT / TPR;
+    __shared__ float2 tmp[NT / 64];
+    __shared__ float join[RPB > 1 ? RPB * TPR * kV : 1];
+    const int t = threadIdx.x % TPR, rg = threadIdx.x / TPR;
+    const float n = (float)a.cols;
+    float sg[CH][kV], sb[CH][kV];
+#pragma unroll
+    for (int k = 0; k < CH; ++k)
+#pragma unroll
+        for (int i = 0; i < kV; ++i) sg[k][i] = sb[k][i] = 0.0f;
+    for (int64_t row = (int64_t)blockIdx.x * RPB + rg; row < a.rows; row += (int64_t)gridDim.x * RPB) {
+        const T *x = reinterpret_cast<const T *>(a.X) + row * a.ldx;
+        const T *dy = reinterpret_cast<const T *>(a.dY) + row * a.lddy;
+        const float mean = a.mean[row], rstd = a.rstd[row];
+        float xn[CH][kV], d[CH][kV];
+        float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            const int c = (k * TPR + t) * kV;
+            float g[kV];
+#pragma unroll
+            for (int i = 0; i < kV; ++i) xn[k][i] = d[k][i] = 0.0f;
+            if (c < a.cols) {
+                load_chunk<T>(x, c, a.cols, xn[k]);
+                load_chunk<T>(dy, c, a.cols, d[k]);
+            }
+            load_param(a.gamma, c, a.cols, 1.0f, g);
+#pragma unroll
+            for (int i = 0; i < kV; ++i) {
+                xn[k][i] = c + i < a.cols ? (xn[k][i] - mean) * rstd : 0.0f;
+                sg[k][i] = fmaf(d[k][i], xn[k][i], sg[k][i]);
+                sb[k][i] += d[k][i];
+                d[k][i] *= g[i];
+                s1 += d[k][i];
+                s2 = fmaf(d[k][i], xn[k][i], s2);
+            }
+        }
+        if (!a.dX) continue;  // the same for every thread
+        row_sums<TPR>(s1, s2, tmp);
+        s1 /= n;
+        s2 /= n;
+        const T *dr = a.dR ? reinterpret_cast<const T *>(a.dR) + row * a.lddr : nullptr;
+        T *dx = reinterpret_cast<T *>(a.dX) + row * a.lddx;
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            const int c = (k * TPR + t) * kV;
+            if (c >= a.cols) continue;
+            float r[kV];
+#pragma unroll
+            for (int i = 0; i < kV; ++i) r[i] = 0.0f;
+            if (dr) load_chunk<T>(dr, c, a.cols, r);
+#pragma unroll
+            for (int i = 0; i < kV; ++i) r[i] += rstd * (d[k][i] - s1 - xn[k][i] * s2);
+            store_chunk<T>(dx, c, a.cols, r);
+        }
+    }
+    if (!a.part) return;
+    float *pg = a.part + (int64_t)blockIdx.x * 2 * a.cols;
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            float v[kV];
+#pragma unroll
+            for (int i = 0; i < kV; ++i) v[i] = half ? sb[k][i] : sg[k][i];
+            if constexpr (RPB > 1) {  // the row groups of the workgroup, in their order
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < kV; ++i) join[(rg * kV + i) * TPR + t] = v[i];
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < kV; ++i) {
+                    v[i] = 0.0f;
+                    for (int w = 0; w < RPB; ++w) v[i] += join[(w * kV + i) * TPR + t];
+                }
+            }
+            const int c = (k * TPR + t) * kV;
+            if (rg == 0 && c < a.cols) store_chunk<float>(pg + half * a.cols, c, a.cols, v);
+        }
+}
+
+// Rows longer than the registers hold: dX in three reads of the row.
+template <typename T>
+__global__ __launch_bounds__(1024) void k_ln_bwd_long(BwdArgs a) {
+    constexpr int NT = 1024;
+    __shared__ float2 tmp[NT / 64];
+    const float n = (float)a.cols;
+    const int64_t row = blockIdx.x;
+    const T *x = reinterpret_cast<const T *>(a.X) + row * a.ldx;
+    const T *dy = reinterpret_cast<const T *>(a.dY) + row * a.lddy;
+    const T *dr = a.dR ? reinterpret_cast<const T *>(a.dR) + row * a.lddr : nullptr;
+    T *dx = reinterpret_cast<T *>(a.dX) + row * a.lddx;
+    const float mean = a.mean[row], rstd = a.rstd[row];
+    float s1 = 0.0f, s2 = 0.0f, v[kV], d[kV], g[kV], r[kV];
+    for (int c = threadIdx.x * kV; c < a.cols; c += NT * kV) {
+        load_chunk<T>(x, c, a.cols, v);
+        load_chunk<T>(dy, c, a.cols, d);
+        load_param(a.gamma, c, a.cols, 1.0f, g);
+#pragma unroll
+        for (int i = 0; i < kV; ++i) {
+            const float xn = c + i < a.cols ? (v[i] - mean) * rstd : 0.0f;
+            s1 += d[i] * g[i];
+            s2 = fmaf(d[i] * g[i], xn, s2);
+        }
+    }
+    row_sums<NT>(s1, s2, tmp);
+    s1 /= n;
+    s2 /= n;
+    for (int c = threadIdx.x * kV; c < a.cols; c += NT * kV) {
+        load_chunk<T>(x, c, a.cols, v);
+        load_chunk<T>(dy, c, a.cols, d);
+        load_param(a.gamma, c, a.cols, 1.0f, g);
+#pragma unroll
+        for (int i = 0; i < kV; ++i) r[i] = 0.0f;
+        if (dr) load_chunk<T>(dr, c, a.cols, r);
+#pragma unroll
+        for (int i = 0; i < kV; ++i) r[i] += rstd * (d[i] * g[i] - s1 - (v[i] - mean) * rstd * s2);
+        store_chunk<T>(dx, c, a.cols, r);
+    }
+}
+
+// Their column sums: workgroup (x, y) takes 64 columns and every gridDim.y-th row.
+template <typename T>
+__global__ __launch_bounds__(64) void k_ln_params_long(BwdArgs a) {
+    const int c = blockIdx.x * 64 + threadIdx.x;
+    if (c >= a.cols) return;
+    float g = 0.0f, b = 0.0f;
+    for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
+        const float x = (float)reinterpret_cast<const T *>(a.X)[row * a.ldx + c];
+        const float dy = (float)reinterpret_cast<const T *>(a.dY)[row * a.lddy + c];
+        g = fmaf(dy, (x - a.mean[row]) * a.rstd[row], g);
+        b += dy;
+    }
+    float *p = a.part + (int64_t)blockIdx.y * 2 * a.cols;
+    p[c] = g;
+    p[a.cols + c] = b;
+}
+
+// dgamma and dbeta: the partial sums of n workgroups in their order, four
+// interleaved strands of them by four groups of 64 threads.
+__global__ __launch_bounds__(256) void k_ln_join(const float *part, int n, int cols, float *dgamma, float *dbeta) {
+    __shared__ float tmp[4][64];
+    const int c = blockIdx.x * 64 + (threadIdx.x & 63), w = threadIdx.x >> 6, half = blockIdx.y;
+    float *out = half ? dbeta : dgamma;
+    float s = 0.0f;
+    if (c < cols)
+        for (int b = w; b < n; b += 4) s += part[((int64_t)b * 2 + half) * cols + c];
+    tmp[w][threadIdx.x & 63] = s;
+    __syncthreads();
+    if (w == 0 && c < cols && out)
+        out[c] = (tmp[0][threadIdx.x] + tmp[1][threadIdx.x]) + (tmp[2][threadIdx.x] + tmp[3][threadIdx.x]);
+}
+
+constexpr int kMaxRegCols = 1024 * 4 * kV;  // the longest row held in registers
+constexpr int kParamGroups = 512;           // workgroups whose column sums are joined, at most
+
+// Calls f<TPR, CH>() for the narrowest shape that holds a row.
+template <typename F>
+void by_width(int cols, F &&f) {
+    const int v = (cols + kV - 1) / kV;
+    if (v <= 64) f.template operator()<64, 1>();
+    else if (v <= 128) f.template operator()<64, 2>();
+    else if (v <= 256) f.template operator()<256, 1>();
+    else if (v <= 512) f.template operator()<256, 2>();
+    else if (v <= 1024) f.template operator()<256, 4>();
+    else if (v <= 2048) f.template operator()<512, 4>();
+    else f.template operator()<1024, 4>();
+}
+
+template <typename T>
+struct LaunchFwd {
+    const FwdArgs &a;
+    hipStream_t stream;
+    template <int TPR, int CH>
+    void operator()() {
+        constexpr int NT = TPR < 256 ? 256 : TPR, RPB = NT / TPR;
+        hipLaunchKernelGGL((k_ln_fwd<T, TPR, CH>), dim3((unsigned)((a.rows + RPB - 1) / RPB)), dim3(NT), 0, stream, a);
+    }
+};
+
+template <typename T>
+struct LaunchBwd {
+    const BwdArgs &a;
+    int groups;
+    hipStream_t stream;
+    template <int TPR, int CH>
+    void operator()() {
+        constexpr int NT = TPR < 256 ? 256 : TPR;
+        hipLaunchKernelGGL((k_ln_bwd<T, TPR, CH>), dim3(groups), dim3(NT), 0, stream, a);
+    }
+};
+
+// Rows that one workgroup of the backward kernel holds at a time.
+int rows_per_group(int64_t cols) { return cols <= 64 * 2 * kV ? 4 : 1; }
+
+// Workgroups of the backward pass (0: no rows).
+int bwd_groups(int64_t rows, int64_t cols) {
+    const int rpb = rows_per_group(cols);
+    return (int)std::min<int64_t>((rows + rpb - 1) / rpb, kParamGroups);
+}
+
+template <typename T>
+int fwd(const FwdArgs &a, hipStream_t stream) {
+    if (a.cols <= kMaxRegCols) by_width(a.cols, LaunchFwd<T>{a, stream});
+    else hipLaunchKernelGGL(k_ln_fwd_long<T>, dim3((unsigned)a.rows), dim3(1024), 0, stream, a);
+    return check_hip(hipGetLastError(), "k_ln_fwd");
+}
+
+template <typename T>
+int bwd(const BwdArgs &a, int groups, hipStream_t stream) {
+    if (a.cols <= kMaxRegCols) {
+        by_width(a.cols, LaunchBwd<T>{a, groups, stream});
+        return check_hip(hipGetLastError(), "k_ln_bwd");
+    }
+    if (a.part)  // first: dX may overwrite dY
+        hipLaunchKernelGGL(k_ln_params_long<T>, dim3((a.cols + 63) / 64, groups), dim3(64), 0, stream, a);
+    if (a.dX) hipLaunchKernelGGL(k_ln_bwd_long<T>, dim3((unsigned)a.rows), dim3(1024), 0, stream, a);
+    return check_hip(hipGetLastError(), "k_ln_bwd_long");
+}
+
+}  // namespace
+}  // namespace sa
+
+using namespace sa;
+
+extern "C" int structadmm_layer_norm_fwd(const sa_layer_norm_desc *desc, hipStream_t stream) {
+    clear_error();
+    if (!desc) return fail(SA_E_ARG, "layer_norm_fwd: desc is required");
+    const sa_layer_norm_desc &d = *desc;
+    if (int rc = validate_layer_norm(d)) return rc;
+    if (d.rows == 0) return SA_OK;
+    const FwdArgs a{d.rows, d.ldx, d.ldy, (int)d.cols, d.eps, d.X, d.gamma, d.beta, d.Y, d.mean, d.rstd};
+    if (d.type == SA_BF16) return fwd<__bf16>(a, stream);
+    if (d.type == SA_F16) return fwd<_Float16>(a, stream);
+    return fwd<float>(a, stream);
+}
+
+static size_t ln_bwd_bytes(const sa_layer_norm_bwd_desc &d) {
+    return d.dgamma || d.dbeta ? (size_t)bwd_groups(d.rows, d.cols) * 2 * d.cols * sizeof(float) : 0;
+}
+
+extern "C" size_t structadmm_layer_norm_bwd_workspace(const sa_layer_norm_bwd_desc *desc) {
+    if (!desc || validate_layer_norm_bwd_sizes(*desc) != SA_OK) return 0;
+    return ln_bwd_bytes(*desc);
+}
+
+extern "C" int structadmm_layer_norm_bwd(const sa_layer_norm_bwd_desc *desc, hipStream_t stream) {
+    clear_error();
+    if (!desc) return fail(SA_E_ARG, "layer_norm_bwd: desc is required");
+    const sa_layer_norm_bwd_desc &d = *desc;
+    if (int rc = validate_layer_norm_bwd(d)) return rc;
+    const size_t need = ln_bwd_bytes(d);
+    if (int rc = check_workspace("layer_norm_bwd", d.ws, d.ws_bytes, need)) return rc;
+    const int groups = bwd_groups(d.rows, d.cols);
+    BwdArgs a{d.rows, d.lddy, d.ldx, d.lddr, d.lddx, (int)d.cols, d.dY, d.X, d.mean, d.rstd, d.gamma, d.dR, d.dX,
+              d.dgamma || d.dbeta ? static_cast<float *>(d.ws) : nullptr};
+    if (groups > 0) {
+        int rc;
+        if (d.type == SA_BF16) rc = bwd<__bf16>(a, groups, stream);
+        else if (d.type == SA_F16) rc = bwd<_Float16>(a, groups, stream);
+        else rc = bwd<float>(a, groups, stream);
+        if (rc) return rc;
+    }
+    if (d.dgamma || d.dbeta) {
+        hipLaunchKernelGGL(k_ln_join, dim3(((int)d.cols + 63) / 64, 2), dim3(256), 0, stream,
+                           static_cast<const float *>(d.ws), groups, (int)d.cols, d.dgamma, d.dbeta);
+        return check_hip(hipGetLastError(), "k_ln_join");
+    }
+    return SA_OK;
+}

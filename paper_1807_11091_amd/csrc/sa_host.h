@@ -35,6 +35,21 @@ int validate_dual(const sa_dual_desc &d, int i);
 int validate_sgd(const sa_sgd_desc &d, int i);
 int validate_compact(const sa_compact_desc &d);
 int validate_conv(const sa_conv_desc &d);
+// Feed-forward operators; the *_sizes forms leave out the checks of required
+// pointers (a workspace query may come before the buffers).
+int validate_layer_norm(const sa_layer_norm_desc &d);
+int validate_layer_norm_bwd_sizes(const sa_layer_norm_bwd_desc &d);
+int validate_layer_norm_bwd(const sa_layer_norm_bwd_desc &d);
+int validate_linear_sizes(const sa_linear_desc &d);
+int validate_linear(const sa_linear_desc &d);
+int validate_linear_bwd_sizes(const sa_linear_bwd_desc &d);
+int validate_linear_bwd(const sa_linear_bwd_desc &d);
+int validate_glu_sizes(const sa_glu_desc &d);
+int validate_glu(const sa_glu_desc &d);
+int validate_glu_bwd_sizes(const sa_glu_bwd_desc &d);
+int validate_glu_bwd(const sa_glu_bwd_desc &d);
+// ws holds `need` bytes and is 256-byte aligned (when need > 0)
+int check_workspace(const char *who, const void *ws, size_t have, size_t need);
 
 inline int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
