@@ -5,6 +5,7 @@
 #include <cstdint>
 #include <mutex>
 #include <set>
+#include <type_traits>
 #include <utility>
 
 #include "nn_gemm.h"
@@ -135,67 +136,68 @@ struct Side {
         else if constexpr (BK == 64) return NSIDE ? ((r >> 1) & 1) | ((r >> 3) & 3) << 1 : (r >> 1) & 7;
         else return NSIDE ? (r >> 3) & 3 : (r >> 2) & 3;
     }
-    // LDS row and source chunk of this lane's part of load i
-    __device__ static void place(int i, int wave, int lane, int &row, int &chunk) {
-        const int at = (i * NW + wave) * 64 + lane;
+    // This lane's LDS row in load 0 and its source chunk.  Load i lies `step` rows
+    // further on, a multiple of the swizzle's period: its chunk is the same.
+    static constexpr int step = NW * 64 / cpr;
+    static_assert(step % (ACROSS ? 16 : NSIDE ? 32 : 16) == 0 || loads == 1, "one chunk per lane");
+    __device__ static void place(int wave, int lane, int &row, int &chunk) {
+        const int at = wave * 64 + lane;
         row = at / cpr;
         const int c = at % cpr;
         chunk = ACROSS ? (((c >> 2) ^ swz(row)) << 2) | (c & 3) : c ^ swz(row);
     }
 
     uint32_t off[loads];  // byte offset of each load from the tile's origin
+    int kc;               // first k of this lane's chunk (rows along k)
 
     __device__ void setup(int64_t ld, int wave, int lane) {
+        int row, chunk;
+        place(wave, lane, row, chunk);
+        kc = chunk * 8;
 #pragma unroll
-        for (int i = 0; i < loads; ++i) {
-            int row, chunk;
-            place(i, wave, lane, row, chunk);
-            off[i] = (uint32_t)row * (uint32_t)ld * 2u + chunk * 16u;
-        }
+        for (int i = 0; i < loads; ++i) off[i] = (uint32_t)(row + i * step) * (uint32_t)ld * 2u + chunk * 16u;
     }
 
-    // Loads k0 .. k0 + BK of the rows at `p` (the tile's first row; `rows` of them
-    // in the matrix) to LDS at `lds`.  Rows past the matrix and k past K read as 0;
+    // The loads of one stage: k0 .. k0 + BK of the rows at p (the tile's first row;
+    // `rows` of them in the matrix).  Rows past the matrix and k past K read as 0;
     // a chunk that K cuts is completed by mend().  The buffer's range is rounded up
     // to whole chunks: the bytes past the matrix's end lie in the aligned 16 bytes
     // that hold its last element, and never reach a result.
-    __device__ void load(const T *p, int64_t ld, int64_t rows, int64_t K, int64_t k0, uint32_t lds, int wave, int lane) const {
-        const int r = uni((int)min(rows, (int64_t)B));
+    struct Stage {
+        i32x4 rs;
+        uint32_t so;
+        bool in;  // this lane's chunk begins below K
+    };
+    __device__ Stage stage(const T *p, int64_t ld, int rows, int K, int k0) const {
+        Stage st;
+        const int r = min(rows, B);
         if constexpr (ACROSS) {
-            const int n = uni((int)min(K - k0, (int64_t)BK));
+            const int n = min(K - k0, BK);
             const uint32_t range = (((uint32_t)(n - 1) * (uint32_t)ld + r) * 2u + 15u) & ~15u;
-            const i32x4 rs = buffer_at(reinterpret_cast<uint64_t>(p) + (uint64_t)(k0 * ld) * 2u, range);
-#pragma unroll
-            for (int i = 0; i < loads; ++i) dma16(rs, off[i], 0u, lds + (i * NW + wave) * 1024);
+            st.rs = buffer_at(reinterpret_cast<uint64_t>(p) + (uint64_t)k0 * (uint64_t)ld * 2u, range);
+            st.so = 0;
         } else {
             const uint32_t range = (((uint32_t)(r - 1) * (uint32_t)ld + (uint32_t)K) * 2u + 15u) & ~15u;
-            const i32x4 rs = buffer_at(reinterpret_cast<uint64_t>(p), range);
-            const uint32_t so = uni((int)(k0 * 2));
-            if (k0 + BK <= K) {
-#pragma unroll
-                for (int i = 0; i < loads; ++i) dma16(rs, off[i], so, lds + (i * NW + wave) * 1024);
-            } else {
-#pragma unroll
-                for (int i = 0; i < loads; ++i) {
-                    int row, chunk;
-                    place(i, wave, lane, row, chunk);
-                    dma16(rs, k0 + chunk * 8 < K ? off[i] : kInvalidOffset, so, lds + (i * NW + wave) * 1024);
-                }
-            }
+            st.rs = buffer_at(reinterpret_cast<uint64_t>(p), range);
+            st.so = uni(k0 * 2);
+            st.in = kc < K - k0;
         }
+        return st;
+    }
+    __device__ void load(const Stage &st, int i, uint32_t lds, int wave) const {
+        const uint32_t at = uni(lds + (i * NW + wave) * 1024);
+        if constexpr (ACROSS) dma16(st.rs, off[i], st.so, at);
+        else dma16(st.rs, st.in ? off[i] : kInvalidOffset, st.so, at);
     }
 
     // The chunk that holds k = K - 1 of a stage at k0, in LDS: its elements past K
     // become +0 (after this wavefront's loads have landed).
-    __device__ static void mend(uint8_t *lds, int64_t K, int64_t k0, int wave, int lane) {
+    __device__ void mend(uint8_t *lds, int K, int k0, int wave, int lane) const {
         if constexpr (!ACROSS) {
-            const int n = (int)(K - k0);  // valid k of the stage
-            if ((n & 7) == 0 || n > BK) return;
+            const int n = K - k0;  // valid k of the stage
+            if (kc != (n & ~7)) return;
 #pragma unroll
             for (int i = 0; i < loads; ++i) {
-                int row, chunk;
-                place(i, wave, lane, row, chunk);
-                if (chunk != n >> 3) continue;
                 vec *q = reinterpret_cast<vec *>(lds + (i * NW + wave) * 1024 + lane * 16);
                 vec v = *q;
 #pragma unroll
@@ -284,37 +286,52 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
     }
     constexpr int NROWS = GATED ? BN / 2 : BN;  // n of a tile
     const int64_t m0 = (int64_t)mt * BM, n0 = (int64_t)nt * NROWS;
-    const int sp = uni((int)((g.K + BK - 1) / BK)), ns = sp * g.parts;  // stages of a part, of all
+    const int K = uni((int)g.K), nrows = uni((int)min(g.N - n0, (int64_t)NROWS)), mrows = uni((int)min(g.M - m0, (int64_t)BM));
+    const int sp = (K + BK - 1) / BK, ns = sp * uni(g.parts);  // stages of a part, of all
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)smem;
 
-    NSide ns_;
-    MSide ms_;
-    ns_.setup(g.n[0].ld, wave, lane);
-    ms_.setup(g.m[0].ld, wave, lane);
-    ns_.setup_reads(lane);
-    ms_.setup_reads(lane);
+    NSide nside;
+    MSide mside;
+    nside.setup(g.n[0].ld, wave, lane);
+    mside.setup(g.m[0].ld, wave, lane);
+    nside.setup_reads(lane);
+    mside.setup_reads(lane);
     const int64_t nld = g.n[0].ld, mld = g.m[0].ld;  // parts and batches share their pitch
-    auto issue = [&](int st) {
-        const int part = st >= sp ? 1 : 0;
-        const int64_t k0 = (int64_t)(st - part * sp) * BK;
-        const uint32_t at = lds0 + (st % S) * Cfg::stage;
-        const T *np = reinterpret_cast<const T *>(part ? g.n[1].p : g.n[0].p) + (NA ? n0 : n0 * nld);
-        const T *mp = reinterpret_cast<const T *>(part | z ? g.m[1].p : g.m[0].p) + (MA ? m0 : m0 * mld);
-        ns_.load(np, nld, g.N - n0, g.K, k0, at, wave, lane);
-        if constexpr (GATED) {
-            const T *up = reinterpret_cast<const T *>(g.n[1].p) + (NA ? n0 : n0 * nld);
-            ns_.load(up, nld, g.N - n0, g.K, k0, at + NSide::bytes, wave, lane);
-        }
-        ms_.load(mp, mld, g.M - m0, g.K, k0, at + BN * BK * 2, wave, lane);
+    const T *np0 = reinterpret_cast<const T *>(g.n[0].p) + (NA ? n0 : n0 * nld);
+    const T *np1 = reinterpret_cast<const T *>(g.n[1].p) + (NA ? n0 : n0 * nld);
+    const T *mp0 = reinterpret_cast<const T *>(z ? g.m[1].p : g.m[0].p) + (MA ? m0 : m0 * mld);
+    const T *mp1 = reinterpret_cast<const T *>(g.m[1].p) + (MA ? m0 : m0 * mld);
+    // the loads of a stage, in the order of their issue
+    struct Loads {
+        typename NSide::Stage n, n1;
+        typename MSide::Stage m;
+        uint32_t at;
     };
-    auto mend = [&](int st) {
-        const int64_t k0 = (int64_t)(st >= sp ? st - sp : st) * BK;
-        uint8_t *at = smem + (st % S) * Cfg::stage;
-        NSide::mend(at, g.K, k0, wave, lane);
-        if constexpr (GATED) NSide::mend(at + NSide::bytes, g.K, k0, wave, lane);
-        MSide::mend(at + BN * BK * 2, g.K, k0, wave, lane);
+    auto stage = [&](int st, int slot) {
+        const bool second = st >= sp;
+        const int k0 = (second ? st - sp : st) * BK;
+        Loads l;
+        l.at = lds0 + slot * Cfg::stage;
+        l.n = nside.stage(second ? np1 : np0, nld, nrows, K, k0);
+        if constexpr (GATED) l.n1 = nside.stage(np1, nld, nrows, K, k0);
+        l.m = mside.stage(second ? mp1 : mp0, mld, mrows, K, k0);
+        return l;
     };
-    const bool cut = (g.K & 7) != 0;
+    auto load = [&](const Loads &l, int i) {
+        constexpr int NL = NSide::loads, NT = GATED ? 2 * NL : NL;
+        if (i < NL) nside.load(l.n, i, l.at, wave);
+        else if (GATED && i < NT) nside.load(l.n1, i - NL, l.at + NSide::bytes, wave);
+        else mside.load(l.m, i - NT, l.at + BN * BK * 2, wave);
+    };
+    const bool cut = (K & 7) != 0;
+    auto mend = [&](int st, int slot) {
+        const int k0 = (st >= sp ? st - sp : st) * BK;
+        if (!cut || k0 + BK < K) return;
+        uint8_t *at = smem + slot * Cfg::stage;
+        nside.mend(at, K, k0, wave, lane);
+        if constexpr (GATED) nside.mend(at + NSide::bytes, K, k0, wave, lane);
+        mside.mend(at + BN * BK * 2, K, k0, wave, lane);
+    };
 
     f32x4 acc[TN][TM];
 #pragma unroll
@@ -325,15 +342,19 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
     if (ns > 0) {
         const int nrow = wn * (BN / WN) / (GATED ? 2 : 1), mrow = wm * (BM / WM);
         auto readn = [&](const uint8_t *st, int i, int q) {
-            if constexpr (GATED) return ns_.read(st + (i >= TNG ? NSide::bytes : 0), nrow, i % TNG, q);
-            else return ns_.read(st, nrow, i, q);
+            if constexpr (GATED) return nside.read(st + (i >= TNG ? NSide::bytes : 0), nrow, i % TNG, q);
+            else return nside.read(st, nrow, i, q);
         };
-        auto readm = [&](const uint8_t *st, int j, int q) { return ms_.read(st + BN * BK * 2, mrow, j, q); };
-        for (int s = 0; s < S && s < ns; ++s) issue(s);
+        auto readm = [&](const uint8_t *st, int j, int q) { return mside.read(st + BN * BK * 2, mrow, j, q); };
+        for (int s = 0; s < S && s < ns; ++s) {
+            const Loads l = stage(s, s);
+#pragma unroll
+            for (int i = 0; i < L; ++i) load(l, i);
+        }
         // stage 0 has landed when at most the later ones are outstanding
         if (ns >= S) wait_vm<L *(S - 1)>();
         else wait_vm<0>();
-        if (cut && sp == 1) mend(0);
+        mend(0, 0);
         lds_barrier();
         vec fa[TN], fb[2][TM];
 #pragma unroll
@@ -341,35 +362,51 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
 #pragma unroll
         for (int i = 0; i < TN; ++i) fa[i] = readn(smem, i, 0);
         int slot = 0;
-        for (int s = 0; s < ns; ++s) {
+        // Stage s is multiplied; in its last step the fragments of stage s + 1 are read
+        // (MORE) and stage s + S is loaded into this one's buffer (FULL).
+        auto multiply = [&](int s, auto more, auto full) {
+            constexpr bool MORE = decltype(more)::value, FULL = decltype(full)::value;
             const uint8_t *cur = smem + slot * Cfg::stage;
+            const int here = slot;
             slot = slot + 1 == S ? 0 : slot + 1;
             const uint8_t *nxt = smem + slot * Cfg::stage;
-            const bool more = s + 1 < ns;
+            Loads l;
+            if constexpr (FULL) l = stage(s + S, here);
 #pragma unroll
             for (int q = 0; q < KS; ++q) {
                 const bool last = q == KS - 1;
                 const uint8_t *from = last ? nxt : cur;
                 const int fq = last ? 0 : q + 1;
+                constexpr int HOLD = 1;  // rows multiplied before the barrier
 #pragma unroll
                 for (int i = 0; i < TN; ++i) {
+                    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
                     for (int j = 0; j < TM; ++j) acc[i][j] = mfma(fa[i], fb[q & 1][j], acc[i][j]);
-                    if (i == 1 && last && more) {
+                    __builtin_amdgcn_s_setprio(0);
+                    if (i == HOLD && last && MORE) {
                         // the next stage has landed, this one has been read by all
-                        if (s + S <= ns) wait_vm<L *(S - 2)>();
+                        if constexpr (FULL) wait_vm<L *(S - 2)>();
                         else wait_vm<0>();
-                        if (cut && (s + 1 == sp - 1 || s + 1 == ns - 1)) mend(s + 1);
+                        mend(s + 1, slot);
                         lds_barrier();
-                        if (s + S < ns) issue(s + S);
                     }
-                    if (i >= 1 && (!last || more)) {
-                        if (i == 1) {
+                    if (i >= HOLD && (!last || MORE)) {
+                        if (i == HOLD) {
 #pragma unroll
                             for (int j = 0; j < TM; ++j) fb[(q + 1) & 1][j] = readm(from, j, fq);
-                            fa[0] = readn(from, 0, fq);
+#pragma unroll
+                            for (int h = 0; h < HOLD; ++h) fa[h] = readn(from, h, fq);
                         }
                         fa[i] = readn(from, i, fq);
+                    }
+                    if constexpr (FULL) {
+                        if (last && i >= HOLD) {  // the loads, spread over the remaining rows
+                            constexpr int per = (L + TN - HOLD - 1) / (TN - HOLD);
+#pragma unroll
+                            for (int e = 0; e < per; ++e)
+                                if ((i - HOLD) * per + e < L) load(l, (i - HOLD) * per + e);
+                        }
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
@@ -378,7 +415,11 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
 #pragma unroll
                 for (int j = 0; j < TM; ++j) fb[0][j] = fb[1][j];
             }
-        }
+        };
+        int s = 0;
+        for (; s + S < ns; ++s) multiply(s, std::true_type{}, std::true_type{});
+        for (; s + 1 < ns; ++s) multiply(s, std::true_type{}, std::false_type{});
+        multiply(s, std::false_type{}, std::false_type{});
     }
 
     // The sums go through LDS, 16 rows of each wavefront at a time, and out in
@@ -386,9 +427,8 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
     float *sc = reinterpret_cast<float *>(smem);
     constexpr int CP = Cfg::cpitch, CHUNKS = NROWS / 8;
     void *Y = z ? g.y1 : g.e.Y;
-#pragma unroll
-    for (int j = 0; j < TM; ++j) {
-        lds_barrier();
+    auto stage_sums = [&](auto jc) {
+        constexpr int j = decltype(jc)::value;
 #pragma unroll
         for (int i = 0; i < TN; ++i) {
             const int f = GATED ? i % TNG : i;
@@ -396,6 +436,15 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
                           8 * (lane >> 4) + 4 * (f & 1);
             *reinterpret_cast<f32x4 *>(sc + (wm * 16 + (lane & 15)) * CP + n) = acc[i][j];
         }
+    };
+    static_assert(TM == 4, "the passes below");
+#pragma unroll 1
+    for (int j = 0; j < TM; ++j) {
+        lds_barrier();
+        if (j == 0) stage_sums(std::integral_constant<int, 0>{});
+        else if (j == 1) stage_sums(std::integral_constant<int, 1>{});
+        else if (j == 2) stage_sums(std::integral_constant<int, 2>{});
+        else stage_sums(std::integral_constant<int, 3>{});
         lds_barrier();
         for (int c = tid; c < Cfg::rows * CHUNKS; c += Cfg::NT) {
             const int r = c / CHUNKS, nl = (c - r * CHUNKS) * 8;
