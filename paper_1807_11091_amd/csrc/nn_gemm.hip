@@ -3,8 +3,8 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <map>
 #include <mutex>
-#include <set>
 #include <type_traits>
 #include <utility>
 
@@ -25,13 +25,9 @@ __device__ inline f32x4 mfma(Vec8<_Float16>::type a, Vec8<_Float16>::type b, f32
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
 
-// Eight (n < 8 at a row's end) consecutive outputs from their sums.
-template <typename T>
-__device__ inline void finish8(const Epilogue &e, bool gated, void *Y, int64_t m, int64_t n, int cnt, const float *s,
-                               const float *s2) {
-    float z[8], u[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) z[i] = s[i];
+// Eight (cnt < 8 at a row's end) consecutive outputs from their sums z (and u).
+template <typename T, bool GATED>
+__device__ inline void finish8(const Epilogue &e, void *Y, int64_t m, int64_t n, int cnt, float (&z)[8], float (&u)[8]) {
     auto add = [&](const float *b, float (&v)[8]) {
         float t[8];
         if (cnt == 8) load_vec<float, 8>(b + n, t);
@@ -48,9 +44,7 @@ __device__ inline void finish8(const Epilogue &e, bool gated, void *Y, int64_t m
     if (e.act != SA_ACT_NONE)
 #pragma unroll
         for (int i = 0; i < 8; ++i) z[i] = act_value(e.act, z[i]);
-    if (gated) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) u[i] = s2[i];
+    if constexpr (GATED) {
         if (e.bias2) add(e.bias2, u);
         if (e.Z2) put(e.Z2, m * e.ldz + n, u);
 #pragma unroll
@@ -79,15 +73,14 @@ __device__ inline void finish8(const Epilogue &e, bool gated, void *Y, int64_t m
 // buffer_load ... lds (16 bytes per lane, S - 1 stages ahead).  The N side is the
 // row operand of the MFMAs, so a lane's four sums are consecutive in n.
 //
-// LDS layouts (bank conflicts: 64 banks of 4 bytes):
+// LDS layouts (64 banks of 4 bytes, 256 bytes per clock):
 //   - an operand whose rows run along k: [row][BK], the 16-byte chunks of a row
-//     XOR-swizzled so that the 16 rows of one fragment read hit 16 distinct chunks;
+//     XOR-swizzled so that the 16 rows of a fragment read hit 16 distinct chunks;
 //   - an operand whose rows run across k: [k][rows], read by ds_read_b64_tr_b16,
 //     which hands each lane 4 consecutive k of its row (16 lanes transpose a block
-//     of 4 k by 16 rows); its 64-byte units are XOR-swizzled by k.
+//     of 4 k by 16 rows); its 32-byte units are XOR-swizzled by k, so that 8 k of
+//     one unit hit distinct banks.
 // The swizzle is applied to the source address (the DMA writes lanes in order).
-// Rows of the N side are dealt to fragments so that two fragments hold 8
-// consecutive n in each lane.
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -120,42 +113,42 @@ __device__ inline void wait_vm() {
 __device__ inline void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // One operand's part of a stage: B rows by BK k, NW wavefronts.
-template <typename T, bool ACROSS, bool NSIDE, int B, int BK, int NW>
+template <typename T, bool ACROSS, int B, int BK, int NW>
 struct Side {
     typedef typename Vec8<T>::type vec;
     static constexpr int bytes = B * BK * 2;
     static constexpr int loads = bytes / 1024 / NW;  // per wavefront
     static constexpr int pitch = ACROSS ? B * 2 : BK * 2;
     static constexpr int cpr = pitch / 16;           // 16-byte chunks of an LDS row
-    static constexpr int units = B / 32;             // 64-byte units of a k (ACROSS)
     static_assert(bytes % (1024 * NW) == 0, "whole loads per wavefront");
 
     // swizzle of row r (rows along k) or of k (rows across)
     __device__ static int swz(int r) {
-        if constexpr (ACROSS) return ((r & 3) | ((r >> 3) & 1) << 2) & (units - 1);
-        else if constexpr (BK == 64) return NSIDE ? ((r >> 1) & 1) | ((r >> 3) & 3) << 1 : (r >> 1) & 7;
-        else return NSIDE ? (r >> 3) & 3 : (r >> 2) & 3;
+        if constexpr (ACROSS) return (r & 3) | ((r >> 3) & 1) << 2;
+        else if constexpr (BK == 64) return (r >> 1) & 7;
+        else return (((r >> 2) ^ (r >> 3)) & 1) << 1 | ((r >> 3) & 1);
     }
-    // This lane's LDS row in load 0 and its source chunk.  Load i lies `step` rows
-    // further on, a multiple of the swizzle's period: its chunk is the same.
-    static constexpr int step = NW * 64 / cpr;
-    static_assert(step % (ACROSS ? 16 : NSIDE ? 32 : 16) == 0 || loads == 1, "one chunk per lane");
-    __device__ static void place(int wave, int lane, int &row, int &chunk) {
-        const int at = wave * 64 + lane;
+    // LDS row and source chunk of this lane's part of load i.  Where rows run along
+    // k the loads lie a multiple of the swizzle's period apart: one chunk for all.
+    static_assert(ACROSS || NW * 64 / cpr % 16 == 0 || loads == 1, "one chunk per lane");
+    __device__ static void place(int i, int wave, int lane, int &row, int &chunk) {
+        const int at = (i * NW + wave) * 64 + lane;
         row = at / cpr;
         const int c = at % cpr;
-        chunk = ACROSS ? (((c >> 2) ^ swz(row)) << 2) | (c & 3) : c ^ swz(row);
+        chunk = ACROSS ? (((c >> 1) ^ swz(row)) << 1) | (c & 1) : c ^ swz(row);
     }
 
     uint32_t off[loads];  // byte offset of each load from the tile's origin
-    int kc;               // first k of this lane's chunk (rows along k)
+    int kc;               // first k of this lane's chunks (rows along k)
 
     __device__ void setup(int64_t ld, int wave, int lane) {
-        int row, chunk;
-        place(wave, lane, row, chunk);
-        kc = chunk * 8;
 #pragma unroll
-        for (int i = 0; i < loads; ++i) off[i] = (uint32_t)(row + i * step) * (uint32_t)ld * 2u + chunk * 16u;
+        for (int i = 0; i < loads; ++i) {
+            int row, chunk;
+            place(i, wave, lane, row, chunk);
+            off[i] = (uint32_t)row * (uint32_t)ld * 2u + chunk * 16u;
+            if (i == 0) kc = chunk * 8;
+        }
     }
 
     // The loads of one stage: k0 .. k0 + BK of the rows at p (the tile's first row;
@@ -173,13 +166,13 @@ struct Side {
         const int r = min(rows, B);
         if constexpr (ACROSS) {
             const int n = min(K - k0, BK);
-            const uint32_t range = (((uint32_t)(n - 1) * (uint32_t)ld + r) * 2u + 15u) & ~15u;
+            const uint32_t range = rows > 0 ? (((uint32_t)(n - 1) * (uint32_t)ld + r) * 2u + 15u) & ~15u : 0u;
             st.rs = buffer_at(reinterpret_cast<uint64_t>(p) + (uint64_t)k0 * (uint64_t)ld * 2u, range);
             st.so = 0;
         } else {
-            const uint32_t range = (((uint32_t)(r - 1) * (uint32_t)ld + (uint32_t)K) * 2u + 15u) & ~15u;
+            const uint32_t range = rows > 0 ? (((uint32_t)(r - 1) * (uint32_t)ld + (uint32_t)K) * 2u + 15u) & ~15u : 0u;
             st.rs = buffer_at(reinterpret_cast<uint64_t>(p), range);
-            st.so = uni(k0 * 2);
+            st.so = rows > 0 ? uni(k0 * 2) : 0;
             st.in = kc < K - k0;
         }
         return st;
@@ -208,8 +201,7 @@ struct Side {
         }
     }
 
-    // Lane offsets of fragment reads.  Fragment f holds 16 rows: rows 16 f + (0 .. 15)
-    // of the M side, rows 32 (f / 2) + 4 (f % 2) + {0-3, 8-11, 16-19, 24-27} of the N side.
+    // Lane offsets of fragment reads: fragment f holds rows 16 f + (0 .. 15).
     static constexpr int nfo = ACROSS ? 1 : BK / 32;
     uint32_t fo[nfo];
 
@@ -217,20 +209,18 @@ struct Side {
         const int r = lane & 15, g = lane >> 4;
         if constexpr (ACROSS) {
             const int k = g * 8 + (r >> 2), piece = lane & 3;
-            fo[0] = k * pitch + (swz(k) << 6) + piece * (NSIDE ? 16 : 8);
+            fo[0] = k * pitch + (swz(k) << 5) + piece * 8;
         } else {
-            const int row = NSIDE ? 8 * (r >> 2) + (r & 3) : r;
 #pragma unroll
-            for (int q = 0; q < BK / 32; ++q) fo[q] = row * pitch + (((q * 4 + g) ^ swz(row)) << 4);
+            for (int q = 0; q < BK / 32; ++q) fo[q] = r * pitch + (((q * 4 + g) ^ swz(r)) << 4);
         }
     }
 
-    // fragment f (rows from `row0`, a multiple of 32) of k step q
+    // fragment f (rows from row0, a multiple of 16) of k step q
     __device__ vec read(const uint8_t *lds, int row0, int f, int q) const {
         if constexpr (ACROSS) {
             typedef __attribute__((address_space(3))) s16x4 *ptr;
-            const int unit = row0 / 32 + (f >> 1);
-            const uint8_t *p = lds + (fo[0] ^ (unit << 6)) + (f & 1) * (NSIDE ? 8 : 32) + q * 32 * pitch;
+            const uint8_t *p = lds + (fo[0] ^ (uint32_t)((row0 / 16 + f) << 5)) + q * 32 * pitch;
             union {
                 s16x4 h[2];
                 vec v;
@@ -239,8 +229,7 @@ struct Side {
             x.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ptr)(p + 4 * pitch));
             return x.v;
         } else {
-            const int at = NSIDE ? 32 * (f >> 1) + 4 * (f & 1) : 16 * f;
-            return *reinterpret_cast<const vec *>(lds + fo[q] + (row0 + at) * pitch);
+            return *reinterpret_cast<const vec *>(lds + fo[q] + (row0 + 16 * f) * pitch);
         }
     }
 };
@@ -250,83 +239,130 @@ struct TileCfg {
     static constexpr int NW = WN * WM, NT = NW * 64;
     static constexpr int TN = BN / WN / 16, TM = BM / WM / 16;  // fragments of a wavefront
     static constexpr int stage = (BN + BM) * BK * 2;
-    static constexpr int rows = 16 * WM;                        // rows of an epilogue pass
-    static constexpr int cpitch = BN + 4;                       // its pitch in binary32
-    static constexpr int lds = S * stage > rows * cpitch * 4 ? S * stage : rows * cpitch * 4;
+    static constexpr int lds = S * stage;
     static_assert(lds <= kMaxLds, "LDS");
 };
 
+// f(j) with j, below N, as a constant: registers cannot be indexed
+template <int N, typename F>
+__device__ inline void pick(int j, F &&f) {
+    if constexpr (N > 0) {
+        if (j == N - 1) f(std::integral_constant<int, N - 1>{});
+        else pick<N - 1>(j, f);
+    }
+}
+
 struct TileArgs {
     Gemm g;
-    int mtiles, ntiles;
+    int mtiles, ntiles, tiles, groups;  // tiles: of all batches; groups: workgroups
 };
 
 template <typename T, bool NA, bool MA, bool GATED, int BN, int BM, int WN, int WM, int BK, int S>
 __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
     using Cfg = TileCfg<BN, BM, WN, WM, BK, S>;
-    using NSide = Side<T, NA, true, GATED ? BN / 2 : BN, BK, Cfg::NW>;  // gated: one half per projection
-    using MSide = Side<T, MA, false, BM, BK, Cfg::NW>;
+    constexpr int NROWS = GATED ? BN / 2 : BN;  // n of a tile; gated: one half of the N side per projection
+    using NSide = Side<T, NA, NROWS, BK, Cfg::NW>;
+    using MSide = Side<T, MA, BM, BK, Cfg::NW>;
     typedef typename Vec8<T>::type vec;
     constexpr int TN = Cfg::TN, TM = Cfg::TM, KS = BK / 32, TNG = GATED ? TN / 2 : TN;
-    constexpr int L = NSide::loads * (GATED ? 2 : 1) + MSide::loads;
+    constexpr int NL = NSide::loads * (GATED ? 2 : 1), L = NL + MSide::loads;  // loads of a stage
+    static_assert(KS == 2 && TNG % 2 == 0 && L * (S - 1) < 64, "shape");
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
 
     const Gemm &g = a.g;
     const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
     const int wn = wave % WN, wm = wave / WN;
-    const int z = blockIdx.z;
-    // XCD x walks one contiguous range of tiles; within it, bands of 8 M tiles
-    int mt, nt;
-    {
-        const int t = xcd_remap(blockIdx.x, a.mtiles * a.ntiles);
+
+    // Workgroup b runs on XCD b mod 8, which walks one contiguous range of tiles
+    // (its own L2); its workgroups take the range's tiles in turn.
+    const int xcd = blockIdx.x & 7, local = blockIdx.x >> 3;
+    const int per = a.tiles >> 3, extra = a.tiles & 7;
+    const int first = uni(xcd * per + min(xcd, extra) + local);
+    const int end = uni((xcd + 1) * per + min(xcd + 1, extra));
+    const int stride = uni((a.groups >> 3) + (xcd < (a.groups & 7) ? 1 : 0));
+    if (first >= end) return;
+    const int mine = (end - first + stride - 1) / stride;  // tiles of this workgroup
+
+    const int K = uni((int)g.K);
+    const int sp = (K + BK - 1) / BK, ns = NA && !MA ? sp * uni(g.parts) : sp;  // stages of a part, of a tile
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)smem;
+    const int64_t nld = g.n[0].ld, mld = g.m[0].ld;  // parts and batches share their pitch
+
+    // A tile: bands of 8 M tiles, down each band first, so that neighbours share operands
+    struct Tile {
+        int64_t m0, n0;
+        int z;
+    };
+    auto tile_at = [&](int i) {
+        int t = first + i * stride;
+        const int one = a.mtiles * a.ntiles;
+        Tile q;
+        q.z = t / one;
+        t -= q.z * one;
         const int band = t / (8 * a.ntiles), in = t - band * 8 * a.ntiles;
         const int h = min(8, a.mtiles - band * 8);
-        mt = uni(band * 8 + in % h);
-        nt = uni(in / h);
-    }
-    constexpr int NROWS = GATED ? BN / 2 : BN;  // n of a tile
-    const int64_t m0 = (int64_t)mt * BM, n0 = (int64_t)nt * NROWS;
-    const int K = uni((int)g.K), nrows = uni((int)min(g.N - n0, (int64_t)NROWS)), mrows = uni((int)min(g.M - m0, (int64_t)BM));
-    const int sp = (K + BK - 1) / BK, ns = sp * uni(g.parts);  // stages of a part, of all
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)smem;
+        q.m0 = (int64_t)(band * 8 + in % h) * BM;
+        q.n0 = (int64_t)(in / h) * NROWS;
+        return q;
+    };
 
     NSide nside;
     MSide mside;
-    nside.setup(g.n[0].ld, wave, lane);
-    mside.setup(g.m[0].ld, wave, lane);
+    nside.setup(nld, wave, lane);
+    mside.setup(mld, wave, lane);
     nside.setup_reads(lane);
     mside.setup_reads(lane);
-    const int64_t nld = g.n[0].ld, mld = g.m[0].ld;  // parts and batches share their pitch
-    const T *np0 = reinterpret_cast<const T *>(g.n[0].p) + (NA ? n0 : n0 * nld);
-    const T *np1 = reinterpret_cast<const T *>(g.n[1].p) + (NA ? n0 : n0 * nld);
-    const T *mp0 = reinterpret_cast<const T *>(z ? g.m[1].p : g.m[0].p) + (MA ? m0 : m0 * mld);
-    const T *mp1 = reinterpret_cast<const T *>(g.m[1].p) + (MA ? m0 : m0 * mld);
-    // the loads of a stage, in the order of their issue
+
+    // The loads run over the stages of all tiles without a break, S stages ahead of
+    // the products: the next tile's first stages arrive while this one's results go out.
     struct Loads {
         typename NSide::Stage n, n1;
         typename MSide::Stage m;
         uint32_t at;
     };
-    auto stage = [&](int st, int slot) {
-        const bool second = st >= sp;
-        const int k0 = (second ? st - sp : st) * BK;
+    constexpr bool TWO = NA && !MA;  // the sum may have two parts (MA: there may be two batches)
+    const T *np0, *np1 = nullptr, *mp0, *mp1 = nullptr;
+    int nrows, mrows, ltile = 0, lstage = 0, lslot = 0;
+    auto enter = [&](int i) {
+        const Tile q = tile_at(i);
+        const int64_t no = NA ? q.n0 : q.n0 * nld, mo = MA ? q.m0 : q.m0 * mld;
+        np0 = reinterpret_cast<const T *>(g.n[0].p) + no;
+        if constexpr (GATED || TWO) np1 = reinterpret_cast<const T *>(g.n[1].p) + no;
+        mp0 = reinterpret_cast<const T *>(MA && q.z ? g.m[1].p : g.m[0].p) + mo;
+        if constexpr (TWO) mp1 = reinterpret_cast<const T *>(g.m[1].p) + mo;
+        nrows = uni((int)min(g.N - q.n0, (int64_t)NROWS));
+        mrows = uni((int)min(g.M - q.m0, (int64_t)BM));
+    };
+    auto next_loads = [&]() {
+        if (ltile >= mine) {  // past the last stage: rows 0, the loads write zeros that are not used
+            nrows = 0;
+            mrows = 0;
+        }
+        const bool second = TWO && lstage >= sp;
+        const int k0 = (second ? lstage - sp : lstage) * BK;
         Loads l;
-        l.at = lds0 + slot * Cfg::stage;
+        l.at = lds0 + lslot * Cfg::stage;
         l.n = nside.stage(second ? np1 : np0, nld, nrows, K, k0);
         if constexpr (GATED) l.n1 = nside.stage(np1, nld, nrows, K, k0);
         l.m = mside.stage(second ? mp1 : mp0, mld, mrows, K, k0);
+        lslot = lslot + 1 == S ? 0 : lslot + 1;
+        if (++lstage == ns) {
+            lstage = 0;
+            if (++ltile < mine) enter(ltile);
+        }
         return l;
     };
     auto load = [&](const Loads &l, int i) {
-        constexpr int NL = NSide::loads, NT = GATED ? 2 * NL : NL;
-        if (i < NL) nside.load(l.n, i, l.at, wave);
-        else if (GATED && i < NT) nside.load(l.n1, i - NL, l.at + NSide::bytes, wave);
-        else mside.load(l.m, i - NT, l.at + BN * BK * 2, wave);
+        if (i < NSide::loads) nside.load(l.n, i, l.at, wave);
+        else if (i < NL) nside.load(l.n1, i - NSide::loads, l.at + NSide::bytes, wave);
+        else mside.load(l.m, i - NL, l.at + BN * BK * 2, wave);
     };
     const bool cut = (K & 7) != 0;
-    auto mend = [&](int st, int slot) {
-        const int k0 = (st >= sp ? st - sp : st) * BK;
-        if (!cut || k0 + BK < K) return;
+    // stage s of a tile, landed in `slot`: zeros past K
+    auto mend = [&](int s, int slot) {
+        if (!cut) return;
+        const int k0 = (TWO && s >= sp ? s - sp : s) * BK;
+        if (k0 + BK < K) return;
         uint8_t *at = smem + slot * Cfg::stage;
         nside.mend(at, K, k0, wave, lane);
         if constexpr (GATED) nside.mend(at + NSide::bytes, K, k0, wave, lane);
@@ -334,126 +370,120 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
     };
 
     f32x4 acc[TN][TM];
-#pragma unroll
-    for (int i = 0; i < TN; ++i)
-#pragma unroll
-        for (int j = 0; j < TM; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    vec fa[TN], fb[2][TM];
+    const int nrow = wn * (NROWS / WN), mrow = wm * (BM / WM);
+    auto readn = [&](const uint8_t *st, int i, int q) {
+        if constexpr (GATED) return nside.read(st + (i >= TNG ? NSide::bytes : 0), nrow, i % TNG, q);
+        else return nside.read(st, nrow, i, q);
+    };
+    auto readm = [&](const uint8_t *st, int j, int q) { return mside.read(st + BN * BK * 2, mrow, j, q); };
 
+    int slot = 0;
     if (ns > 0) {
-        const int nrow = wn * (BN / WN) / (GATED ? 2 : 1), mrow = wm * (BM / WM);
-        auto readn = [&](const uint8_t *st, int i, int q) {
-            if constexpr (GATED) return nside.read(st + (i >= TNG ? NSide::bytes : 0), nrow, i % TNG, q);
-            else return nside.read(st, nrow, i, q);
-        };
-        auto readm = [&](const uint8_t *st, int j, int q) { return mside.read(st + BN * BK * 2, mrow, j, q); };
-        for (int s = 0; s < S && s < ns; ++s) {
-            const Loads l = stage(s, s);
+        enter(0);
+        for (int s = 0; s < S; ++s) {
+            const Loads l = next_loads();
 #pragma unroll
             for (int i = 0; i < L; ++i) load(l, i);
         }
-        // stage 0 has landed when at most the later ones are outstanding
-        if (ns >= S) wait_vm<L *(S - 1)>();
-        else wait_vm<0>();
+        wait_vm<L *(S - 1)>();
         mend(0, 0);
         lds_barrier();
-        vec fa[TN], fb[2][TM];
-#pragma unroll
-        for (int j = 0; j < TM; ++j) fb[0][j] = readm(smem, j, 0);
-#pragma unroll
-        for (int i = 0; i < TN; ++i) fa[i] = readn(smem, i, 0);
-        int slot = 0;
-        // Stage s is multiplied; in its last step the fragments of stage s + 1 are read
-        // (MORE) and stage s + S is loaded into this one's buffer (FULL).
-        auto multiply = [&](int s, auto more, auto full) {
-            constexpr bool MORE = decltype(more)::value, FULL = decltype(full)::value;
-            const uint8_t *cur = smem + slot * Cfg::stage;
-            const int here = slot;
-            slot = slot + 1 == S ? 0 : slot + 1;
-            const uint8_t *nxt = smem + slot * Cfg::stage;
-            Loads l;
-            if constexpr (FULL) l = stage(s + S, here);
-#pragma unroll
-            for (int q = 0; q < KS; ++q) {
-                const bool last = q == KS - 1;
-                const uint8_t *from = last ? nxt : cur;
-                const int fq = last ? 0 : q + 1;
-                constexpr int HOLD = 1;  // rows multiplied before the barrier
-#pragma unroll
-                for (int i = 0; i < TN; ++i) {
-                    __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-                    for (int j = 0; j < TM; ++j) acc[i][j] = mfma(fa[i], fb[q & 1][j], acc[i][j]);
-                    __builtin_amdgcn_s_setprio(0);
-                    if (i == HOLD && last && MORE) {
-                        // the next stage has landed, this one has been read by all
-                        if constexpr (FULL) wait_vm<L *(S - 2)>();
-                        else wait_vm<0>();
-                        mend(s + 1, slot);
-                        lds_barrier();
-                    }
-                    if (i >= HOLD && (!last || MORE)) {
-                        if (i == HOLD) {
-#pragma unroll
-                            for (int j = 0; j < TM; ++j) fb[(q + 1) & 1][j] = readm(from, j, fq);
-#pragma unroll
-                            for (int h = 0; h < HOLD; ++h) fa[h] = readn(from, h, fq);
-                        }
-                        fa[i] = readn(from, i, fq);
-                    }
-                    if constexpr (FULL) {
-                        if (last && i >= HOLD) {  // the loads, spread over the remaining rows
-                            constexpr int per = (L + TN - HOLD - 1) / (TN - HOLD);
-#pragma unroll
-                            for (int e = 0; e < per; ++e)
-                                if ((i - HOLD) * per + e < L) load(l, (i - HOLD) * per + e);
-                        }
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-            }
-            if constexpr (KS % 2 == 1) {
-#pragma unroll
-                for (int j = 0; j < TM; ++j) fb[0][j] = fb[1][j];
-            }
-        };
-        int s = 0;
-        for (; s + S < ns; ++s) multiply(s, std::true_type{}, std::true_type{});
-        for (; s + 1 < ns; ++s) multiply(s, std::true_type{}, std::false_type{});
-        multiply(s, std::false_type{}, std::false_type{});
     }
 
-    // The sums go through LDS, 16 rows of each wavefront at a time, and out in
-    // vectors of 8 consecutive n.
-    float *sc = reinterpret_cast<float *>(smem);
-    constexpr int CP = Cfg::cpitch, CHUNKS = NROWS / 8;
-    void *Y = z ? g.y1 : g.e.Y;
-    auto stage_sums = [&](auto jc) {
-        constexpr int j = decltype(jc)::value;
+    // Stage s is multiplied, a fragment row at a time; each row's N fragment is
+    // replaced by the next step's as soon as the row has been issued.  In the last
+    // step the next stage's fragments are read, and the stage S ahead is loaded into
+    // this one's buffer.
+    auto multiply = [&](int s) {
+        const uint8_t *cur = smem + slot * Cfg::stage;
+        slot = slot + 1 == S ? 0 : slot + 1;
+        const uint8_t *nxt = smem + slot * Cfg::stage;
+        const Loads l = next_loads();
 #pragma unroll
-        for (int i = 0; i < TN; ++i) {
-            const int f = GATED ? i % TNG : i;
-            const int n = (GATED ? (i >= TNG ? BN / 2 : 0) + wn * (BN / WN / 2) : wn * (BN / WN)) + 32 * (f >> 1) +
-                          8 * (lane >> 4) + 4 * (f & 1);
-            *reinterpret_cast<f32x4 *>(sc + (wm * 16 + (lane & 15)) * CP + n) = acc[i][j];
+        for (int q = 0; q < KS; ++q) {
+            const bool last = q == KS - 1;
+            const uint8_t *from = last ? nxt : cur;
+            const int fq = last ? 0 : q + 1;
+#pragma unroll
+            for (int i = 0; i < TN; ++i) {
+#pragma unroll
+                for (int j = 0; j < TM; ++j) acc[i][j] = mfma(fa[i], fb[q & 1][j], acc[i][j]);
+                if (i == 0 && last) {
+                    // the next stage has landed, this one has been read by all
+                    wait_vm<L *(S - 2)>();
+                    mend(s + 1 == ns ? 0 : s + 1, slot);
+                    lds_barrier();
+                }
+                if (i == 0) {
+#pragma unroll
+                    for (int j = 0; j < TM; ++j) fb[(q + 1) & 1][j] = readm(from, j, fq);
+                }
+                fa[i] = readn(from, i, fq);
+                if (last) {  // the loads, spread over the rows
+                    constexpr int rate = (L + TN - 1) / TN;
+#pragma unroll
+                    for (int e = 0; e < rate; ++e)
+                        if (i * rate + e < L) load(l, i * rate + e);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
     };
-    static_assert(TM == 4, "the passes below");
+
 #pragma unroll 1
-    for (int j = 0; j < TM; ++j) {
-        lds_barrier();
-        if (j == 0) stage_sums(std::integral_constant<int, 0>{});
-        else if (j == 1) stage_sums(std::integral_constant<int, 1>{});
-        else if (j == 2) stage_sums(std::integral_constant<int, 2>{});
-        else stage_sums(std::integral_constant<int, 3>{});
-        lds_barrier();
-        for (int c = tid; c < Cfg::rows * CHUNKS; c += Cfg::NT) {
-            const int r = c / CHUNKS, nl = (c - r * CHUNKS) * 8;
-            const int64_t m = m0 + (r >> 4) * (BM / WM) + j * 16 + (r & 15), n = n0 + nl;
-            if (m < g.M && n < g.N)
-                finish8<T>(g.e, GATED, Y, m, n, (int)min((int64_t)8, g.N - n), sc + r * CP + nl,
-                           GATED ? sc + r * CP + BN / 2 + nl : nullptr);
+    for (int ti = 0; ti < mine; ++ti) {
+#pragma unroll
+        for (int i = 0; i < TN; ++i)
+#pragma unroll
+            for (int j = 0; j < TM; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (ns > 0) {
+#pragma unroll
+            for (int j = 0; j < TM; ++j) fb[0][j] = readm(smem + slot * Cfg::stage, j, 0);
+#pragma unroll
+            for (int i = 0; i < TN; ++i) fa[i] = readn(smem + slot * Cfg::stage, i, 0);
+#pragma unroll 1
+            for (int s = 0; s < ns; ++s) multiply(s);
+        }
+
+        // Results straight from the registers.  Exchanging the odd rows of 16 lanes of
+        // one fragment with the even ones of the next leaves 8 consecutive n in each
+        // lane: 16-byte stores, 64 bytes of a row by 4 lanes.
+        const Tile q = tile_at(ti);
+        void *Y = q.z ? g.y1 : g.e.Y;
+        const int64_t nb = q.n0 + nrow + ((lane >> 4) & 1) * 16 + (lane >> 5) * 8;
+#pragma unroll 1
+        for (int j = 0; j < TM; ++j) {
+            f32x4 t[TN];
+            pick<TM>(j, [&](auto jc) {
+#pragma unroll
+                for (int i = 0; i < TN; ++i) t[i] = acc[i][decltype(jc)::value];
+            });
+#pragma unroll
+            for (int i = 0; i < TN; i += 2)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const auto w = __builtin_amdgcn_permlane16_swap(__float_as_uint(t[i][e]), __float_as_uint(t[i + 1][e]),
+                                                                    false, false);
+                    t[i][e] = __uint_as_float(w[0]);
+                    t[i + 1][e] = __uint_as_float(w[1]);
+                }
+            const int64_t m = q.m0 + mrow + j * 16 + (lane & 15);
+            if (m >= g.M) continue;
+#pragma unroll
+            for (int i = 0; i < TNG; i += 2) {
+                const int64_t n = nb + i * 16;
+                float z[8], u[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    z[e] = t[i + (e >> 2)][e & 3];
+                    if constexpr (GATED) u[e] = t[TNG + i + (e >> 2)][e & 3];
+                }
+                if (n < g.N) finish8<T, GATED>(g.e, Y, m, n, (int)min((int64_t)8, g.N - n), z, u);
+            }
         }
     }
+    wait_vm<0>();  // the loads past the last stage still write to LDS
 }
 
 // Copies a matrix to rows of whole 16-byte chunks.
@@ -474,31 +504,45 @@ __global__ __launch_bounds__(256) void k_align_rows(const T *p, int64_t ld, int6
 }
 
 // ---------------------------------------------------------------- host side
-// Raises the kernel's LDS limit once per kernel and device.
-int allow_lds(const void *kern, int lds) {
+// Workgroups of `kern` (nt threads, lds bytes) that the GPU holds at once; raises
+// the kernel's LDS limit on the first call per device.
+int resident(const void *kern, int nt, int lds, int *groups) {
     static std::mutex mu;
-    static std::set<std::pair<const void *, int>> known;
+    static std::map<std::pair<const void *, int>, int> known;
     int dev = 0;
     if (int rc = check_hip(hipGetDevice(&dev), "matrix product: current device")) return rc;
     std::lock_guard<std::mutex> lock(mu);
-    if (known.count({kern, dev})) return SA_OK;
+    const auto it = known.find({kern, dev});
+    if (it != known.end()) {
+        *groups = it->second;
+        return SA_OK;
+    }
     if (int rc = check_hip(hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds), "matrix product: LDS"))
         return rc;
-    known.insert({kern, dev});
+    int per_cu = 0, cus = 0;
+    if (int rc = check_hip(hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, kern, nt, lds), "matrix product: occupancy"))
+        return rc;
+    if (int rc = check_hip(hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev), "matrix product: CU count"))
+        return rc;
+    *groups = std::max(1, per_cu) * std::max(1, cus);
+    known[{kern, dev}] = *groups;
     return SA_OK;
 }
 
 template <typename T, bool NA, bool MA, bool GATED, int BN, int BM, int WN, int WM, int BK, int S>
 int launch(const Gemm &g, hipStream_t stream) {
     using Cfg = TileCfg<BN, BM, WN, WM, BK, S>;
-    TileArgs a{g, 0, 0};
+    TileArgs a{g, 0, 0, 0, 0};
     const int64_t mt = (g.M + BM - 1) / BM, nt = (g.N + (GATED ? BN / 2 : BN) - 1) / (GATED ? BN / 2 : BN);
     if (mt * nt >= (int64_t(1) << 28)) return fail(SA_E_UNSUPPORTED, "matrix product of more than 2^28 tiles");
     a.mtiles = (int)mt;
     a.ntiles = (int)nt;
+    a.tiles = (int)(mt * nt) * g.batch;
     auto kern = k_gemm<T, NA, MA, GATED, BN, BM, WN, WM, BK, S>;
-    if (int rc = allow_lds(reinterpret_cast<const void *>(kern), Cfg::lds)) return rc;
-    hipLaunchKernelGGL(kern, dim3(a.mtiles * a.ntiles, 1, g.batch), dim3(Cfg::NT), Cfg::lds, stream, a);
+    int groups = 0;
+    if (int rc = resident(reinterpret_cast<const void *>(kern), Cfg::NT, Cfg::lds, &groups)) return rc;
+    a.groups = std::min(a.tiles, groups);
+    hipLaunchKernelGGL(kern, dim3(a.groups), dim3(Cfg::NT), Cfg::lds, stream, a);
     return check_hip(hipGetLastError(), "k_gemm");
 }
 
