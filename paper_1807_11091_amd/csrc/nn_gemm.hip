@@ -25,45 +25,173 @@ __device__ inline f32x4 mfma(Vec8<_Float16>::type a, Vec8<_Float16>::type b, f32
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
 
-// Eight (cnt < 8 at a row's end) consecutive outputs from their sums z (and u).
-template <typename T, bool GATED>
-__device__ inline void finish8(const Epilogue &e, void *Y, int64_t m, int64_t n, int cnt, float (&z)[8], float (&u)[8]) {
-    auto add = [&](const float *b, float (&v)[8]) {
-        float t[8];
-        if (cnt == 8) load_vec<float, 8>(b + n, t);
-        else load_part<float, 8>(b + n, cnt, t);
+// V (cnt < V at a row's end) consecutive outputs from their sums z (and u).
+template <typename T, bool GATED, int V>
+__device__ inline void finish(const Epilogue &e, void *Y, int64_t m, int64_t n, int cnt, float (&z)[V], float (&u)[V]) {
+    auto add = [&](const auto *p, float (&v)[V]) {
+        using E = typename std::remove_cv<typename std::remove_reference<decltype(*p)>::type>::type;
+        float t[V];
+        if (cnt == V) load_vec<E, V>(p, t);
+        else load_part<E, V>(p, cnt, t);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] += t[i];
+        for (int i = 0; i < V; ++i) v[i] += t[i];
     };
-    auto put = [&](void *p, int64_t at, const float (&v)[8]) {
-        if (cnt == 8) store_vec<T, 8>(reinterpret_cast<T *>(p) + at, v);
-        else store_part<T, 8>(reinterpret_cast<T *>(p) + at, cnt, v);
+    auto put = [&](auto *p, const float (&v)[V]) {
+        using E = typename std::remove_reference<decltype(*p)>::type;
+        if (cnt == V) store_vec<E, V>(p, v);
+        else store_part<E, V>(p, cnt, v);
     };
-    if (e.bias) add(e.bias, z);
-    if (e.Z) put(e.Z, m * e.ldz + n, z);
+    if (e.bias) add(e.bias + n, z);
+    if (e.Z) put(reinterpret_cast<T *>(e.Z) + m * e.ldz + n, z);
     if (e.act != SA_ACT_NONE)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) z[i] = act_value(e.act, z[i]);
+        for (int i = 0; i < V; ++i) z[i] = act_value(e.act, z[i]);
     if constexpr (GATED) {
-        if (e.bias2) add(e.bias2, u);
-        if (e.Z2) put(e.Z2, m * e.ldz + n, u);
+        if (e.bias2) add(e.bias2 + n, u);
+        if (e.Z2) put(reinterpret_cast<T *>(e.Z2) + m * e.ldz + n, u);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) z[i] *= u[i];
+        for (int i = 0; i < V; ++i) z[i] *= u[i];
     }
     if (e.out_f32) {
-        float *y = reinterpret_cast<float *>(Y) + m * e.ldy + n;
-        if (e.R) add(reinterpret_cast<const float *>(e.R) + m * e.ldr, z);
-        if (cnt == 8) store_vec<float, 8>(y, z);
-        else store_part<float, 8>(y, cnt, z);
+        if (e.R) add(reinterpret_cast<const float *>(e.R) + m * e.ldr + n, z);
+        put(reinterpret_cast<float *>(Y) + m * e.ldy + n, z);
     } else {
-        if (e.R) {
-            const T *r = reinterpret_cast<const T *>(e.R) + m * e.ldr + n;
-            if (cnt == 8) load_vec<T, 8>(r, u);
-            else load_part<T, 8>(r, cnt, u);
+        if (e.R) add(reinterpret_cast<const T *>(e.R) + m * e.ldr + n, z);
+        put(reinterpret_cast<T *>(Y) + m * e.ldy + n, z);
+    }
+}
+
+// Where binary32 partial sums of a product go when k is split over workgroups:
+// [split][batch][gated ? 2 : 1][M][pitch].
+struct Partial {
+    float *p;
+    int64_t pitch;  // N rounded up to 8
+    int split;      // 1: none
+};
+
+__device__ inline float *partial_at(const Partial &q, const Gemm &g, int chunk, int z, int half, int64_t m, int64_t n) {
+    const int64_t plane = ((int64_t)chunk * g.batch + z) * (g.gated ? 2 : 1) + half;
+    return q.p + (plane * g.M + m) * q.pitch + n;
+}
+
+// Adds the chunks in their order and finishes 8 outputs per thread.
+template <typename T, bool GATED>
+__global__ __launch_bounds__(256) void k_join(Gemm g, Partial q) {
+    const int64_t chunks = q.pitch / 8;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= g.M * chunks) return;
+    const int64_t m = i / chunks, n = (i - m * chunks) * 8;
+    const int z = blockIdx.y;
+    float s[8] = {}, u[8] = {}, t[8];
+    for (int c = 0; c < q.split; ++c) {
+        load_vec<float, 8>(partial_at(q, g, c, z, 0, m, n), t);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) z[i] += u[i];
+        for (int e = 0; e < 8; ++e) s[e] += t[e];
+        if constexpr (GATED) {
+            load_vec<float, 8>(partial_at(q, g, c, z, 1, m, n), t);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) u[e] += t[e];
         }
-        put(Y, m * e.ldy + n, z);
+    }
+    finish<T, GATED, 8>(g.e, z ? g.y1 : g.e.Y, m, n, (int)min((int64_t)8, g.N - n), s, u);
+}
+
+// ------------------------------------------------------------- few rows of M
+// k_rows: products of at most 16 * MF rows of M (single tokens, small batches),
+// bound by reading the N side's matrices once.  A workgroup of 8 wavefronts takes
+// NF * 16 of their rows; its wavefronts take k in turn, in blocks of U * 32, and
+// feed the MFMAs straight from memory (the weights are used once: LDS would only
+// add a copy).  Their sums are joined through LDS in a fixed order.  Rows past M
+// or N read the last row and are not stored.
+template <typename T, bool GATED, int NF, int MF, int U>
+__global__ __launch_bounds__(512) void k_rows(Gemm g, Partial q) {
+    typedef typename Vec8<T>::type vec;
+    constexpr int NW = 8, H = GATED ? 2 : 1, STEP = 32 * U;
+    __shared__ float sums[NW][NF * H * MF][256];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int r = lane & 15, kg = (lane >> 4) * 8;
+    const int64_t n0 = (int64_t)blockIdx.x * NF * 16;
+    const int K = (int)g.K;
+    // chunk of k of this workgroup, in whole blocks of all its wavefronts
+    const int blocks = (K + STEP - 1) / STEP;
+    const int b0 = (int)((int64_t)blocks * blockIdx.y / q.split), b1 = (int)((int64_t)blocks * (blockIdx.y + 1) / q.split);
+
+    const T *wp[H * NF], *xp[MF];
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+#pragma unroll
+        for (int f = 0; f < NF; ++f)
+            wp[h * NF + f] = reinterpret_cast<const T *>(g.n[h].p) + min(n0 + f * 16 + r, g.N - 1) * g.n[h].ld + kg;
+#pragma unroll
+    for (int j = 0; j < MF; ++j) xp[j] = reinterpret_cast<const T *>(g.m[0].p) + min((int64_t)(j * 16 + r), g.M - 1) * g.m[0].ld + kg;
+
+    f32x4 acc[H * NF][MF] = {};
+    for (int b = b0 + wave; b < b1; b += NW) {
+        const int k = b * STEP;
+        if (k + STEP <= K) {
+            vec w[U][H * NF], x[U][MF];
+#pragma unroll
+            for (int s = 0; s < U; ++s) {
+#pragma unroll
+                for (int f = 0; f < H * NF; ++f) __builtin_memcpy(&w[s][f], wp[f] + k + s * 32, 16);
+#pragma unroll
+                for (int j = 0; j < MF; ++j) __builtin_memcpy(&x[s][j], xp[j] + k + s * 32, 16);
+            }
+#pragma unroll
+            for (int s = 0; s < U; ++s)
+#pragma unroll
+                for (int f = 0; f < H * NF; ++f)
+#pragma unroll
+                    for (int j = 0; j < MF; ++j) acc[f][j] = mfma(w[s][f], x[s][j], acc[f][j]);
+        } else {  // the last block: zeros past K
+            auto part = [&](const T *p, int at) {
+                vec v = {};
+                const int n = K - at - kg;
+                if (n >= 8) __builtin_memcpy(&v, p + at, 16);
+                else
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (e < n) v[e] = p[at + e];
+                return v;
+            };
+#pragma unroll 1
+            for (int at = k; at < K; at += 32) {
+                vec x[MF];
+#pragma unroll
+                for (int j = 0; j < MF; ++j) x[j] = part(xp[j], at);
+#pragma unroll
+                for (int f = 0; f < H * NF; ++f) {
+                    const vec w = part(wp[f], at);
+#pragma unroll
+                    for (int j = 0; j < MF; ++j) acc[f][j] = mfma(w, x[j], acc[f][j]);
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int f = 0; f < H * NF; ++f)
+#pragma unroll
+        for (int j = 0; j < MF; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sums[wave][f * MF + j][r * 16 + (lane >> 4) * 4 + e] = acc[f][j][e];
+    __syncthreads();
+    // one output per thread: row m of M, 16 consecutive n
+    for (int i = threadIdx.x; i < NF * MF * 256; i += 512) {
+        const int f = i / (MF * 256), j = i / 256 % MF, at = i & 255;
+        const int64_t m = j * 16 + (at >> 4), n = n0 + f * 16 + (at & 15);
+        if (m >= g.M || n >= g.N) continue;
+        float z[1] = {0.0f}, u[1] = {0.0f};
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            z[0] += sums[w][f * MF + j][at];
+            if constexpr (GATED) u[0] += sums[w][(NF + f) * MF + j][at];
+        }
+        if (q.split > 1) {
+            *partial_at(q, g, blockIdx.y, 0, 0, m, n) = z[0];
+            if constexpr (GATED) *partial_at(q, g, blockIdx.y, 0, 1, m, n) = u[0];
+        } else {
+            finish<T, GATED, 1>(g.e, g.e.Y, m, n, 1, z, u);
+        }
     }
 }
 
@@ -254,7 +382,8 @@ __device__ inline void pick(int j, F &&f) {
 
 struct TileArgs {
     Gemm g;
-    int mtiles, ntiles, tiles, groups;  // tiles: of all batches; groups: workgroups
+    Partial part;
+    int mtiles, ntiles, tiles, groups;  // tiles: of all batches and chunks; groups: workgroups
 };
 
 template <typename T, bool NA, bool MA, bool GATED, int BN, int BM, int WN, int WM, int BK, int S>
@@ -291,14 +420,19 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
     // A tile: bands of 8 M tiles, down each band first, so that neighbours share operands
     struct Tile {
         int64_t m0, n0;
-        int z;
+        int z, chunk;
+        int s0, s1;  // its stages
     };
     auto tile_at = [&](int i) {
         int t = first + i * stride;
         const int one = a.mtiles * a.ntiles;
         Tile q;
+        q.chunk = t / (one * g.batch);
+        t -= q.chunk * one * g.batch;
         q.z = t / one;
         t -= q.z * one;
+        q.s0 = uni((int)((int64_t)ns * q.chunk / a.part.split));
+        q.s1 = uni((int)((int64_t)ns * (q.chunk + 1) / a.part.split));
         const int band = t / (8 * a.ntiles), in = t - band * 8 * a.ntiles;
         const int h = min(8, a.mtiles - band * 8);
         q.m0 = (int64_t)(band * 8 + in % h) * BM;
@@ -322,7 +456,7 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
     };
     constexpr bool TWO = NA && !MA;  // the sum may have two parts (MA: there may be two batches)
     const T *np0, *np1 = nullptr, *mp0, *mp1 = nullptr;
-    int nrows, mrows, ltile = 0, lstage = 0, lslot = 0;
+    int nrows, mrows, ltile = 0, lstage = 0, lend = 0, lslot = 0;
     auto enter = [&](int i) {
         const Tile q = tile_at(i);
         const int64_t no = NA ? q.n0 : q.n0 * nld, mo = MA ? q.m0 : q.m0 * mld;
@@ -330,6 +464,8 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
         if constexpr (GATED || TWO) np1 = reinterpret_cast<const T *>(g.n[1].p) + no;
         mp0 = reinterpret_cast<const T *>(MA && q.z ? g.m[1].p : g.m[0].p) + mo;
         if constexpr (TWO) mp1 = reinterpret_cast<const T *>(g.m[1].p) + mo;
+        lstage = q.s0;
+        lend = q.s1;
         nrows = uni((int)min(g.N - q.n0, (int64_t)NROWS));
         mrows = uni((int)min(g.M - q.m0, (int64_t)BM));
     };
@@ -346,10 +482,7 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
         if constexpr (GATED) l.n1 = nside.stage(np1, nld, nrows, K, k0);
         l.m = mside.stage(second ? mp1 : mp0, mld, mrows, K, k0);
         lslot = lslot + 1 == S ? 0 : lslot + 1;
-        if (++lstage == ns) {
-            lstage = 0;
-            if (++ltile < mine) enter(ltile);
-        }
+        if (++lstage == lend && ++ltile < mine) enter(ltile);
         return l;
     };
     auto load = [&](const Loads &l, int i) {
@@ -387,15 +520,15 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
             for (int i = 0; i < L; ++i) load(l, i);
         }
         wait_vm<L *(S - 1)>();
-        mend(0, 0);
+        mend(tile_at(0).s0, 0);
         lds_barrier();
     }
 
-    // Stage s is multiplied, a fragment row at a time; each row's N fragment is
+    // A stage is multiplied, a fragment row at a time; each row's N fragment is
     // replaced by the next step's as soon as the row has been issued.  In the last
     // step the next stage's fragments are read, and the stage S ahead is loaded into
     // this one's buffer.
-    auto multiply = [&](int s) {
+    auto multiply = [&](int next) {  // next: the stage that follows
         const uint8_t *cur = smem + slot * Cfg::stage;
         slot = slot + 1 == S ? 0 : slot + 1;
         const uint8_t *nxt = smem + slot * Cfg::stage;
@@ -412,7 +545,7 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
                 if (i == 0 && last) {
                     // the next stage has landed, this one has been read by all
                     wait_vm<L *(S - 2)>();
-                    mend(s + 1 == ns ? 0 : s + 1, slot);
+                    mend(next, slot);
                     lds_barrier();
                 }
                 if (i == 0) {
@@ -433,6 +566,7 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
 
 #pragma unroll 1
     for (int ti = 0; ti < mine; ++ti) {
+        const Tile q = tile_at(ti);
 #pragma unroll
         for (int i = 0; i < TN; ++i)
 #pragma unroll
@@ -443,13 +577,12 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
 #pragma unroll
             for (int i = 0; i < TN; ++i) fa[i] = readn(smem + slot * Cfg::stage, i, 0);
 #pragma unroll 1
-            for (int s = 0; s < ns; ++s) multiply(s);
+            for (int s = q.s0; s < q.s1; ++s) multiply(s + 1 < q.s1 ? s + 1 : ti + 1 < mine ? tile_at(ti + 1).s0 : 0);
         }
 
         // Results straight from the registers.  Exchanging the odd rows of 16 lanes of
         // one fragment with the even ones of the next leaves 8 consecutive n in each
         // lane: 16-byte stores, 64 bytes of a row by 4 lanes.
-        const Tile q = tile_at(ti);
         void *Y = q.z ? g.y1 : g.e.Y;
         const int64_t nb = q.n0 + nrow + ((lane >> 4) & 1) * 16 + (lane >> 5) * 8;
 #pragma unroll 1
@@ -479,7 +612,13 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
                     z[e] = t[i + (e >> 2)][e & 3];
                     if constexpr (GATED) u[e] = t[TNG + i + (e >> 2)][e & 3];
                 }
-                if (n < g.N) finish8<T, GATED>(g.e, Y, m, n, (int)min((int64_t)8, g.N - n), z, u);
+                if (n >= g.N) continue;
+                if (a.part.split > 1) {
+                    store_vec<float, 8>(partial_at(a.part, g, q.chunk, q.z, 0, m, n), z);
+                    if constexpr (GATED) store_vec<float, 8>(partial_at(a.part, g, q.chunk, q.z, 1, m, n), u);
+                } else {
+                    finish<T, GATED, 8>(g.e, Y, m, n, (int)min((int64_t)8, g.N - n), z, u);
+                }
             }
         }
     }
@@ -529,36 +668,88 @@ int resident(const void *kern, int nt, int lds, int *groups) {
     return SA_OK;
 }
 
+// How a product runs.
+enum Path { kRows16, kRows32, kRows64, kTile128, kTile256 };
+struct Plan {
+    Path path;
+    int split;  // chunks of k
+};
+
+// Workgroups of k_gemm that the chip's 256 CUs hold: the 256 x 256 tile's LDS fills a CU, two of the
+// 128 x 128 tile's share one.
+constexpr int kSlots256 = 256, kSlots128 = 512;
+
+Plan plan_of(const Gemm &g) {
+    const int64_t nn = g.N * (g.gated ? 2 : 1), steps = (g.K + 63) / 64 * g.parts;
+    if (g.M <= 64 && !g.n[0].across) {
+        const Path path = g.M <= 16 ? kRows16 : g.M <= 32 ? kRows32 : kRows64;
+        const int64_t groups = (g.N + 15) / 16, blocks = (g.K + 255) / 256;
+        int split = 1;
+        while (groups * split < 192 && blocks >= 16 * split) split *= 2;
+        return {path, split};
+    }
+    const int64_t t256 = ((g.M + 255) / 256) * ((nn + 255) / 256) * g.batch;
+    if (t256 >= 128) return {kTile256, 1};
+    const int64_t t128 = ((g.M + 127) / 128) * ((nn + 127) / 128) * g.batch;
+    int split = 1;
+    while (t128 * split * 2 <= kSlots128 && steps >= 16 * split) split *= 2;
+    return {kTile128, split};
+}
+
+size_t partial_bytes(const Gemm &g, int split) {
+    return split > 1 ? (size_t)split * g.batch * (g.gated ? 2 : 1) * g.M * round_up(g.N, 8) * sizeof(float) : 0;
+}
+
+template <typename T, bool GATED>
+int join(const Gemm &g, const Partial &q, hipStream_t stream) {
+    const int64_t blocks = (g.M * (q.pitch / 8) + 255) / 256;
+    hipLaunchKernelGGL((k_join<T, GATED>), dim3((unsigned)blocks, g.batch), dim3(256), 0, stream, g, q);
+    return check_hip(hipGetLastError(), "k_join");
+}
+
 template <typename T, bool NA, bool MA, bool GATED, int BN, int BM, int WN, int WM, int BK, int S>
-int launch(const Gemm &g, hipStream_t stream) {
+int launch(const Gemm &g, const Partial &q, hipStream_t stream) {
     using Cfg = TileCfg<BN, BM, WN, WM, BK, S>;
-    TileArgs a{g, 0, 0, 0, 0};
+    TileArgs a{g, q, 0, 0, 0, 0};
     const int64_t mt = (g.M + BM - 1) / BM, nt = (g.N + (GATED ? BN / 2 : BN) - 1) / (GATED ? BN / 2 : BN);
     if (mt * nt >= (int64_t(1) << 28)) return fail(SA_E_UNSUPPORTED, "matrix product of more than 2^28 tiles");
     a.mtiles = (int)mt;
     a.ntiles = (int)nt;
-    a.tiles = (int)(mt * nt) * g.batch;
+    a.tiles = (int)(mt * nt) * g.batch * q.split;
     auto kern = k_gemm<T, NA, MA, GATED, BN, BM, WN, WM, BK, S>;
     int groups = 0;
     if (int rc = resident(reinterpret_cast<const void *>(kern), Cfg::NT, Cfg::lds, &groups)) return rc;
     a.groups = std::min(a.tiles, groups);
     hipLaunchKernelGGL(kern, dim3(a.groups), dim3(Cfg::NT), Cfg::lds, stream, a);
-    return check_hip(hipGetLastError(), "k_gemm");
+    if (int rc = check_hip(hipGetLastError(), "k_gemm")) return rc;
+    return q.split > 1 ? join<T, GATED>(g, q, stream) : SA_OK;
+}
+
+template <typename T, bool GATED, int NF, int MF, int U>
+int launch_rows(const Gemm &g, const Partial &q, hipStream_t stream) {
+    hipLaunchKernelGGL((k_rows<T, GATED, NF, MF, U>), dim3((unsigned)((g.N + NF * 16 - 1) / (NF * 16)), q.split), dim3(512), 0,
+                       stream, g, q);
+    if (int rc = check_hip(hipGetLastError(), "k_rows")) return rc;
+    return q.split > 1 ? join<T, GATED>(g, q, stream) : SA_OK;
 }
 
 template <typename T, bool NA, bool MA, bool GATED>
-int by_size(const Gemm &g, hipStream_t stream) {
-    const int64_t big = ((g.M + 255) / 256) * ((g.N * (GATED ? 2 : 1) + 255) / 256) * g.batch;
-    if (big >= 128) return launch<T, NA, MA, GATED, 256, 256, 2, 4, 64, 2>(g, stream);
-    return launch<T, NA, MA, GATED, 128, 128, 2, 2, 64, 2>(g, stream);
+int by_size(const Gemm &g, const Plan &p, const Partial &q, hipStream_t stream) {
+    if constexpr (!NA) {
+        if (p.path == kRows16) return launch_rows<T, GATED, 1, 1, GATED ? 4 : 8>(g, q, stream);
+        if (p.path == kRows32) return launch_rows<T, GATED, 1, 2, 4>(g, q, stream);
+        if (p.path == kRows64) return launch_rows<T, GATED, 1, 4, GATED ? 2 : 4>(g, q, stream);
+    }
+    if (p.path == kTile256) return launch<T, NA, MA, GATED, 256, 256, 2, 4, 64, 2>(g, q, stream);
+    return launch<T, NA, MA, GATED, 128, 128, 2, 2, 64, 2>(g, q, stream);
 }
 
 template <typename T>
-int run(const Gemm &g, hipStream_t stream) {
-    if (g.gated) return by_size<T, false, false, true>(g, stream);
-    if (!g.n[0].across) return by_size<T, false, false, false>(g, stream);
-    if (!g.m[0].across) return by_size<T, true, false, false>(g, stream);
-    return by_size<T, true, true, false>(g, stream);
+int run(const Gemm &g, const Plan &p, const Partial &q, hipStream_t stream) {
+    if (g.gated) return by_size<T, false, false, true>(g, p, q, stream);
+    if (!g.n[0].across) return by_size<T, false, false, false>(g, p, q, stream);
+    if (!g.m[0].across) return by_size<T, true, false, false>(g, p, q, stream);
+    return by_size<T, true, true, false>(g, p, q, stream);
 }
 
 // Rows and columns of an operand as it is stored.
@@ -570,9 +761,12 @@ Shape shape_of(const Operand &o, int64_t r, int64_t K) { return o.across ? Shape
 // Do the rows start on 16-byte boundaries (a single row needs no pitch)?
 bool rows_aligned(const Operand &o, const Shape &s) { return aligned(o.p, 16) && (s.rows <= 1 || o.ld % 8 == 0); }
 
-// Visits the operands of a product with the length of their rows' axis.
+// Does the product's path read rows of any alignment?
+bool any_rows(const Plan &p) { return p.path <= kRows64; }
+
+// Visits the operands that have to be copied to aligned rows.
 template <typename F>
-int each_operand(Gemm &g, F &&f) {
+int each_copied(Gemm &g, F &&f) {
     const int nm = std::max(g.parts, g.batch), nn = g.gated ? 2 : g.parts;
     // the two of a side share one pitch, so both are copied if one is
     bool cm = false, cn = false;
@@ -591,41 +785,48 @@ int64_t aligned_pitch(const Shape &s) { return round_up(s.cols, 8); }
 
 size_t gemm_workspace(const Gemm &g0) {
     Gemm g = g0;
-    size_t need = 0;
     if (g.M == 0 || g.N == 0) return 0;
-    each_operand(g, [&](Operand &, const Shape &s) {
-        need += (size_t)round_up(s.rows * aligned_pitch(s) * 2, 256);
-        return SA_OK;
-    });
+    const Plan p = plan_of(g);
+    size_t need = round_up(partial_bytes(g, p.split), 256);
+    if (!any_rows(p))
+        each_copied(g, [&](Operand &, const Shape &s) {
+            need += (size_t)round_up(s.rows * aligned_pitch(s) * 2, 256);
+            return SA_OK;
+        });
     return need;
 }
 
 int gemm(const Gemm &g0, void *ws, hipStream_t stream) {
     Gemm g = g0;
     if (g.M == 0 || g.N == 0) return SA_OK;
+    const Plan p = plan_of(g);
     uint8_t *at = static_cast<uint8_t *>(ws);
-    int rc = each_operand(g, [&](Operand &o, const Shape &s) {
-        const int64_t ldo = aligned_pitch(s), chunks = s.rows * (ldo / 8);
-        if (chunks > 0) {
-            // the element's type does not matter to a copy
-            hipLaunchKernelGGL(k_align_rows<_Float16>, dim3((unsigned)std::min<int64_t>((chunks + 255) / 256, 8192)), dim3(256), 0,
-                               stream, static_cast<const _Float16 *>(o.p), o.ld, s.rows, (int)s.cols,
-                               reinterpret_cast<_Float16 *>(at), ldo);
-            if (int e = check_hip(hipGetLastError(), "k_align_rows")) return e;
-        }
-        o.p = at;
-        o.ld = ldo;
-        at += round_up(s.rows * ldo * 2, 256);
-        return SA_OK;
-    });
-    if (rc) return rc;
+    const Partial q{reinterpret_cast<float *>(at), round_up(g.N, 8), p.split};
+    at += round_up(partial_bytes(g, p.split), 256);
+    if (!any_rows(p)) {
+        const int rc = each_copied(g, [&](Operand &o, const Shape &s) {
+            const int64_t ldo = aligned_pitch(s), chunks = s.rows * (ldo / 8);
+            if (chunks > 0) {
+                // the element's type does not matter to a copy
+                hipLaunchKernelGGL(k_align_rows<_Float16>, dim3((unsigned)std::min<int64_t>((chunks + 255) / 256, 8192)), dim3(256),
+                                   0, stream, static_cast<const _Float16 *>(o.p), o.ld, s.rows, (int)s.cols,
+                                   reinterpret_cast<_Float16 *>(at), ldo);
+                if (int e = check_hip(hipGetLastError(), "k_align_rows")) return e;
+            }
+            o.p = at;
+            o.ld = ldo;
+            at += round_up(s.rows * ldo * 2, 256);
+            return SA_OK;
+        });
+        if (rc) return rc;
+    }
     // a single row has no pitch: one of whole chunks keeps the loads' ranges whole
     const int64_t mr = g.m[0].across ? g.K : g.M, nr = g.n[0].across ? g.K : g.N;
     for (int i = 0; i < 2; ++i) {
         if (mr <= 1) g.m[i].ld = round_up(g.m[0].across ? g.M : g.K, 8);
         if (nr <= 1) g.n[i].ld = round_up(g.n[0].across ? g.N : g.K, 8);
     }
-    return g.type == SA_BF16 ? run<__bf16>(g, stream) : run<_Float16>(g, stream);
+    return g.type == SA_BF16 ? run<__bf16>(g, p, q, stream) : run<_Float16>(g, p, q, stream);
 }
 
 }  // namespace sa
