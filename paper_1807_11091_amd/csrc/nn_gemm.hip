@@ -97,12 +97,13 @@ __global__ __launch_bounds__(256) void k_join(Gemm g, Partial q) {
 }
 
 // ------------------------------------------------------------- few rows of M
-// k_rows: products of at most 16 * MF rows of M (single tokens, small batches),
-// bound by reading the N side's matrices once.  A workgroup of 8 wavefronts takes
-// NF * 16 of their rows; its wavefronts take k in turn, in blocks of U * 32, and
-// feed the MFMAs straight from memory (the weights are used once: LDS would only
-// add a copy).  Their sums are joined through LDS in a fixed order.  Rows past M
-// or N read the last row and are not stored.
+// k_rows: products with few rows of M (single tokens, small batches), bound by
+// reading the N side's matrices once and by latency.  A workgroup of 8 wavefronts
+// takes NF * 16 of their rows and MF * 16 of M; its wavefronts take k in turn, in
+// blocks of U * 32, and feed the MFMAs straight from memory (the weights are used
+// once or a few times: LDS would only add a copy, and barriers).  Their sums are
+// joined through LDS in a fixed order.  Rows past M or N read the last row and are
+// not stored.
 template <typename T, bool GATED, int NF, int MF, int U>
 __global__ __launch_bounds__(512) void k_rows(Gemm g, Partial q) {
     typedef typename Vec8<T>::type vec;
@@ -110,7 +111,7 @@ __global__ __launch_bounds__(512) void k_rows(Gemm g, Partial q) {
     __shared__ float sums[NW][NF * H * MF][256];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int r = lane & 15, kg = (lane >> 4) * 8;
-    const int64_t n0 = (int64_t)blockIdx.x * NF * 16;
+    const int64_t n0 = (int64_t)blockIdx.x * NF * 16, m0 = (int64_t)blockIdx.z * MF * 16;
     const int K = (int)g.K;
     // chunk of k of this workgroup, in whole blocks of all its wavefronts
     const int blocks = (K + STEP - 1) / STEP;
@@ -123,7 +124,7 @@ __global__ __launch_bounds__(512) void k_rows(Gemm g, Partial q) {
         for (int f = 0; f < NF; ++f)
             wp[h * NF + f] = reinterpret_cast<const T *>(g.n[h].p) + min(n0 + f * 16 + r, g.N - 1) * g.n[h].ld + kg;
 #pragma unroll
-    for (int j = 0; j < MF; ++j) xp[j] = reinterpret_cast<const T *>(g.m[0].p) + min((int64_t)(j * 16 + r), g.M - 1) * g.m[0].ld + kg;
+    for (int j = 0; j < MF; ++j) xp[j] = reinterpret_cast<const T *>(g.m[0].p) + min(m0 + j * 16 + r, g.M - 1) * g.m[0].ld + kg;
 
     f32x4 acc[H * NF][MF] = {};
     for (int b = b0 + wave; b < b1; b += NW) {
@@ -137,6 +138,7 @@ __global__ __launch_bounds__(512) void k_rows(Gemm g, Partial q) {
 #pragma unroll
                 for (int j = 0; j < MF; ++j) __builtin_memcpy(&x[s][j], xp[j] + k + s * 32, 16);
             }
+            __builtin_amdgcn_sched_barrier(0);  // every load of the block goes out before the first product
 #pragma unroll
             for (int s = 0; s < U; ++s)
 #pragma unroll
@@ -178,7 +180,7 @@ __global__ __launch_bounds__(512) void k_rows(Gemm g, Partial q) {
     // one output per thread: row m of M, 16 consecutive n
     for (int i = threadIdx.x; i < NF * MF * 256; i += 512) {
         const int f = i / (MF * 256), j = i / 256 % MF, at = i & 255;
-        const int64_t m = j * 16 + (at >> 4), n = n0 + f * 16 + (at & 15);
+        const int64_t m = m0 + j * 16 + (at >> 4), n = n0 + f * 16 + (at & 15);
         if (m >= g.M || n >= g.N) continue;
         float z[1] = {0.0f}, u[1] = {0.0f};
 #pragma unroll
@@ -222,15 +224,16 @@ __device__ inline i32x4 buffer_at(uint64_t base, uint32_t bytes) {
     return i32x4{uni((int)(uint32_t)base), uni((int)((uint32_t)(base >> 32) & 0xffffu)), uni((int)bytes), kRsrcWord3};
 }
 
-// 16 bytes per lane straight from memory to LDS: lane i's land at lds + 16 * i.
+// 16 bytes per lane straight from memory to LDS: lane i's land at lds + AT + 16 * i.
 // Inline asm: after the compiler's own LDS-DMA builtin every LDS read waits for
 // all loads in flight.  The statement has no outputs; the waits are wait_vm().
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
+template <int AT>
 __device__ inline void dma16(i32x4 r, uint32_t voff, uint32_t soff, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(voff),
-                 "s"(r), "s"(soff)
-                 : "memory", "m0");
+    asm volatile("s_add_u32 m0, %0, %4\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(voff),
+                 "s"(r), "s"(soff), "n"(AT)
+                 : "memory", "scc", "m0");
 }
 #pragma clang diagnostic pop
 template <int N>
@@ -279,43 +282,52 @@ struct Side {
         }
     }
 
-    // The loads of one stage: k0 .. k0 + BK of the rows at p (the tile's first row;
-    // `rows` of them in the matrix).  Rows past the matrix and k past K read as 0;
-    // a chunk that K cuts is completed by mend().  The buffer's range is rounded up
-    // to whole chunks: the bytes past the matrix's end lie in the aligned 16 bytes
-    // that hold its last element, and never reach a result.
-    struct Stage {
+    // Where the next stage's loads read: BK k of the rows at the buffer's base.  Rows
+    // past the matrix and k past K read as 0; a chunk that K cuts is completed by
+    // mend().  The buffer's range is rounded up to whole chunks: the bytes past the
+    // matrix's end lie in the aligned 16 bytes that hold its last element, and never
+    // reach a result.
+    struct Cursor {
         i32x4 rs;
         uint32_t so;
-        bool in;  // this lane's chunk begins below K
     };
-    __device__ Stage stage(const T *p, int64_t ld, int rows, int K, int k0) const {
-        Stage st;
+    // at k0 of the rows at p (the tile's first row; `rows` of them in the matrix)
+    __device__ static Cursor open(const T *p, int64_t ld, int rows, int K, int k0) {
+        Cursor c;
         const int r = min(rows, B);
         if constexpr (ACROSS) {
             const int n = min(K - k0, BK);
-            const uint32_t range = rows > 0 ? (((uint32_t)(n - 1) * (uint32_t)ld + r) * 2u + 15u) & ~15u : 0u;
-            st.rs = buffer_at(reinterpret_cast<uint64_t>(p) + (uint64_t)k0 * (uint64_t)ld * 2u, range);
-            st.so = 0;
+            const uint32_t range = (((uint32_t)(n - 1) * (uint32_t)ld + r) * 2u + 15u) & ~15u;
+            c.rs = buffer_at(reinterpret_cast<uint64_t>(p) + (uint64_t)k0 * (uint64_t)ld * 2u, range);
+            c.so = 0;
         } else {
-            const uint32_t range = rows > 0 ? (((uint32_t)(r - 1) * (uint32_t)ld + (uint32_t)K) * 2u + 15u) & ~15u : 0u;
-            st.rs = buffer_at(reinterpret_cast<uint64_t>(p), range);
-            st.so = rows > 0 ? uni(k0 * 2) : 0;
-            st.in = kc < K - k0;
+            const uint32_t range = (((uint32_t)(r - 1) * (uint32_t)ld + (uint32_t)K) * 2u + 15u) & ~15u;
+            c.rs = buffer_at(reinterpret_cast<uint64_t>(p), range);
+            c.so = uni(k0 * 2);
         }
-        return st;
+        return c;
     }
-    __device__ void load(const Stage &st, int i, uint32_t lds, int wave) const {
-        const uint32_t at = uni(lds + (i * NW + wave) * 1024);
-        if constexpr (ACROSS) dma16(st.rs, off[i], st.so, at);
-        else dma16(st.rs, st.in ? off[i] : kInvalidOffset, st.so, at);
+    // to the stage that follows; step = BK * ld * 2 (ACROSS)
+    __device__ static void advance(Cursor &c, uint32_t step) {
+        if constexpr (ACROSS) {
+            const uint64_t base = ((uint64_t)(uint32_t)c.rs[1] << 32 | (uint32_t)c.rs[0]) + step;
+            c.rs[0] = uni((int)(uint32_t)base);
+            c.rs[1] = uni((int)(uint32_t)(base >> 32));
+        } else {
+            c.so = uni(c.so + BK * 2);
+        }
+    }
+    // load I of a stage; `in`: this lane's chunk begins below K (rows along k)
+    template <int I>
+    __device__ void load(const Cursor &c, bool in, uint32_t lds) const {
+        if constexpr (ACROSS) dma16<I * NW * 1024>(c.rs, off[I], c.so, lds);
+        else dma16<I * NW * 1024>(c.rs, in ? off[I] : kInvalidOffset, c.so, lds);
     }
 
-    // The chunk that holds k = K - 1 of a stage at k0, in LDS: its elements past K
-    // become +0 (after this wavefront's loads have landed).
-    __device__ void mend(uint8_t *lds, int K, int k0, int wave, int lane) const {
+    // The chunk that holds k = K - 1, in LDS: its elements past K become +0 (after this
+    // wavefront's loads have landed); n: k of K's last stage.
+    __device__ void mend(uint8_t *lds, int n, int wave, int lane) const {
         if constexpr (!ACROSS) {
-            const int n = K - k0;  // valid k of the stage
             if (kc != (n & ~7)) return;
 #pragma unroll
             for (int i = 0; i < loads; ++i) {
@@ -380,6 +392,15 @@ __device__ inline void pick(int j, F &&f) {
     }
 }
 
+// f(0), .. f(N - 1) with constants
+template <int N, int I = 0, typename F>
+__device__ inline void each(F &&f) {
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>{});
+        each<N, I + 1>(f);
+    }
+}
+
 struct TileArgs {
     Gemm g;
     Partial part;
@@ -431,8 +452,8 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
         t -= q.chunk * one * g.batch;
         q.z = t / one;
         t -= q.z * one;
-        q.s0 = uni((int)((int64_t)ns * q.chunk / a.part.split));
-        q.s1 = uni((int)((int64_t)ns * (q.chunk + 1) / a.part.split));
+        q.s0 = uni(ns * q.chunk / a.part.split);
+        q.s1 = uni(ns * (q.chunk + 1) / a.part.split);
         const int band = t / (8 * a.ntiles), in = t - band * 8 * a.ntiles;
         const int h = min(8, a.mtiles - band * 8);
         q.m0 = (int64_t)(band * 8 + in % h) * BM;
@@ -448,58 +469,71 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
     mside.setup_reads(lane);
 
     // The loads run over the stages of all tiles without a break, S stages ahead of
-    // the products: the next tile's first stages arrive while this one's results go out.
-    struct Loads {
-        typename NSide::Stage n, n1;
-        typename MSide::Stage m;
-        uint32_t at;
-    };
+    // the products: the next tile's first stages arrive while this one's results go
+    // out.  A run of stages below K differs from stage to stage by one addition per
+    // operand; what else there is to work out (60 and more scalar instructions, which
+    // a wavefront's products do not hide) is done between runs.
     constexpr bool TWO = NA && !MA;  // the sum may have two parts (MA: there may be two batches)
-    const T *np0, *np1 = nullptr, *mp0, *mp1 = nullptr;
-    int nrows, mrows, ltile = 0, lstage = 0, lend = 0, lslot = 0;
-    auto enter = [&](int i) {
-        const Tile q = tile_at(i);
-        const int64_t no = NA ? q.n0 : q.n0 * nld, mo = MA ? q.m0 : q.m0 * mld;
-        np0 = reinterpret_cast<const T *>(g.n[0].p) + no;
-        if constexpr (GATED || TWO) np1 = reinterpret_cast<const T *>(g.n[1].p) + no;
-        mp0 = reinterpret_cast<const T *>(MA && q.z ? g.m[1].p : g.m[0].p) + mo;
-        if constexpr (TWO) mp1 = reinterpret_cast<const T *>(g.m[1].p) + mo;
-        lstage = q.s0;
-        lend = q.s1;
-        nrows = uni((int)min(g.N - q.n0, (int64_t)NROWS));
-        mrows = uni((int)min(g.M - q.m0, (int64_t)BM));
-    };
-    auto next_loads = [&]() {
-        if (ltile >= mine) {  // past the last stage: rows 0, the loads write zeros that are not used
-            nrows = 0;
-            mrows = 0;
+    typename NSide::Cursor nc, nc1;
+    typename MSide::Cursor mc;
+    bool in = true;
+    uint32_t lat = lds0 + wave * 1024, nstep = uni((int)(BK * nld * 2)), mstep = uni((int)(BK * mld * 2));
+    int run = 0, lstage = 0, lend = 0, ltile = -1, lslot = 0;
+    int cuts = 0;  // slots that hold a chunk which K cuts
+    bool last_of_k = false;
+    auto next_run = [&]() {
+        if (lstage == lend) ++ltile;
+        if (ltile >= mine) {  // past the last stage: the loads write zeros that are not used
+            nc.rs[2] = nc1.rs[2] = mc.rs[2] = 0;
+            nc.so = nc1.so = mc.so = 0;
+            last_of_k = false;
+            run = 1;
+            return;
         }
+        const Tile q = tile_at(ltile);
+        if (lstage == lend) {
+            lstage = q.s0;
+            lend = q.s1;
+        }
+        const int64_t no = NA ? q.n0 : q.n0 * nld, mo = MA ? q.m0 : q.m0 * mld;
+        const int nrows = uni((int)min(g.N - q.n0, (int64_t)NROWS)), mrows = uni((int)min(g.M - q.m0, (int64_t)BM));
         const bool second = TWO && lstage >= sp;
-        const int k0 = (second ? lstage - sp : lstage) * BK;
-        Loads l;
-        l.at = lds0 + lslot * Cfg::stage;
-        l.n = nside.stage(second ? np1 : np0, nld, nrows, K, k0);
-        if constexpr (GATED) l.n1 = nside.stage(np1, nld, nrows, K, k0);
-        l.m = mside.stage(second ? mp1 : mp0, mld, mrows, K, k0);
+        const int st = second ? lstage - sp : lstage, k0 = st * BK;
+        nc = NSide::open(reinterpret_cast<const T *>(second ? g.n[1].p : g.n[0].p) + no, nld, nrows, K, k0);
+        if constexpr (GATED) nc1 = NSide::open(reinterpret_cast<const T *>(g.n[1].p) + no, nld, nrows, K, k0);
+        mc = MSide::open(reinterpret_cast<const T *>(second || (MA && q.z) ? g.m[1].p : g.m[0].p) + mo, mld, mrows, K, k0);
+        in = (NA ? mside.kc : nside.kc) < K - k0;  // both sides' lanes hold the same chunk column
+        run = uni(k0 + BK <= K ? min(K / BK - st, lend - lstage) : 1);
+        last_of_k = k0 + BK > K && (K & 7) != 0;
+        lstage += run;
+    };
+    // The stage that is loaded next: begin, its loads 0 .. L - 1, end.
+    const int tail = K & (BK - 1);
+    auto begin_stage = [&]() {
+        if (run == 0) next_run();
+        --run;
+    };
+    auto load = [&](auto which) {
+        constexpr int i = decltype(which)::value;
+        if constexpr (i < NSide::loads) nside.template load<i>(nc, in, lat);
+        else if constexpr (i < NL) nside.template load<i - NSide::loads>(nc1, in, lat + NSide::bytes);
+        else if constexpr (i < L) mside.template load<i - NL>(mc, in, lat + BN * BK * 2);
+    };
+    auto end_stage = [&]() {
+        cuts = last_of_k ? cuts | 1 << lslot : cuts & ~(1 << lslot);
+        NSide::advance(nc, nstep);
+        if constexpr (GATED) NSide::advance(nc1, nstep);
+        MSide::advance(mc, mstep);
         lslot = lslot + 1 == S ? 0 : lslot + 1;
-        if (++lstage == lend && ++ltile < mine) enter(ltile);
-        return l;
+        lat = lslot == 0 ? lds0 + wave * 1024 : lat + Cfg::stage;
     };
-    auto load = [&](const Loads &l, int i) {
-        if (i < NSide::loads) nside.load(l.n, i, l.at, wave);
-        else if (i < NL) nside.load(l.n1, i - NSide::loads, l.at + NSide::bytes, wave);
-        else mside.load(l.m, i - NL, l.at + BN * BK * 2, wave);
-    };
-    const bool cut = (K & 7) != 0;
-    // stage s of a tile, landed in `slot`: zeros past K
-    auto mend = [&](int s, int slot) {
-        if (!cut) return;
-        const int k0 = (TWO && s >= sp ? s - sp : s) * BK;
-        if (k0 + BK < K) return;
+    // zeros past K in the stage that has landed in `slot`
+    auto mend = [&](int slot) {
+        if ((cuts >> slot & 1) == 0) return;
         uint8_t *at = smem + slot * Cfg::stage;
-        nside.mend(at, K, k0, wave, lane);
-        if constexpr (GATED) nside.mend(at + NSide::bytes, K, k0, wave, lane);
-        mside.mend(at + BN * BK * 2, K, k0, wave, lane);
+        nside.mend(at, tail, wave, lane);
+        if constexpr (GATED) nside.mend(at + NSide::bytes, tail, wave, lane);
+        mside.mend(at + BN * BK * 2, tail, wave, lane);
     };
 
     f32x4 acc[TN][TM];
@@ -513,14 +547,13 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
 
     int slot = 0;
     if (ns > 0) {
-        enter(0);
         for (int s = 0; s < S; ++s) {
-            const Loads l = next_loads();
-#pragma unroll
-            for (int i = 0; i < L; ++i) load(l, i);
+            begin_stage();
+            each<L>(load);
+            end_stage();
         }
         wait_vm<L *(S - 1)>();
-        mend(tile_at(0).s0, 0);
+        mend(0);
         lds_barrier();
     }
 
@@ -528,11 +561,11 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
     // replaced by the next step's as soon as the row has been issued.  In the last
     // step the next stage's fragments are read, and the stage S ahead is loaded into
     // this one's buffer.
-    auto multiply = [&](int next) {  // next: the stage that follows
+    auto multiply = [&]() {
         const uint8_t *cur = smem + slot * Cfg::stage;
         slot = slot + 1 == S ? 0 : slot + 1;
         const uint8_t *nxt = smem + slot * Cfg::stage;
-        const Loads l = next_loads();
+        begin_stage();
 #pragma unroll
         for (int q = 0; q < KS; ++q) {
             const bool last = q == KS - 1;
@@ -545,7 +578,7 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
                 if (i == 0 && last) {
                     // the next stage has landed, this one has been read by all
                     wait_vm<L *(S - 2)>();
-                    mend(next, slot);
+                    mend(slot);
                     lds_barrier();
                 }
                 if (i == 0) {
@@ -555,13 +588,14 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
                 fa[i] = readn(from, i, fq);
                 if (last) {  // the loads, spread over the rows
                     constexpr int rate = (L + TN - 1) / TN;
-#pragma unroll
-                    for (int e = 0; e < rate; ++e)
-                        if (i * rate + e < L) load(l, i * rate + e);
+                    pick<TN>(i, [&](auto ic) {
+                        each<rate>([&](auto e) { load(std::integral_constant<int, decltype(ic)::value * rate + decltype(e)::value>{}); });
+                    });
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
+        end_stage();
     };
 
 #pragma unroll 1
@@ -577,7 +611,7 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
 #pragma unroll
             for (int i = 0; i < TN; ++i) fa[i] = readn(smem + slot * Cfg::stage, i, 0);
 #pragma unroll 1
-            for (int s = q.s0; s < q.s1; ++s) multiply(s + 1 < q.s1 ? s + 1 : ti + 1 < mine ? tile_at(ti + 1).s0 : 0);
+            for (int s = q.s0; s < q.s1; ++s) multiply();
         }
 
         // Results straight from the registers.  Exchanging the odd rows of 16 lanes of
@@ -669,7 +703,7 @@ int resident(const void *kern, int nt, int lds, int *groups) {
 }
 
 // How a product runs.
-enum Path { kRows16, kRows32, kRows64, kTile128, kTile256 };
+enum Path { kRows16, kRows32, kRows64, kTile64, kTile128, kTile256, kRows64x2 };
 struct Plan {
     Path path;
     int split;  // chunks of k
@@ -727,8 +761,8 @@ int launch(const Gemm &g, const Partial &q, hipStream_t stream) {
 
 template <typename T, bool GATED, int NF, int MF, int U>
 int launch_rows(const Gemm &g, const Partial &q, hipStream_t stream) {
-    hipLaunchKernelGGL((k_rows<T, GATED, NF, MF, U>), dim3((unsigned)((g.N + NF * 16 - 1) / (NF * 16)), q.split), dim3(512), 0,
-                       stream, g, q);
+    hipLaunchKernelGGL((k_rows<T, GATED, NF, MF, U>), dim3((unsigned)((g.N + NF * 16 - 1) / (NF * 16)), q.split,
+                       (unsigned)((g.M + MF * 16 - 1) / (MF * 16))), dim3(512), 0, stream, g, q);
     if (int rc = check_hip(hipGetLastError(), "k_rows")) return rc;
     return q.split > 1 ? join<T, GATED>(g, q, stream) : SA_OK;
 }
@@ -738,9 +772,12 @@ int by_size(const Gemm &g, const Plan &p, const Partial &q, hipStream_t stream) 
     if constexpr (!NA) {
         if (p.path == kRows16) return launch_rows<T, GATED, 1, 1, GATED ? 4 : 8>(g, q, stream);
         if (p.path == kRows32) return launch_rows<T, GATED, 1, 2, 4>(g, q, stream);
+        if constexpr (!GATED)
+            if (p.path == kRows64x2) return launch_rows<T, GATED, 2, 4, 4>(g, q, stream);
         if (p.path == kRows64) return launch_rows<T, GATED, 1, 4, GATED ? 2 : 4>(g, q, stream);
     }
     if (p.path == kTile256) return launch<T, NA, MA, GATED, 256, 256, 2, 4, 64, 2>(g, q, stream);
+    if (p.path == kTile64) return launch<T, NA, MA, GATED, 128, 64, 2, 2, 64, 3>(g, q, stream);
     return launch<T, NA, MA, GATED, 128, 128, 2, 2, 64, 2>(g, q, stream);
 }
 
@@ -762,7 +799,7 @@ Shape shape_of(const Operand &o, int64_t r, int64_t K) { return o.across ? Shape
 bool rows_aligned(const Operand &o, const Shape &s) { return aligned(o.p, 16) && (s.rows <= 1 || o.ld % 8 == 0); }
 
 // Does the product's path read rows of any alignment?
-bool any_rows(const Plan &p) { return p.path <= kRows64; }
+bool any_rows(const Plan &p) { return p.path <= kRows64 || p.path == kRows64x2; }
 
 // Visits the operands that have to be copied to aligned rows.
 template <typename F>
