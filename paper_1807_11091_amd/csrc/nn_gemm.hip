@@ -17,12 +17,20 @@ namespace sa {
 namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 __device__ inline f32x4 mfma(Vec8<__bf16>::type a, Vec8<__bf16>::type b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 __device__ inline f32x4 mfma(Vec8<_Float16>::type a, Vec8<_Float16>::type b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
+__device__ inline f32x16 mfma32(Vec8<__bf16>::type a, Vec8<__bf16>::type b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ inline f32x16 mfma32(Vec8<_Float16>::type a, Vec8<_Float16>::type b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
 }
 
 // V (cnt < V at a row's end) consecutive outputs from their sums z (and u).
@@ -205,11 +213,11 @@ __global__ __launch_bounds__(512) void k_rows(Gemm g, Partial q) {
 //
 // LDS layouts (64 banks of 4 bytes, 256 bytes per clock):
 //   - an operand whose rows run along k: [row][BK], the 16-byte chunks of a row
-//     XOR-swizzled so that the 16 rows of a fragment read hit 16 distinct chunks;
+//     XOR-swizzled so that the rows of a fragment read hit distinct banks;
 //   - an operand whose rows run across k: [k][rows], read by ds_read_b64_tr_b16,
 //     which hands each lane 4 consecutive k of its row (16 lanes transpose a block
-//     of 4 k by 16 rows); its 32-byte units are XOR-swizzled by k, so that 8 k of
-//     one unit hit distinct banks.
+//     of 4 k by 16 rows); its 64-byte units are XOR-swizzled by k, so that the 4 k
+//     and 32 rows of half a fragment read hit distinct banks.
 // The swizzle is applied to the source address (the DMA writes lanes in order).
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
@@ -255,7 +263,7 @@ struct Side {
 
     // swizzle of row r (rows along k) or of k (rows across)
     __device__ static int swz(int r) {
-        if constexpr (ACROSS) return (r & 3) | ((r >> 3) & 1) << 2;
+        if constexpr (ACROSS) return r & 3;
         else if constexpr (BK == 64) return (r >> 1) & 7;
         else return (((r >> 2) ^ (r >> 3)) & 1) << 1 | ((r >> 3) & 1);
     }
@@ -266,7 +274,7 @@ struct Side {
         const int at = (i * NW + wave) * 64 + lane;
         row = at / cpr;
         const int c = at % cpr;
-        chunk = ACROSS ? (((c >> 1) ^ swz(row)) << 1) | (c & 1) : c ^ swz(row);
+        chunk = ACROSS ? (((c >> 2) ^ swz(row)) << 2) | (c & 3) : c ^ swz(row);
     }
 
     uint32_t off[loads];  // byte offset of each load from the tile's origin
@@ -341,26 +349,27 @@ struct Side {
         }
     }
 
-    // Lane offsets of fragment reads: fragment f holds rows 16 f + (0 .. 15).
-    static constexpr int nfo = ACROSS ? 1 : BK / 32;
+    // Lane offsets of fragment reads: fragment f holds rows 32 f + (0 .. 31), step q
+    // the k 16 q + (0 .. 15), 8 of them in each half of the wavefront.
+    static constexpr int nfo = ACROSS ? 1 : BK / 16;
     uint32_t fo[nfo];
 
     __device__ void setup_reads(int lane) {
-        const int r = lane & 15, g = lane >> 4;
         if constexpr (ACROSS) {
-            const int k = g * 8 + (r >> 2), piece = lane & 3;
-            fo[0] = k * pitch + (swz(k) << 5) + piece * 8;
+            const int k = (lane >> 5) * 8 + ((lane & 15) >> 2);
+            fo[0] = k * pitch + (swz(k) << 6) + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
         } else {
+            const int r = lane & 31;
 #pragma unroll
-            for (int q = 0; q < BK / 32; ++q) fo[q] = r * pitch + (((q * 4 + g) ^ swz(r)) << 4);
+            for (int q = 0; q < BK / 16; ++q) fo[q] = r * pitch + (((q * 2 + (lane >> 5)) ^ swz(r)) << 4);
         }
     }
 
-    // fragment f (rows from row0, a multiple of 16) of k step q
+    // fragment f (rows from row0, a multiple of 32) of step q
     __device__ vec read(const uint8_t *lds, int row0, int f, int q) const {
         if constexpr (ACROSS) {
             typedef __attribute__((address_space(3))) s16x4 *ptr;
-            const uint8_t *p = lds + (fo[0] ^ (uint32_t)((row0 / 16 + f) << 5)) + q * 32 * pitch;
+            const uint8_t *p = lds + (fo[0] ^ (uint32_t)((row0 / 32 + f) << 6)) + q * 16 * pitch;
             union {
                 s16x4 h[2];
                 vec v;
@@ -369,7 +378,7 @@ struct Side {
             x.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ptr)(p + 4 * pitch));
             return x.v;
         } else {
-            return *reinterpret_cast<const vec *>(lds + fo[q] + (row0 + 16 * f) * pitch);
+            return *reinterpret_cast<const vec *>(lds + fo[q] + (row0 + 32 * f) * pitch);
         }
     }
 };
@@ -377,7 +386,7 @@ struct Side {
 template <int BN, int BM, int WN, int WM, int BK, int S>
 struct TileCfg {
     static constexpr int NW = WN * WM, NT = NW * 64;
-    static constexpr int TN = BN / WN / 16, TM = BM / WM / 16;  // fragments of a wavefront
+    static constexpr int TN = BN / WN / 32, TM = BM / WM / 32;  // fragments of a wavefront
     static constexpr int stage = (BN + BM) * BK * 2;
     static constexpr int lds = S * stage;
     static_assert(lds <= kMaxLds, "LDS");
@@ -414,9 +423,11 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
     using NSide = Side<T, NA, NROWS, BK, Cfg::NW>;
     using MSide = Side<T, MA, BM, BK, Cfg::NW>;
     typedef typename Vec8<T>::type vec;
-    constexpr int TN = Cfg::TN, TM = Cfg::TM, KS = BK / 32, TNG = GATED ? TN / 2 : TN;
+    constexpr int TN = Cfg::TN, TM = Cfg::TM, KS = BK / 16, TNG = GATED ? TN / 2 : TN;
     constexpr int NL = NSide::loads * (GATED ? 2 : 1), L = NL + MSide::loads;  // loads of a stage
-    static_assert(KS == 2 && TNG % 2 == 0 && L * (S - 1) < 64, "shape");
+    constexpr int RATE = (L + 2 * TN - 1) / (2 * TN);                  // loads that go out with a fragment row
+    constexpr int L0 = TN * RATE < L ? TN * RATE : L;                  // loads of a stage in the step that begins it
+    static_assert(BK == 64 && TNG > 0 && L * (S - 1) < 64, "shape");
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
 
     const Gemm &g = a.g;
@@ -536,7 +547,7 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
         mside.mend(at + BN * BK * 2, tail, wave, lane);
     };
 
-    f32x4 acc[TN][TM];
+    f32x16 acc[TN][TM];
     vec fa[TN], fb[2][TM];
     const int nrow = wn * (NROWS / WN), mrow = wm * (BM / WM);
     auto readn = [&](const uint8_t *st, int i, int q) {
@@ -547,25 +558,29 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
 
     int slot = 0;
     if (ns > 0) {
-        for (int s = 0; s < S; ++s) {
+        for (int s = 0; s + 1 < S; ++s) {
             begin_stage();
             each<L>(load);
             end_stage();
         }
-        wait_vm<L *(S - 1)>();
+        begin_stage();
+        each<L0>(load);  // the others go out with the first products
+        wait_vm<L *(S - 2) + L0>();
         mend(0);
         lds_barrier();
     }
 
     // A stage is multiplied, a fragment row at a time; each row's N fragment is
     // replaced by the next step's as soon as the row has been issued.  In the last
-    // step the next stage's fragments are read, and the stage S ahead is loaded into
-    // this one's buffer.
+    // step the next stage's fragments are read, and the loads of the stage S ahead,
+    // into this one's buffer, begin; they end in the first step of the next stage.
+    // The 32 x 32 x 16 MFMA keeps the matrix core busy for 32 clocks, behind which a
+    // row's reads and loads disappear; of 16 x 16 x 32 ones, 16 clocks each, a row of
+    // four with one read and one load took 85 clocks instead of 64.
     auto multiply = [&]() {
         const uint8_t *cur = smem + slot * Cfg::stage;
         slot = slot + 1 == S ? 0 : slot + 1;
         const uint8_t *nxt = smem + slot * Cfg::stage;
-        begin_stage();
 #pragma unroll
         for (int q = 0; q < KS; ++q) {
             const bool last = q == KS - 1;
@@ -574,28 +589,30 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
 #pragma unroll
             for (int i = 0; i < TN; ++i) {
 #pragma unroll
-                for (int j = 0; j < TM; ++j) acc[i][j] = mfma(fa[i], fb[q & 1][j], acc[i][j]);
+                for (int j = 0; j < TM; ++j) acc[i][j] = mfma32(fa[i], fb[q & 1][j], acc[i][j]);
                 if (i == 0 && last) {
                     // the next stage has landed, this one has been read by all
                     wait_vm<L *(S - 2)>();
                     mend(slot);
                     lds_barrier();
+                    begin_stage();
                 }
                 if (i == 0) {
 #pragma unroll
                     for (int j = 0; j < TM; ++j) fb[(q + 1) & 1][j] = readm(from, j, fq);
                 }
                 fa[i] = readn(from, i, fq);
-                if (last) {  // the loads, spread over the rows
-                    constexpr int rate = (L + TN - 1) / TN;
+                if (last || q == 0) {
                     pick<TN>(i, [&](auto ic) {
-                        each<rate>([&](auto e) { load(std::integral_constant<int, decltype(ic)::value * rate + decltype(e)::value>{}); });
+                        constexpr int at = decltype(ic)::value * RATE;
+                        if (last) each<RATE>([&](auto e) { load(std::integral_constant<int, at + decltype(e)::value>{}); });
+                        else each<RATE>([&](auto e) { load(std::integral_constant<int, TN * RATE + at + decltype(e)::value>{}); });
                     });
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
+            if (q == 0) end_stage();
         }
-        end_stage();
     };
 
 #pragma unroll 1
@@ -604,7 +621,7 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
 #pragma unroll
         for (int i = 0; i < TN; ++i)
 #pragma unroll
-            for (int j = 0; j < TM; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int j = 0; j < TM; ++j) acc[i][j] = f32x16{};
         if (ns > 0) {
 #pragma unroll
             for (int j = 0; j < TM; ++j) fb[0][j] = readm(smem + slot * Cfg::stage, j, 0);
@@ -614,37 +631,39 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
             for (int s = q.s0; s < q.s1; ++s) multiply();
         }
 
-        // Results straight from the registers.  Exchanging the odd rows of 16 lanes of
-        // one fragment with the even ones of the next leaves 8 consecutive n in each
-        // lane: 16-byte stores, 64 bytes of a row by 4 lanes.
+        // Results straight from the registers.  A lane holds 4 consecutive n of every 8;
+        // exchanging the upper half of one group of 8 with the lower half of the next
+        // leaves 8 consecutive n in each lane, for 16-byte stores.
         void *Y = q.z ? g.y1 : g.e.Y;
-        const int64_t nb = q.n0 + nrow + ((lane >> 4) & 1) * 16 + (lane >> 5) * 8;
+        constexpr int H = GATED ? 2 : 1;
 #pragma unroll 1
-        for (int j = 0; j < TM; ++j) {
-            f32x4 t[TN];
-            pick<TM>(j, [&](auto jc) {
-#pragma unroll
-                for (int i = 0; i < TN; ++i) t[i] = acc[i][decltype(jc)::value];
+        for (int f = 0; f < TNG * TM; ++f) {
+            f32x16 t[H];
+            pick<TNG * TM>(f, [&](auto fc) {
+                constexpr int i = decltype(fc)::value / TM, j = decltype(fc)::value % TM;
+                t[0] = acc[i][j];
+                if constexpr (GATED) t[GATED] = acc[TNG + i][j];
             });
 #pragma unroll
-            for (int i = 0; i < TN; i += 2)
+            for (int h = 0; h < H; ++h)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const auto w = __builtin_amdgcn_permlane16_swap(__float_as_uint(t[i][e]), __float_as_uint(t[i + 1][e]),
-                                                                    false, false);
-                    t[i][e] = __uint_as_float(w[0]);
-                    t[i + 1][e] = __uint_as_float(w[1]);
+                for (int e = 0; e < 16; e += e % 4 == 3 ? 5 : 1) {
+                    const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(t[h][e]), __float_as_uint(t[h][e + 4]), false,
+                                                                    false);
+                    t[h][e] = __uint_as_float(w[0]);
+                    t[h][e + 4] = __uint_as_float(w[1]);
                 }
-            const int64_t m = q.m0 + mrow + j * 16 + (lane & 15);
+            const int64_t m = q.m0 + mrow + f % TM * 32 + (lane & 31);
+            const int64_t nb = q.n0 + nrow + f / TM * 32 + (lane >> 5) * 8;
             if (m >= g.M) continue;
 #pragma unroll
-            for (int i = 0; i < TNG; i += 2) {
-                const int64_t n = nb + i * 16;
+            for (int r = 0; r < 16; r += 8) {
+                const int64_t n = nb + r * 2;
                 float z[8], u[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    z[e] = t[i + (e >> 2)][e & 3];
-                    if constexpr (GATED) u[e] = t[TNG + i + (e >> 2)][e & 3];
+                    z[e] = t[0][r + e];
+                    if constexpr (GATED) u[e] = t[GATED][r + e];
                 }
                 if (n >= g.N) continue;
                 if (a.part.split > 1) {
