@@ -325,11 +325,17 @@ struct Side {
             c.so = uni(c.so + BK * 2);
         }
     }
-    // load I of a stage; `in`: this lane's chunk begins below K (rows along k)
+    // Lanes whose chunk begins at `k` or past it read zeros from here on (rows along k;
+    // offsets are below 2^31, one with the top bit set lies past every range).
+    __device__ void limit(int k) {
+        if constexpr (!ACROSS)
+#pragma unroll
+            for (int i = 0; i < loads; ++i) off[i] = kc < k ? off[i] & ~kInvalidOffset : off[i] | kInvalidOffset;
+    }
+    // load I of a stage
     template <int I>
-    __device__ void load(const Cursor &c, bool in, uint32_t lds) const {
-        if constexpr (ACROSS) dma16<I * NW * 1024>(c.rs, off[I], c.so, lds);
-        else dma16<I * NW * 1024>(c.rs, in ? off[I] : kInvalidOffset, c.so, lds);
+    __device__ void load(const Cursor &c, uint32_t lds) const {
+        dma16<I * NW * 1024>(c.rs, off[I], c.so, lds);
     }
 
     // The chunk that holds k = K - 1, in LDS: its elements past K become +0 (after this
@@ -487,17 +493,14 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
     constexpr bool TWO = NA && !MA;  // the sum may have two parts (MA: there may be two batches)
     typename NSide::Cursor nc, nc1;
     typename MSide::Cursor mc;
-    bool in = true;
     uint32_t lat = lds0 + wave * 1024, nstep = uni((int)(BK * nld * 2)), mstep = uni((int)(BK * mld * 2));
     int run = 0, lstage = 0, lend = 0, ltile = -1, lslot = 0;
-    int cuts = 0;  // slots that hold a chunk which K cuts
-    bool last_of_k = false;
+    int cuts = 0;  // slots that hold, or will, a chunk which K cuts
     auto next_run = [&]() {
         if (lstage == lend) ++ltile;
         if (ltile >= mine) {  // past the last stage: the loads write zeros that are not used
             nc.rs[2] = nc1.rs[2] = mc.rs[2] = 0;
             nc.so = nc1.so = mc.so = 0;
-            last_of_k = false;
             run = 1;
             return;
         }
@@ -513,9 +516,10 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
         nc = NSide::open(reinterpret_cast<const T *>(second ? g.n[1].p : g.n[0].p) + no, nld, nrows, K, k0);
         if constexpr (GATED) nc1 = NSide::open(reinterpret_cast<const T *>(g.n[1].p) + no, nld, nrows, K, k0);
         mc = MSide::open(reinterpret_cast<const T *>(second || (MA && q.z) ? g.m[1].p : g.m[0].p) + mo, mld, mrows, K, k0);
-        in = (NA ? mside.kc : nside.kc) < K - k0;  // both sides' lanes hold the same chunk column
+        nside.limit(K - k0);
+        mside.limit(K - k0);
+        if (k0 + BK > K && (K & 7) != 0) cuts |= 1 << lslot;
         run = uni(k0 + BK <= K ? min(K / BK - st, lend - lstage) : 1);
-        last_of_k = k0 + BK > K && (K & 7) != 0;
         lstage += run;
     };
     // The stage that is loaded next: begin, its loads 0 .. L - 1, end.
@@ -526,12 +530,11 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
     };
     auto load = [&](auto which) {
         constexpr int i = decltype(which)::value;
-        if constexpr (i < NSide::loads) nside.template load<i>(nc, in, lat);
-        else if constexpr (i < NL) nside.template load<i - NSide::loads>(nc1, in, lat + NSide::bytes);
-        else if constexpr (i < L) mside.template load<i - NL>(mc, in, lat + BN * BK * 2);
+        if constexpr (i < NSide::loads) nside.template load<i>(nc, lat);
+        else if constexpr (i < NL) nside.template load<i - NSide::loads>(nc1, lat + NSide::bytes);
+        else if constexpr (i < L) mside.template load<i - NL>(mc, lat + BN * BK * 2);
     };
     auto end_stage = [&]() {
-        cuts = last_of_k ? cuts | 1 << lslot : cuts & ~(1 << lslot);
         NSide::advance(nc, nstep);
         if constexpr (GATED) NSide::advance(nc1, nstep);
         MSide::advance(mc, mstep);
@@ -540,7 +543,9 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
     };
     // zeros past K in the stage that has landed in `slot`
     auto mend = [&](int slot) {
-        if ((cuts >> slot & 1) == 0) return;
+        if (uni(cuts >> slot & 1) == 0) return;
+        asm volatile("" ::: "memory");  // a branch of its own: nothing below is done without it
+        cuts &= ~(1 << slot);
         uint8_t *at = smem + slot * Cfg::stage;
         nside.mend(at, tail, wave, lane);
         if constexpr (GATED) nside.mend(at + NSide::bytes, tail, wave, lane);
