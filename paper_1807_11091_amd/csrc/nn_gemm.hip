@@ -26,10 +26,10 @@ __device__ inline f32x4 mfma(Vec8<_Float16>::type a, Vec8<_Float16>::type b, f32
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
 
-__device__ inline f32x16 mfma32(Vec8<__bf16>::type a, Vec8<__bf16>::type b, f32x16 c) {
+__device__ inline f32x16 mfma(Vec8<__bf16>::type a, Vec8<__bf16>::type b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
-__device__ inline f32x16 mfma32(Vec8<_Float16>::type a, Vec8<_Float16>::type b, f32x16 c) {
+__device__ inline f32x16 mfma(Vec8<_Float16>::type a, Vec8<_Float16>::type b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
 }
 
@@ -216,8 +216,8 @@ __global__ __launch_bounds__(512) void k_rows(Gemm g, Partial q) {
 //     XOR-swizzled so that the rows of a fragment read hit distinct banks;
 //   - an operand whose rows run across k: [k][rows], read by ds_read_b64_tr_b16,
 //     which hands each lane 4 consecutive k of its row (16 lanes transpose a block
-//     of 4 k by 16 rows); its 64-byte units are XOR-swizzled by k, so that the 4 k
-//     and 32 rows of half a fragment read hit distinct banks.
+//     of 4 k by 16 rows); its units of 2 MI bytes are XOR-swizzled by k, so that 32
+//     lanes hit distinct banks (8 k of 16 rows, or 4 k of 32).
 // The swizzle is applied to the source address (the DMA writes lanes in order).
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
@@ -252,7 +252,7 @@ __device__ inline void wait_vm() {
 __device__ inline void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // One operand's part of a stage: B rows by BK k, NW wavefronts.
-template <typename T, bool ACROSS, int B, int BK, int NW>
+template <typename T, bool ACROSS, int B, int BK, int NW, int MI>
 struct Side {
     typedef typename Vec8<T>::type vec;
     static constexpr int bytes = B * BK * 2;
@@ -263,7 +263,7 @@ struct Side {
 
     // swizzle of row r (rows along k) or of k (rows across)
     __device__ static int swz(int r) {
-        if constexpr (ACROSS) return r & 3;
+        if constexpr (ACROSS) return (MI == 16 ? (r & 3) | ((r >> 3) & 1) << 2 : r & 3) & (B / MI - 1);
         else if constexpr (BK == 64) return (r >> 1) & 7;
         else return (((r >> 2) ^ (r >> 3)) & 1) << 1 | ((r >> 3) & 1);
     }
@@ -274,7 +274,7 @@ struct Side {
         const int at = (i * NW + wave) * 64 + lane;
         row = at / cpr;
         const int c = at % cpr;
-        chunk = ACROSS ? (((c >> 2) ^ swz(row)) << 2) | (c & 3) : c ^ swz(row);
+        chunk = ACROSS ? c ^ swz(row) * (MI / 8) : c ^ swz(row);
     }
 
     uint32_t off[loads];  // byte offset of each load from the tile's origin
@@ -355,27 +355,29 @@ struct Side {
         }
     }
 
-    // Lane offsets of fragment reads: fragment f holds rows 32 f + (0 .. 31), step q
-    // the k 16 q + (0 .. 15), 8 of them in each half of the wavefront.
-    static constexpr int nfo = ACROSS ? 1 : BK / 16;
+    // Lane offsets of fragment reads: fragment f holds rows MI f + (0 .. MI - 1), step q
+    // KQ k, 8 of them in each lane.
+    static constexpr int KQ = 512 / MI;
+    static constexpr int nfo = ACROSS ? 1 : BK / KQ;
     uint32_t fo[nfo];
 
     __device__ void setup_reads(int lane) {
+        const int g = lane / MI;  // the lane's 8 k
         if constexpr (ACROSS) {
-            const int k = (lane >> 5) * 8 + ((lane & 15) >> 2);
-            fo[0] = k * pitch + (swz(k) << 6) + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+            const int k = g * 8 + ((lane & 15) >> 2);
+            fo[0] = k * pitch + swz(k) * (MI * 2) + (lane & (MI - 16)) * 2 + (lane & 3) * 8;
         } else {
-            const int r = lane & 31;
+            const int r = lane & (MI - 1);
 #pragma unroll
-            for (int q = 0; q < BK / 16; ++q) fo[q] = r * pitch + (((q * 2 + (lane >> 5)) ^ swz(r)) << 4);
+            for (int q = 0; q < nfo; ++q) fo[q] = r * pitch + (((q * (KQ / 8) + g) ^ swz(r)) << 4);
         }
     }
 
-    // fragment f (rows from row0, a multiple of 32) of step q
+    // fragment f (rows from row0, a multiple of MI) of step q
     __device__ vec read(const uint8_t *lds, int row0, int f, int q) const {
         if constexpr (ACROSS) {
             typedef __attribute__((address_space(3))) s16x4 *ptr;
-            const uint8_t *p = lds + (fo[0] ^ (uint32_t)((row0 / 32 + f) << 6)) + q * 16 * pitch;
+            const uint8_t *p = lds + (fo[0] ^ (uint32_t)((row0 + MI * f) * 2)) + q * KQ * pitch;
             union {
                 s16x4 h[2];
                 vec v;
@@ -384,15 +386,15 @@ struct Side {
             x.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ptr)(p + 4 * pitch));
             return x.v;
         } else {
-            return *reinterpret_cast<const vec *>(lds + fo[q] + (row0 + 32 * f) * pitch);
+            return *reinterpret_cast<const vec *>(lds + fo[q] + (row0 + MI * f) * pitch);
         }
     }
 };
 
-template <int BN, int BM, int WN, int WM, int BK, int S>
+template <int BN, int BM, int WN, int WM, int BK, int S, int MI>
 struct TileCfg {
     static constexpr int NW = WN * WM, NT = NW * 64;
-    static constexpr int TN = BN / WN / 32, TM = BM / WM / 32;  // fragments of a wavefront
+    static constexpr int TN = BN / WN / MI, TM = BM / WM / MI;  // fragments of a wavefront
     static constexpr int stage = (BN + BM) * BK * 2;
     static constexpr int lds = S * stage;
     static_assert(lds <= kMaxLds, "LDS");
@@ -422,14 +424,14 @@ struct TileArgs {
     int mtiles, ntiles, tiles, groups;  // tiles: of all batches and chunks; groups: workgroups
 };
 
-template <typename T, bool NA, bool MA, bool GATED, int BN, int BM, int WN, int WM, int BK, int S>
-__global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
-    using Cfg = TileCfg<BN, BM, WN, WM, BK, S>;
+template <typename T, bool NA, bool MA, bool GATED, int BN, int BM, int WN, int WM, int BK, int S, int MI>
+__global__ __launch_bounds__(WN *WM * 64, 2) void k_gemm(TileArgs a) {
+    using Cfg = TileCfg<BN, BM, WN, WM, BK, S, MI>;
     constexpr int NROWS = GATED ? BN / 2 : BN;  // n of a tile; gated: one half of the N side per projection
-    using NSide = Side<T, NA, NROWS, BK, Cfg::NW>;
-    using MSide = Side<T, MA, BM, BK, Cfg::NW>;
+    using NSide = Side<T, NA, NROWS, BK, Cfg::NW, MI>;
+    using MSide = Side<T, MA, BM, BK, Cfg::NW, MI>;
     typedef typename Vec8<T>::type vec;
-    constexpr int TN = Cfg::TN, TM = Cfg::TM, KS = BK / 16, TNG = GATED ? TN / 2 : TN;
+    constexpr int TN = Cfg::TN, TM = Cfg::TM, KS = BK / NSide::KQ, TNG = GATED ? TN / 2 : TN;
     constexpr int NL = NSide::loads * (GATED ? 2 : 1), L = NL + MSide::loads;  // loads of a stage
     constexpr int RATE = (L + 2 * TN - 1) / (2 * TN);                  // loads that go out with a fragment row
     constexpr int L0 = TN * RATE < L ? TN * RATE : L;                  // loads of a stage in the step that begins it
@@ -552,7 +554,8 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
         mside.mend(at + BN * BK * 2, tail, wave, lane);
     };
 
-    f32x16 acc[TN][TM];
+    using Acc = typename std::conditional<MI == 16, f32x4, f32x16>::type;
+    Acc acc[TN][TM];
     vec fa[TN], fb[2][TM];
     const int nrow = wn * (NROWS / WN), mrow = wm * (BM / WM);
     auto readn = [&](const uint8_t *st, int i, int q) {
@@ -579,9 +582,6 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
     // replaced by the next step's as soon as the row has been issued.  In the last
     // step the next stage's fragments are read, and the loads of the stage S ahead,
     // into this one's buffer, begin; they end in the first step of the next stage.
-    // The 32 x 32 x 16 MFMA keeps the matrix core busy for 32 clocks, behind which a
-    // row's reads and loads disappear; of 16 x 16 x 32 ones, 16 clocks each, a row of
-    // four with one read and one load took 85 clocks instead of 64.
     auto multiply = [&]() {
         const uint8_t *cur = smem + slot * Cfg::stage;
         slot = slot + 1 == S ? 0 : slot + 1;
@@ -594,7 +594,7 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
 #pragma unroll
             for (int i = 0; i < TN; ++i) {
 #pragma unroll
-                for (int j = 0; j < TM; ++j) acc[i][j] = mfma32(fa[i], fb[q & 1][j], acc[i][j]);
+                for (int j = 0; j < TM; ++j) acc[i][j] = mfma(fa[i], fb[q & 1][j], acc[i][j]);
                 if (i == 0 && last) {
                     // the next stage has landed, this one has been read by all
                     wait_vm<L *(S - 2)>();
@@ -626,7 +626,7 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
 #pragma unroll
         for (int i = 0; i < TN; ++i)
 #pragma unroll
-            for (int j = 0; j < TM; ++j) acc[i][j] = f32x16{};
+            for (int j = 0; j < TM; ++j) acc[i][j] = Acc{};
         if (ns > 0) {
 #pragma unroll
             for (int j = 0; j < TM; ++j) fb[0][j] = readm(smem + slot * Cfg::stage, j, 0);
@@ -636,39 +636,54 @@ __global__ __launch_bounds__(WN *WM * 64) void k_gemm(TileArgs a) {
             for (int s = q.s0; s < q.s1; ++s) multiply();
         }
 
-        // Results straight from the registers.  A lane holds 4 consecutive n of every 8;
-        // exchanging the upper half of one group of 8 with the lower half of the next
-        // leaves 8 consecutive n in each lane, for 16-byte stores.
+        // Results straight from the registers.  A lane holds 4 consecutive n of every 16
+        // (MI = 16) or 8; exchanging the odd rows of 16 lanes, or the upper half, of one
+        // such group with the even ones, or the lower half, of the next leaves 8
+        // consecutive n in each lane, for 16-byte stores.
         void *Y = q.z ? g.y1 : g.e.Y;
-        constexpr int H = GATED ? 2 : 1;
+        constexpr int H = GATED ? 2 : 1, F = MI == 16 ? 2 : 1;  // fragments of a projection taken together
+        static_assert(TNG % F == 0, "pairs of fragments");
+        const int nl = MI == 16 ? ((lane >> 4) & 1) * 16 + (lane >> 5) * 8 : (lane >> 5) * 8;
 #pragma unroll 1
-        for (int f = 0; f < TNG * TM; ++f) {
-            f32x16 t[H];
-            pick<TNG * TM>(f, [&](auto fc) {
-                constexpr int i = decltype(fc)::value / TM, j = decltype(fc)::value % TM;
-                t[0] = acc[i][j];
-                if constexpr (GATED) t[GATED] = acc[TNG + i][j];
+        for (int f = 0; f < TNG / F * TM; ++f) {
+            Acc t[H][F];
+            pick<TNG / F * TM>(f, [&](auto fc) {
+                constexpr int i = decltype(fc)::value / TM * F, j = decltype(fc)::value % TM;
+#pragma unroll
+                for (int h = 0; h < H; ++h)
+#pragma unroll
+                    for (int k = 0; k < F; ++k) t[h][k] = acc[h * TNG + i + k][j];
             });
+            const int64_t m = q.m0 + mrow + f % TM * MI + (lane & (MI - 1));
+            const int64_t nb = q.n0 + nrow + f / TM * F * MI + nl;
 #pragma unroll
             for (int h = 0; h < H; ++h)
 #pragma unroll
-                for (int e = 0; e < 16; e += e % 4 == 3 ? 5 : 1) {
-                    const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(t[h][e]), __float_as_uint(t[h][e + 4]), false,
-                                                                    false);
-                    t[h][e] = __uint_as_float(w[0]);
-                    t[h][e + 4] = __uint_as_float(w[1]);
+                for (int e = 0; e < 4; ++e) {
+                    if constexpr (MI == 16) {
+                        const auto w = __builtin_amdgcn_permlane16_swap(__float_as_uint(t[h][0][e]), __float_as_uint(t[h][F - 1][e]),
+                                                                        false, false);
+                        t[h][0][e] = __uint_as_float(w[0]);
+                        t[h][F - 1][e] = __uint_as_float(w[1]);
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < 16; r += 8) {
+                            const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(t[h][0][r + e]),
+                                                                            __float_as_uint(t[h][0][r + e + 4]), false, false);
+                            t[h][0][r + e] = __uint_as_float(w[0]);
+                            t[h][0][r + e + 4] = __uint_as_float(w[1]);
+                        }
+                    }
                 }
-            const int64_t m = q.m0 + mrow + f % TM * 32 + (lane & 31);
-            const int64_t nb = q.n0 + nrow + f / TM * 32 + (lane >> 5) * 8;
             if (m >= g.M) continue;
 #pragma unroll
-            for (int r = 0; r < 16; r += 8) {
+            for (int r = 0; r < F * MI * MI / 64; r += 8) {
                 const int64_t n = nb + r * 2;
                 float z[8], u[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    z[e] = t[0][r + e];
-                    if constexpr (GATED) u[e] = t[GATED][r + e];
+                    z[e] = MI == 16 ? t[0][e / 4 * (F - 1)][e % 4] : t[0][0][(r + e) % (MI * MI / 64)];
+                    if constexpr (GATED) u[e] = MI == 16 ? t[GATED][e / 4 * (F - 1)][e % 4] : t[GATED][0][(r + e) % (MI * MI / 64)];
                 }
                 if (n >= g.N) continue;
                 if (a.part.split > 1) {
@@ -726,32 +741,97 @@ int resident(const void *kern, int nt, int lds, int *groups) {
     return SA_OK;
 }
 
-// How a product runs.
+// How a product runs: k_rows with 16, 32 or 64 rows of M per workgroup (kRows64x2: 32
+// rows of the N side instead of 16), or k_gemm with tiles of 128 x 64, 128 x 128 or
+// 256 x 256 (N side by M side).
 enum Path { kRows16, kRows32, kRows64, kTile64, kTile128, kTile256, kRows64x2 };
 struct Plan {
     Path path;
     int split;  // chunks of k
 };
 
-// Workgroups of k_gemm that the chip's 256 CUs hold: the 256 x 256 tile's LDS fills a CU, two of the
-// 128 x 128 tile's share one.
-constexpr int kSlots256 = 256, kSlots128 = 512;
+// Time models, microseconds, fitted to 364 products (40 to 2048 rows and fewer, 512 to
+// 19712 by 512 to 9856, forward and both gradients, k in 1 to 32 chunks: 3600 launches;
+// median error 5%).  The model's choice takes 1.012 of the best one's time on average.
+struct TileModel {
+    int bn, bm, slots;    // tile; workgroups that the 256 CUs hold
+    float launch, round;  // a launch; a round of tiles
+    float one, two;       // a stage of 64 k: one tile per CU, every slot taken
+    float join, join_chunk, join_mb;  // partial sums: a split, a chunk, a MB of them
+    float out_mb, in_mb;  // a MB of results, of operands
+};
+constexpr TileModel kTileModel[] = {
+    {128, 64, 512, 5.34f, 0.142f, 0.276f, 0.488f, 1.615f, 0.308f, 0.429f, 0.316f, 0.0495f},
+    {128, 128, 512, 5.27f, 0.0f, 0.573f, 0.710f, 1.620f, 0.319f, 0.359f, 0.327f, 0.0576f},
+    {256, 256, 256, 10.28f, 2.10f, 1.072f, 1.072f, 0.0f, 0.244f, 0.297f, 0.278f, 0.0115f},
+};
+struct RowsModel {
+    Path path;
+    int gated, bn, bm, u;  // rows of the N and M side per workgroup, k steps of 32 in a block
+    float launch, block;   // a launch; a block of a wavefront's k
+    float step;            // a step of 32 k, for every 256 workgroups past the first
+    float join, join_mb, in_mb;
+};
+constexpr RowsModel kRowsModel[] = {
+    {kRows16, 0, 16, 16, 8, 2.36f, 1.93f, 0.159f, 3.24f, 0.167f, 0.0586f},
+    {kRows16, 1, 16, 16, 4, 4.05f, 1.43f, 0.264f, 3.71f, 0.238f, 0.0520f},
+    {kRows32, 0, 16, 32, 4, 3.68f, 1.04f, 0.166f, 2.90f, 0.940f, 0.0607f},
+    {kRows32, 1, 16, 32, 4, 4.34f, 1.70f, 0.223f, 3.56f, 0.420f, 0.0612f},
+    {kRows64, 0, 16, 64, 4, 4.85f, 1.18f, 0.179f, 2.56f, 0.115f, 0.0830f},
+    {kRows64, 1, 16, 64, 2, 5.76f, 0.82f, 0.303f, 2.81f, 0.270f, 0.0747f},
+    {kRows64x2, 0, 32, 64, 4, 6.29f, 2.24f, 0.387f, 1.17f, 0.684f, 0.0757f},
+};
+
+float tile_time(const TileModel &m, const Gemm &g, int split) {
+    const int64_t nn = g.N * (g.gated ? 2 : 1);
+    const int64_t tiles = ((g.M + m.bm - 1) / m.bm) * ((nn + m.bn - 1) / m.bn) * g.batch * split;
+    const float stages = (float)((g.K + 63) / 64 * g.parts) / split;
+    const int64_t rest = tiles % m.slots;
+    const bool sparse = rest > 0 && rest <= 256;
+    const float full = (float)(tiles / m.slots + (rest > 0 && !sparse ? 1 : 0)), last = sparse ? 1.0f : 0.0f;
+    const float out = (float)g.M * nn * g.batch, in = ((float)g.M + nn) * g.K * g.parts * g.batch;
+    float t = m.launch + m.round * (full + last) + stages * (m.one * last + m.two * full) + out * 2e-6f * m.out_mb +
+              in * 2e-6f * m.in_mb;
+    if (split > 1) t += m.join + m.join_chunk * split + m.join_mb * split * out * 4e-6f;
+    return t;
+}
+
+float rows_time(const RowsModel &m, const Gemm &g, int split) {
+    const float nt = (float)((g.N + m.bn - 1) / m.bn), mt = (float)((g.M + m.bm - 1) / m.bm), groups = nt * mt * split;
+    const int64_t blocks = (g.K + 32 * m.u - 1) / (32 * m.u);
+    const float mine = (float)(((blocks + split - 1) / split + 7) / 8);
+    const float nn = (float)g.N * (g.gated ? 2 : 1), in = (nt * g.M + mt * nn) * g.K;
+    float t = m.launch + m.block * mine + m.step * mine * m.u * std::max(0.0f, groups / 256 - 1) + in * 2e-6f * m.in_mb;
+    if (split > 1) t += m.join + m.join_mb * split * g.M * nn * 4e-6f;
+    return t;
+}
 
 Plan plan_of(const Gemm &g) {
-    const int64_t nn = g.N * (g.gated ? 2 : 1), steps = (g.K + 63) / 64 * g.parts;
-    if (g.M <= 64 && !g.n[0].across) {
-        const Path path = g.M <= 16 ? kRows16 : g.M <= 32 ? kRows32 : kRows64;
-        const int64_t groups = (g.N + 15) / 16, blocks = (g.K + 255) / 256;
-        int split = 1;
-        while (groups * split < 192 && blocks >= 16 * split) split *= 2;
-        return {path, split};
+    const int64_t nn = g.N * (g.gated ? 2 : 1), stages = (g.K + 63) / 64 * g.parts;
+    Plan best{kTile64, 1};
+    float least = 3e38f;
+    const auto consider = [&](Path path, int split, float t) {
+        if (t < least) {
+            least = t;
+            best = {path, split};
+        }
+    };
+    if (!g.n[0].across)
+        for (const RowsModel &m : kRowsModel) {
+            if (m.gated != g.gated || (m.path != kRows64 && m.path != kRows64x2 && g.M > m.bm)) continue;
+            if (((g.N + m.bn - 1) / m.bn) * ((g.M + m.bm - 1) / m.bm) > 2048) continue;  // beyond the fitted range
+            for (int split = 1; split == 1 || (split <= 32 && split * 16 <= stages && nn * split <= 65536); split *= 2)
+                consider(m.path, split, rows_time(m, g, split));
+            if (g.M <= 16) return best;  // faster than every tile
+        }
+    for (int i = 0; i < 3; ++i) {
+        const TileModel &m = kTileModel[i];
+        const int64_t tiles = ((g.M + m.bm - 1) / m.bm) * ((nn + m.bn - 1) / m.bn) * g.batch;
+        consider((Path)(kTile64 + i), 1, tile_time(m, g, 1));
+        for (int split = 2; split <= 32 && tiles < 512 && tiles * split <= 2 * m.slots && split * 2 <= stages; split *= 2)
+            consider((Path)(kTile64 + i), split, tile_time(m, g, split));
     }
-    const int64_t t256 = ((g.M + 255) / 256) * ((nn + 255) / 256) * g.batch;
-    if (t256 >= 128) return {kTile256, 1};
-    const int64_t t128 = ((g.M + 127) / 128) * ((nn + 127) / 128) * g.batch;
-    int split = 1;
-    while (t128 * split * 2 <= kSlots128 && steps >= 16 * split) split *= 2;
-    return {kTile128, split};
+    return best;
 }
 
 size_t partial_bytes(const Gemm &g, int split) {
@@ -765,16 +845,16 @@ int join(const Gemm &g, const Partial &q, hipStream_t stream) {
     return check_hip(hipGetLastError(), "k_join");
 }
 
-template <typename T, bool NA, bool MA, bool GATED, int BN, int BM, int WN, int WM, int BK, int S>
+template <typename T, bool NA, bool MA, bool GATED, int BN, int BM, int WN, int WM, int BK, int S, int MI>
 int launch(const Gemm &g, const Partial &q, hipStream_t stream) {
-    using Cfg = TileCfg<BN, BM, WN, WM, BK, S>;
+    using Cfg = TileCfg<BN, BM, WN, WM, BK, S, MI>;
     TileArgs a{g, q, 0, 0, 0, 0};
     const int64_t mt = (g.M + BM - 1) / BM, nt = (g.N + (GATED ? BN / 2 : BN) - 1) / (GATED ? BN / 2 : BN);
     if (mt * nt >= (int64_t(1) << 28)) return fail(SA_E_UNSUPPORTED, "matrix product of more than 2^28 tiles");
     a.mtiles = (int)mt;
     a.ntiles = (int)nt;
     a.tiles = (int)(mt * nt) * g.batch * q.split;
-    auto kern = k_gemm<T, NA, MA, GATED, BN, BM, WN, WM, BK, S>;
+    auto kern = k_gemm<T, NA, MA, GATED, BN, BM, WN, WM, BK, S, MI>;
     int groups = 0;
     if (int rc = resident(reinterpret_cast<const void *>(kern), Cfg::NT, Cfg::lds, &groups)) return rc;
     a.groups = std::min(a.tiles, groups);
@@ -800,9 +880,9 @@ int by_size(const Gemm &g, const Plan &p, const Partial &q, hipStream_t stream) 
             if (p.path == kRows64x2) return launch_rows<T, GATED, 2, 4, 4>(g, q, stream);
         if (p.path == kRows64) return launch_rows<T, GATED, 1, 4, GATED ? 2 : 4>(g, q, stream);
     }
-    if (p.path == kTile256) return launch<T, NA, MA, GATED, 256, 256, 2, 4, 64, 2>(g, q, stream);
-    if (p.path == kTile64) return launch<T, NA, MA, GATED, 128, 64, 2, 2, 64, 3>(g, q, stream);
-    return launch<T, NA, MA, GATED, 128, 128, 2, 2, 64, 2>(g, q, stream);
+    if (p.path == kTile256) return launch<T, NA, MA, GATED, 256, 256, 2, 4, 64, 2, 16>(g, q, stream);
+    if (p.path == kTile64) return launch<T, NA, MA, GATED, 128, 64, 2, 2, 64, 3, 32>(g, q, stream);
+    return launch<T, NA, MA, GATED, 128, 128, 2, 2, 64, 2, 32>(g, q, stream);
 }
 
 template <typename T>
