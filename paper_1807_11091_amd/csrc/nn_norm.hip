@@ -26,26 +26,92 @@ namespace {
 
 constexpr int kV = 8;  // elements per vector
 
-// Two sums over the TPR threads of a row, in a fixed order; every thread of the
-// row receives them.  Holds barriers when a row has several wavefronts.
+// Rows of TPR threads each that a workgroup of the register kernels takes at a time.
 template <int TPR>
-__device__ inline void row_sums(float &a, float &b, float2 *tmp) {
+struct Rows {
+    static constexpr int per_group = TPR <= 64 ? 8 : TPR <= 128 ? 4 : TPR <= 256 ? 2 : 1;
+    static constexpr int threads = TPR * per_group;
+};
+
+// Two sums over the TPR threads of a row, in a fixed order; every thread of the row
+// receives them.  A row of several wavefronts needs a barrier, which every thread of
+// the workgroup calls; tmp holds two sets, used in turn (turn = 0, 1, 0, ..), so that
+// one barrier per call is enough.
+template <int TPR, int NT>
+__device__ inline void row_sums(float &a, float &b, float2 (*tmp)[NT / 64], int turn) {
     a = wave_sum_f32(a);
     b = wave_sum_f32(b);
     if constexpr (TPR > 64) {
-        const int wave = threadIdx.x >> 6;
-        __syncthreads();  // the sums of the call before have been read
-        if ((threadIdx.x & 63) == 0) tmp[wave] = make_float2(a, b);
+        const int wave = threadIdx.x >> 6, first = threadIdx.x / TPR * (TPR / 64);
+        if ((threadIdx.x & 63) == 0) tmp[turn & 1][wave] = make_float2(a, b);
         __syncthreads();
         a = b = 0.0f;
 #pragma unroll
         for (int w = 0; w < TPR / 64; ++w) {
-            const float2 t = tmp[w];
+            const float2 t = tmp[turn & 1][first + w];
             a += t.x;
             b += t.y;
         }
     }
 }
+
+// A chunk as it is stored, in words, so that it takes no more registers than that.
+template <typename T>
+struct Raw {
+    static constexpr int kWords = kV * sizeof(T) / 4, kPer = 4 / sizeof(T);
+    unsigned w[kWords];
+
+    // The chunk at c of a row.  One load for every thread and no branch, so that nothing
+    // waits for it here: where the row ends inside the chunk or before it, the row's last
+    // kV values, which place() moves.  SHORT: rows of fewer than kV columns, by value.
+    template <bool SHORT>
+    __device__ void load(const T *row, int c, int cols) {
+        if constexpr (!SHORT) {
+            __builtin_memcpy(w, row + (unsigned)min(c, cols - kV), sizeof w);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) w[i] = 0;
+#pragma unroll
+            for (int i = 0; i < kV - 1; ++i)
+                if (i < cols) {
+                    unsigned bits = 0;
+                    __builtin_memcpy(&bits, row + i, sizeof(T));
+                    w[i / kPer] |= bits << (i % kPer * 16);
+                }
+        }
+    }
+
+    // The loaded values to their places, zeros from column end on.
+    template <bool SHORT>
+    __device__ void place(int c, int cols, int end) {
+        const int by = SHORT ? 0 : c + kV - cols;
+        if (by > 0 && by < kV) {
+#pragma unroll
+            for (int step = kWords / 2; step > 0; step /= 2)
+                if (by / kPer & step)
+#pragma unroll
+                    for (int i = 0; i < kWords; ++i) w[i] = i + step < kWords ? w[i + step] : 0;
+            if (by % kPer)
+#pragma unroll
+                for (int i = 0; i < kWords; ++i) w[i] = w[i] >> 16 | (i + 1 < kWords ? w[i + 1] << 16 : 0);
+        }
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) w[i] = c < end ? w[i] : 0;
+    }
+
+    __device__ float operator[](int i) const {
+        T v;
+        const unsigned x = w[i / kPer] >> i % kPer * 16;
+        __builtin_memcpy(&v, &x, sizeof v);
+        return (float)v;
+    }
+
+    // Keeps the compiler from carrying what it computed from the values in registers.
+    __device__ void renew() {
+#pragma unroll
+        for (unsigned &x : w) asm volatile("" : "+v"(x));
+    }
+};
 
 template <typename T>
 __device__ inline void load_chunk(const T *row, int c, int cols, float (&v)[kV]) {
@@ -76,28 +142,30 @@ struct FwdArgs {
     float *mean, *rstd;
 };
 
-template <typename T, int TPR, int CH>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_ln_fwd(FwdArgs a) {
-    constexpr int NT = TPR < 256 ? 256 : TPR, RPB = NT / TPR;
-    __shared__ float2 tmp[NT / 64];
+template <typename T, int TPR, int CH, bool SHORT>
+__global__ __launch_bounds__(Rows<TPR>::threads) void k_ln_fwd(FwdArgs a) {
+    constexpr int NT = Rows<TPR>::threads, RPB = Rows<TPR>::per_group;
+    __shared__ float2 tmp[2][NT / 64];
     const int t = threadIdx.x % TPR;
-    const int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
-    if (row >= a.rows) return;  // whole wavefronts, and whole workgroups where TPR >= 256
-    const T *x = reinterpret_cast<const T *>(a.X) + row * a.ldx;
+    const int64_t row = (int64_t)blockIdx.x * RPB + __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
+    const bool in = row < a.rows;  // threads of a row past the last one only keep the barriers
+    const T *x = reinterpret_cast<const T *>(a.X) + (in ? row : 0) * a.ldx;
     const float n = (float)a.cols;
+    Raw<T> raw[CH];
     float v[CH][kV];
     float s = 0.0f, q = 0.0f;
 #pragma unroll
+    for (int k = 0; k < CH; ++k) raw[k].template load<SHORT>(x, (k * TPR + t) * kV, a.cols);
+#pragma unroll
     for (int k = 0; k < CH; ++k) {
-        const int c = (k * TPR + t) * kV;
-        if (c < a.cols) load_chunk<T>(x, c, a.cols, v[k]);
-        else
+        raw[k].template place<SHORT>((k * TPR + t) * kV, a.cols, a.cols);
 #pragma unroll
-            for (int i = 0; i < kV; ++i) v[k][i] = 0.0f;
-#pragma unroll
-        for (int i = 0; i < kV; ++i) s += v[k][i];
+        for (int i = 0; i < kV; ++i) {
+            v[k][i] = raw[k][i];
+            s += v[k][i];
+        }
     }
-    row_sums<TPR>(s, q, tmp);
+    row_sums<TPR, NT>(s, q, tmp, 0);
     const float mean = s / n;
     s = q = 0.0f;
 #pragma unroll
@@ -108,7 +176,8 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_ln_fwd(FwdArgs a) {
             v[k][i] = d;
             s = fmaf(d, d, s);
         }
-    row_sums<TPR>(s, q, tmp);
+    row_sums<TPR, NT>(s, q, tmp, 1);
+    if (!in) return;
     const float rstd = 1.0f / sqrtf(s / n + a.eps);
     if (t == 0) {
         if (a.mean) a.mean[row] = mean;
@@ -132,7 +201,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_ln_fwd(FwdArgs a) {
 template <typename T>
 __global__ __launch_bounds__(1024) void k_ln_fwd_long(FwdArgs a) {
     constexpr int NT = 1024;
-    __shared__ float2 tmp[NT / 64];
+    __shared__ float2 tmp[2][NT / 64];
     const int64_t row = blockIdx.x;
     const T *x = reinterpret_cast<const T *>(a.X) + row * a.ldx;
     T *y = reinterpret_cast<T *>(a.Y) + row * a.ldy;
@@ -143,7 +212,7 @@ __global__ __launch_bounds__(1024) void k_ln_fwd_long(FwdArgs a) {
 #pragma unroll
         for (int i = 0; i < kV; ++i) s += v[i];
     }
-    row_sums<NT>(s, q, tmp);
+    row_sums<NT, NT>(s, q, tmp, 0);
     const float mean = s / n;
     s = q = 0.0f;
     for (int c = threadIdx.x * kV; c < a.cols; c += NT * kV) {
@@ -154,7 +223,7 @@ __global__ __launch_bounds__(1024) void k_ln_fwd_long(FwdArgs a) {
             s = fmaf(d, d, s);
         }
     }
-    row_sums<NT>(s, q, tmp);
+    row_sums<NT, NT>(s, q, tmp, 1);
     const float rstd = 1.0f / sqrtf(s / n + a.eps);
     if (threadIdx.x == 0) {
         if (a.mean) a.mean[row] = mean;
@@ -181,64 +250,114 @@ struct BwdArgs {
     float *part;  // [workgroups][2][cols]: sums of dy xn and of dy, or NULL
 };
 
-// Workgroup b takes the rows b * RPB + i, then those gridDim.x * RPB further on,
-// and keeps its columns' sums of dy xn and dy in registers.
-template <typename T, int TPR, int CH>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_ln_bwd(BwdArgs a) {
-    constexpr int NT = TPR < 256 ? 256 : TPR, RPB = NT / TPR;
-    __shared__ float2 tmp[NT / 64];
+// Workgroup b takes the rows b * RPB + i, then those gridDim.x * RPB further on, and
+// keeps its columns' sums of dy xn and dy in registers.  A CU holds one workgroup, so
+// what hides the memory's latency is the next row's x and dy, read while this row is
+// worked on: into a second set of registers, the loop unrolled by two, since a copy
+// from one set to the other would wait for them.  Bound by memory: 16384 x 4096
+// bfloat16 in 104 us with the joining of the sums, 5.2 TB/s over x, dy and dx (209 us
+// without the next row, 134 us when copies waited for it).
+template <typename T, int TPR, int CH, bool SHORT>
+__global__ __launch_bounds__(Rows<TPR>::threads, 2) void k_ln_bwd(BwdArgs a) {
+    constexpr int NT = Rows<TPR>::threads, RPB = Rows<TPR>::per_group;
+    constexpr bool kAhead = CH <= 2;  // more would not fit the registers
+    __shared__ float2 tmp[2][NT / 64];
     __shared__ float join[RPB > 1 ? RPB * TPR * kV : 1];
-    const int t = threadIdx.x % TPR, rg = threadIdx.x / TPR;
+    const int t = threadIdx.x % TPR, rg = __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
     const float n = (float)a.cols;
-    float sg[CH][kV], sb[CH][kV];
+    float gamma[CH][kV], sg[CH][kV], sb[CH][kV];
+    auto weigh = [&](int k) { load_param(a.gamma, (k * TPR + t) * kV, a.cols, 1.0f, gamma[k]); };
 #pragma unroll
-    for (int k = 0; k < CH; ++k)
+    for (int k = 0; k < CH; ++k) {
+        if constexpr (kAhead) weigh(k);
 #pragma unroll
         for (int i = 0; i < kV; ++i) sg[k][i] = sb[k][i] = 0.0f;
-    for (int64_t row = (int64_t)blockIdx.x * RPB + rg; row < a.rows; row += (int64_t)gridDim.x * RPB) {
+    }
+    struct Row {
+        Raw<T> x[CH], y[CH];
+        float mean, rstd;
+    };
+    auto fetch = [&](Row &w, int64_t row) {
+        row = min(row, a.rows - 1);
         const T *x = reinterpret_cast<const T *>(a.X) + row * a.ldx;
         const T *dy = reinterpret_cast<const T *>(a.dY) + row * a.lddy;
-        const float mean = a.mean[row], rstd = a.rstd[row];
-        float xn[CH][kV], d[CH][kV];
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            const int c = (k * TPR + t) * kV;
+            w.x[k].template load<SHORT>(x, c, a.cols);
+            w.y[k].template load<SHORT>(dy, c, a.cols);
+        }
+        w.mean = a.mean[row];
+        w.rstd = a.rstd[row];
+    };
+    // Works on the row in w while next is read, after this row's dR.
+    auto work = [&](Row &w, int64_t row, Row &next, int64_t next_row, int turn) {
+        Raw<T> r[CH];
+        if (a.dR) {
+            const T *dr = reinterpret_cast<const T *>(a.dR) + min(row, a.rows - 1) * a.lddr;
+#pragma unroll
+            for (int k = 0; k < CH; ++k) r[k].template load<SHORT>(dr, (k * TPR + t) * kV, a.cols);
+        }
+        if constexpr (kAhead) fetch(next, next_row);
+        const int end = row < a.rows ? a.cols : 0;  // 0: a row past the last one
         float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
             const int c = (k * TPR + t) * kV;
-            float g[kV];
-#pragma unroll
-            for (int i = 0; i < kV; ++i) xn[k][i] = d[k][i] = 0.0f;
-            if (c < a.cols) {
-                load_chunk<T>(x, c, a.cols, xn[k]);
-                load_chunk<T>(dy, c, a.cols, d[k]);
-            }
-            load_param(a.gamma, c, a.cols, 1.0f, g);
+            w.x[k].template place<SHORT>(c, a.cols, end);
+            w.y[k].template place<SHORT>(c, a.cols, end);
+            if constexpr (!kAhead) weigh(k);
 #pragma unroll
             for (int i = 0; i < kV; ++i) {
-                xn[k][i] = c + i < a.cols ? (xn[k][i] - mean) * rstd : 0.0f;
-                sg[k][i] = fmaf(d[k][i], xn[k][i], sg[k][i]);
-                sb[k][i] += d[k][i];
-                d[k][i] *= g[i];
-                s1 += d[k][i];
-                s2 = fmaf(d[k][i], xn[k][i], s2);
+                const float dy = w.y[k][i], d = dy * gamma[k][i];
+                const float xn = c + i < end ? (w.x[k][i] - w.mean) * w.rstd : 0.0f;
+                sg[k][i] = fmaf(dy, xn, sg[k][i]);
+                sb[k][i] += dy;
+                s1 += d;
+                s2 = fmaf(d, xn, s2);
             }
         }
-        if (!a.dX) continue;  // the same for every thread
-        row_sums<TPR>(s1, s2, tmp);
+        if (!a.dX) return;  // the same for every thread
+        row_sums<TPR, NT>(s1, s2, tmp, turn);
         s1 /= n;
         s2 /= n;
-        const T *dr = a.dR ? reinterpret_cast<const T *>(a.dR) + row * a.lddr : nullptr;
         T *dx = reinterpret_cast<T *>(a.dX) + row * a.lddx;
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
             const int c = (k * TPR + t) * kV;
-            if (c >= a.cols) continue;
-            float r[kV];
+            if (c >= end) continue;
+            w.x[k].renew();
+            w.y[k].renew();
+            if constexpr (!kAhead) weigh(k);
+            float o[kV];
 #pragma unroll
-            for (int i = 0; i < kV; ++i) r[i] = 0.0f;
-            if (dr) load_chunk<T>(dr, c, a.cols, r);
+            for (int i = 0; i < kV; ++i) {
+                const float xn = (w.x[k][i] - w.mean) * w.rstd;
+                o[i] = w.rstd * (w.y[k][i] * gamma[k][i] - s1 - xn * s2);
+            }
+            if (a.dR) {
+                r[k].template place<SHORT>(c, a.cols, a.cols);
 #pragma unroll
-            for (int i = 0; i < kV; ++i) r[i] += rstd * (d[k][i] - s1 - xn[k][i] * s2);
-            store_chunk<T>(dx, c, a.cols, r);
+                for (int i = 0; i < kV; ++i) o[i] += r[k][i];
+            }
+            store_chunk<T>(dx, c, a.cols, o);
+        }
+    };
+    const int64_t step = (int64_t)gridDim.x * RPB;
+    int64_t row = (int64_t)blockIdx.x * RPB + rg;
+    Row one, two;
+    if constexpr (!kAhead) {
+        int turn = 0;
+        for (int64_t base = (int64_t)blockIdx.x * RPB; base < a.rows; base += step, row += step, turn ^= 1) {
+            fetch(one, row);
+            work(one, row, two, 0, turn);
+        }
+    } else {
+        fetch(one, row);
+        for (int64_t base = (int64_t)blockIdx.x * RPB; base < a.rows; base += 2 * step, row += 2 * step) {
+            work(one, row, two, row + step, 0);
+            if (base + step >= a.rows) break;
+            work(two, row + step, one, row + 2 * step, 1);
         }
     }
     if (!a.part) return;
@@ -270,7 +389,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_ln_bwd(BwdArgs a) {
 template <typename T>
 __global__ __launch_bounds__(1024) void k_ln_bwd_long(BwdArgs a) {
     constexpr int NT = 1024;
-    __shared__ float2 tmp[NT / 64];
+    __shared__ float2 tmp[2][NT / 64];
     const float n = (float)a.cols;
     const int64_t row = blockIdx.x;
     const T *x = reinterpret_cast<const T *>(a.X) + row * a.ldx;
@@ -290,7 +409,7 @@ __global__ __launch_bounds__(1024) void k_ln_bwd_long(BwdArgs a) {
             s2 = fmaf(d[i] * g[i], xn, s2);
         }
     }
-    row_sums<NT>(s1, s2, tmp);
+    row_sums<NT, NT>(s1, s2, tmp, 0);
     s1 /= n;
     s2 /= n;
     for (int c = threadIdx.x * kV; c < a.cols; c += NT * kV) {
@@ -323,45 +442,51 @@ __global__ __launch_bounds__(64) void k_ln_params_long(BwdArgs a) {
     p[a.cols + c] = b;
 }
 
-// dgamma and dbeta: the partial sums of n workgroups in their order, four
-// interleaved strands of them by four groups of 64 threads.
-__global__ __launch_bounds__(256) void k_ln_join(const float *part, int n, int cols, float *dgamma, float *dbeta) {
-    __shared__ float tmp[4][64];
-    const int c = blockIdx.x * 64 + (threadIdx.x & 63), w = threadIdx.x >> 6, half = blockIdx.y;
+// dgamma and dbeta: the partial sums of n workgroups, sixteen interleaved strands of
+// them by sixteen wavefronts, then the strands in their order.
+__global__ __launch_bounds__(1024) void k_ln_join(const float *part, int n, int cols, float *dgamma, float *dbeta) {
+    __shared__ float tmp[16][64];
+    const int lane = threadIdx.x & 63, c = blockIdx.x * 64 + lane, w = threadIdx.x >> 6, half = blockIdx.y;
     float *out = half ? dbeta : dgamma;
     float s = 0.0f;
     if (c < cols)
-        for (int b = w; b < n; b += 4) s += part[((int64_t)b * 2 + half) * cols + c];
-    tmp[w][threadIdx.x & 63] = s;
+#pragma unroll 4
+        for (int b = w; b < n; b += 16) s += part[((int64_t)b * 2 + half) * cols + c];
+    tmp[w][lane] = s;
     __syncthreads();
-    if (w == 0 && c < cols && out)
-        out[c] = (tmp[0][threadIdx.x] + tmp[1][threadIdx.x]) + (tmp[2][threadIdx.x] + tmp[3][threadIdx.x]);
+    if (w > 0 || c >= cols || !out) return;
+    s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s += tmp[i][lane];
+    out[c] = s;
 }
 
-constexpr int kMaxRegCols = 1024 * 4 * kV;  // the longest row held in registers
-constexpr int kParamGroups = 512;           // workgroups whose column sums are joined, at most
+constexpr int kMaxRegCols = 512 * 4 * kV;  // the longest row held in registers
 
-// Calls f<TPR, CH>() for the narrowest shape that holds a row.
+// Calls f<TPR, CH, SHORT>() for the narrowest shape that holds a row.
 template <typename F>
-void by_width(int cols, F &&f) {
-    const int v = (cols + kV - 1) / kV;
-    if (v <= 64) f.template operator()<64, 1>();
-    else if (v <= 128) f.template operator()<64, 2>();
-    else if (v <= 256) f.template operator()<256, 1>();
-    else if (v <= 512) f.template operator()<256, 2>();
-    else if (v <= 1024) f.template operator()<256, 4>();
-    else if (v <= 2048) f.template operator()<512, 4>();
-    else f.template operator()<1024, 4>();
+void by_width(int64_t cols, F &&f) {
+    const int64_t v = (cols + kV - 1) / kV;
+    if (cols < kV) f.template operator()<64, 1, true>();
+    else if (v <= 64) f.template operator()<64, 1, false>();
+    else if (v <= 128) f.template operator()<128, 1, false>();
+    else if (v <= 256) f.template operator()<128, 2, false>();
+    else if (v <= 384) f.template operator()<192, 2, false>();
+    else if (v <= 512) f.template operator()<256, 2, false>();
+    else if (v <= 768) f.template operator()<384, 2, false>();
+    else if (v <= 1024) f.template operator()<512, 2, false>();
+    else f.template operator()<512, 4, false>();
 }
 
 template <typename T>
 struct LaunchFwd {
     const FwdArgs &a;
     hipStream_t stream;
-    template <int TPR, int CH>
+    template <int TPR, int CH, bool SHORT>
     void operator()() {
-        constexpr int NT = TPR < 256 ? 256 : TPR, RPB = NT / TPR;
-        hipLaunchKernelGGL((k_ln_fwd<T, TPR, CH>), dim3((unsigned)((a.rows + RPB - 1) / RPB)), dim3(NT), 0, stream, a);
+        constexpr int RPB = Rows<TPR>::per_group;
+        hipLaunchKernelGGL((k_ln_fwd<T, TPR, CH, SHORT>), dim3((unsigned)((a.rows + RPB - 1) / RPB)), dim3(Rows<TPR>::threads), 0, stream,
+                           a);
     }
 };
 
@@ -370,20 +495,29 @@ struct LaunchBwd {
     const BwdArgs &a;
     int groups;
     hipStream_t stream;
-    template <int TPR, int CH>
+    template <int TPR, int CH, bool SHORT>
     void operator()() {
-        constexpr int NT = TPR < 256 ? 256 : TPR;
-        hipLaunchKernelGGL((k_ln_bwd<T, TPR, CH>), dim3(groups), dim3(NT), 0, stream, a);
+        hipLaunchKernelGGL((k_ln_bwd<T, TPR, CH, SHORT>), dim3(groups), dim3(Rows<TPR>::threads), 0, stream, a);
     }
 };
 
 // Rows that one workgroup of the backward kernel holds at a time.
-int rows_per_group(int64_t cols) { return cols <= 64 * 2 * kV ? 4 : 1; }
+struct RowsAtATime {
+    int rows = 1;
+    template <int TPR, int CH, bool SHORT>
+    void operator()() {
+        rows = Rows<TPR>::per_group;
+    }
+};
 
-// Workgroups of the backward pass (0: no rows).
+// Workgroups of the backward pass (0: no rows): as many as the CUs hold at a time, so
+// that each runs once.  Rows of up to 1024 columns take half the registers: there two
+// fit a CU (65536 x 1024 bfloat16 114 us with 256 workgroups, 89 with 512); longer ones
+// lose by it (32768 x 2048 86 and 92 us).
 int bwd_groups(int64_t rows, int64_t cols) {
-    const int rpb = rows_per_group(cols);
-    return (int)std::min<int64_t>((rows + rpb - 1) / rpb, kParamGroups);
+    RowsAtATime r;
+    if (cols <= kMaxRegCols) by_width(cols, r);
+    return (int)std::min<int64_t>((rows + r.rows - 1) / r.rows, cols <= 1024 ? 512 : 256);
 }
 
 template <typename T>
@@ -449,7 +583,7 @@ extern "C" int structadmm_layer_norm_bwd(const sa_layer_norm_bwd_desc *desc, hip
         if (rc) return rc;
     }
     if (d.dgamma || d.dbeta) {
-        hipLaunchKernelGGL(k_ln_join, dim3(((int)d.cols + 63) / 64, 2), dim3(256), 0, stream,
+        hipLaunchKernelGGL(k_ln_join, dim3(((int)d.cols + 63) / 64, 2), dim3(1024), 0, stream,
                            static_cast<const float *>(d.ws), groups, (int)d.cols, d.dgamma, d.dbeta);
         return check_hip(hipGetLastError(), "k_ln_join");
     }
