@@ -47,8 +47,13 @@ struct Gemm {
     void *y1;
 };
 
-// Workspace of a product (its pointers are not read) and its launch.
+// Workspace of a product: of its pointers only the operands' alignment matters.
 size_t gemm_workspace(const Gemm &g);
-int gemm(const Gemm &g, void *ws, hipStream_t stream);
+
+constexpr int kMaxProducts = 2;
+
+// Launches n <= kMaxProducts products one after the other, each with a workspace of its
+// own; the operands that they need copied are copied by one launch before them.
+int gemm(const Gemm *const *g, void *const *ws, int n, hipStream_t stream);
 
 }  // namespace sa

@@ -698,21 +698,39 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_gemm(TileArgs a) {
     wait_vm<0>();  // the loads past the last stage still write to LDS
 }
 
-// Copies a matrix to rows of whole 16-byte chunks.
-template <typename T>
-__global__ __launch_bounds__(256) void k_align_rows(const T *p, int64_t ld, int64_t rows, int cols, T *out, int64_t ldo) {
-    const int chunks = (cols + 7) / 8;
-    for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; c < rows * chunks; c += (int64_t)gridDim.x * 256) {
-        const int64_t r = c / chunks;
-        const int k = (int)(c - r * chunks) * 8;
-        typename Vec8<T>::type v = {};
-        if (k + 8 <= cols) __builtin_memcpy(&v, p + r * ld + k, 16);
-        else
+// Matrices to copy to rows of whole 16-byte chunks, one after the other in `rows`.
+struct Copies {
+    static constexpr int kMax = kMaxProducts * 4;
+    int n;
+    struct {
+        const uint16_t *p;
+        uint16_t *out;
+        int64_t ld, ldo, end;  // end: the rows of this matrix and those before it
+        int cols;
+    } m[kMax];
+};
+
+// One wavefront a row at a time; the elements' type does not matter to a copy.
+__global__ __launch_bounds__(256) void k_align_rows(Copies a) {
+    typedef uint16_t vec __attribute__((ext_vector_type(8)));
+    const int lane = threadIdx.x & 63;
+    int64_t row = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), first = 0;
+    for (int i = 0; i < a.n; first = a.m[i++].end)
+        for (; row < a.m[i].end; row += (int64_t)gridDim.x * 4) {
+            const uint16_t *p = a.m[i].p + (row - first) * a.m[i].ld;
+            uint16_t *out = a.m[i].out + (row - first) * a.m[i].ldo;
+            const int cols = a.m[i].cols;
+#pragma unroll 2
+            for (int k = lane * 8; k < cols; k += 512) {
+                vec v = {};
+                if (k + 8 <= cols) __builtin_memcpy(&v, p + k, 16);
+                else
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (k + e < cols) v[e] = p[r * ld + k + e];
-        *reinterpret_cast<typename Vec8<T>::type *>(out + r * ldo + k) = v;
-    }
+                    for (int e = 0; e < 8; ++e)
+                        if (k + e < cols) v[e] = p[k + e];
+                *reinterpret_cast<vec *>(out + k) = v;
+            }
+        }
 }
 
 // ---------------------------------------------------------------- host side
@@ -907,17 +925,14 @@ bool any_rows(const Plan &p) { return p.path <= kRows64 || p.path == kRows64x2; 
 
 // Visits the operands that have to be copied to aligned rows.
 template <typename F>
-int each_copied(Gemm &g, F &&f) {
+void each_copied(Gemm &g, F &&f) {
     const int nm = std::max(g.parts, g.batch), nn = g.gated ? 2 : g.parts;
     // the two of a side share one pitch, so both are copied if one is
     bool cm = false, cn = false;
     for (int i = 0; i < nm; ++i) cm |= !rows_aligned(g.m[i], shape_of(g.m[i], g.M, g.K));
     for (int i = 0; i < nn; ++i) cn |= !rows_aligned(g.n[i], shape_of(g.n[i], g.N, g.K));
-    for (int i = 0; i < nm && cm; ++i)
-        if (int rc = f(g.m[i], shape_of(g.m[i], g.M, g.K))) return rc;
-    for (int i = 0; i < nn && cn; ++i)
-        if (int rc = f(g.n[i], shape_of(g.n[i], g.N, g.K))) return rc;
-    return SA_OK;
+    for (int i = 0; i < nm && cm; ++i) f(g.m[i], shape_of(g.m[i], g.M, g.K));
+    for (int i = 0; i < nn && cn; ++i) f(g.n[i], shape_of(g.n[i], g.N, g.K));
 }
 
 int64_t aligned_pitch(const Shape &s) { return round_up(s.cols, 8); }
@@ -930,44 +945,52 @@ size_t gemm_workspace(const Gemm &g0) {
     const Plan p = plan_of(g);
     size_t need = round_up(partial_bytes(g, p.split), 256);
     if (!any_rows(p))
-        each_copied(g, [&](Operand &, const Shape &s) {
-            need += (size_t)round_up(s.rows * aligned_pitch(s) * 2, 256);
-            return SA_OK;
-        });
+        each_copied(g, [&](Operand &, const Shape &s) { need += (size_t)round_up(s.rows * aligned_pitch(s) * 2, 256); });
     return need;
 }
 
-int gemm(const Gemm &g0, void *ws, hipStream_t stream) {
-    Gemm g = g0;
-    if (g.M == 0 || g.N == 0) return SA_OK;
-    const Plan p = plan_of(g);
-    uint8_t *at = static_cast<uint8_t *>(ws);
-    const Partial q{reinterpret_cast<float *>(at), round_up(g.N, 8), p.split};
-    at += round_up(partial_bytes(g, p.split), 256);
-    if (!any_rows(p)) {
-        const int rc = each_copied(g, [&](Operand &o, const Shape &s) {
-            const int64_t ldo = aligned_pitch(s), chunks = s.rows * (ldo / 8);
-            if (chunks > 0) {
-                // the element's type does not matter to a copy
-                hipLaunchKernelGGL(k_align_rows<_Float16>, dim3((unsigned)std::min<int64_t>((chunks + 255) / 256, 8192)), dim3(256),
-                                   0, stream, static_cast<const _Float16 *>(o.p), o.ld, s.rows, (int)s.cols,
-                                   reinterpret_cast<_Float16 *>(at), ldo);
-                if (int e = check_hip(hipGetLastError(), "k_align_rows")) return e;
-            }
-            o.p = at;
-            o.ld = ldo;
-            at += round_up(s.rows * ldo * 2, 256);
-            return SA_OK;
-        });
+int gemm(const Gemm *const *gs, void *const *ws, int n, hipStream_t stream) {
+    Gemm gemms[kMaxProducts];
+    Plan plans[kMaxProducts];
+    Partial partials[kMaxProducts];
+    Copies copies{};
+    int64_t rows = 0;
+    for (int i = 0; i < n; ++i) {
+        Gemm &g = gemms[i] = *gs[i];
+        if (g.M == 0 || g.N == 0) continue;
+        const Plan &p = plans[i] = plan_of(g);
+        uint8_t *at = static_cast<uint8_t *>(ws[i]);
+        partials[i] = Partial{reinterpret_cast<float *>(at), round_up(g.N, 8), p.split};
+        at += round_up(partial_bytes(g, p.split), 256);
+        if (!any_rows(p))
+            each_copied(g, [&](Operand &o, const Shape &s) {
+                const int64_t ldo = aligned_pitch(s);
+                rows += s.rows;
+                copies.m[copies.n++] = {static_cast<const uint16_t *>(o.p), reinterpret_cast<uint16_t *>(at), o.ld, ldo, rows,
+                                        (int)s.cols};
+                o.p = at;
+                o.ld = ldo;
+                at += round_up(s.rows * ldo * 2, 256);
+            });
+        // a single row has no pitch: one of whole chunks keeps the loads' ranges whole
+        const int64_t mr = g.m[0].across ? g.K : g.M, nr = g.n[0].across ? g.K : g.N;
+        for (int j = 0; j < 2; ++j) {
+            if (mr <= 1) g.m[j].ld = round_up(g.m[0].across ? g.M : g.K, 8);
+            if (nr <= 1) g.n[j].ld = round_up(g.n[0].across ? g.N : g.K, 8);
+        }
+    }
+    if (rows > 0) {
+        hipLaunchKernelGGL(k_align_rows, dim3((unsigned)std::min<int64_t>((rows + 3) / 4, 4096)), dim3(256), 0, stream, copies);
+        if (int rc = check_hip(hipGetLastError(), "k_align_rows")) return rc;
+    }
+    for (int i = 0; i < n; ++i) {
+        const Gemm &g = gemms[i];
+        if (g.M == 0 || g.N == 0) continue;
+        const int rc = g.type == SA_BF16 ? run<__bf16>(g, plans[i], partials[i], stream)
+                                         : run<_Float16>(g, plans[i], partials[i], stream);
         if (rc) return rc;
     }
-    // a single row has no pitch: one of whole chunks keeps the loads' ranges whole
-    const int64_t mr = g.m[0].across ? g.K : g.M, nr = g.n[0].across ? g.K : g.N;
-    for (int i = 0; i < 2; ++i) {
-        if (mr <= 1) g.m[i].ld = round_up(g.m[0].across ? g.M : g.K, 8);
-        if (nr <= 1) g.n[i].ld = round_up(g.n[0].across ? g.N : g.K, 8);
-    }
-    return g.type == SA_BF16 ? run<__bf16>(g, p, q, stream) : run<_Float16>(g, p, q, stream);
+    return SA_OK;
 }
 
 }  // namespace sa

@@ -12,6 +12,7 @@
 #include <algorithm>
 #include <cstdint>
 
+#include "nn_columns.h"
 #include "nn_gemm.h"
 #include "nn_types.h"
 #include "sa_host.h"
@@ -29,7 +30,7 @@ struct SlopeArgs {
     int64_t stripe;             // rows of one workgroup
     const void *dY, *Z, *U;
     void *o0, *o1;              // dz, or dg and du; NULL: sums only
-    float *part;                // [2][stripes][N] column sums of dz, or of dg and du; or NULL
+    float *part;                // [stripes][2][N] column sums of dz, or of dg and du; or NULL
 };
 
 // Workgroup (x, y): 256 columns of the rows [y, y + 1) * stripe.
@@ -83,21 +84,13 @@ __global__ __launch_bounds__(256) void k_slope(SlopeArgs a) {
         float v = 0.0f;
 #pragma unroll
         for (int w = 0; w < kRowGroups; ++w) v += join[w][threadIdx.x];
-        if (col < a.N) a.part[((int64_t)h * gridDim.y + blockIdx.y) * a.N + col] = v;
+        if (col < a.N) a.part[((int64_t)blockIdx.y * 2 + h) * a.N + col] = v;
     }
 }
 
-// out[n] = the stripes' sums in their order.
-__global__ __launch_bounds__(64) void k_slope_join(const float *part, int stripes, int N, float *out0, float *out1) {
-    const int c = blockIdx.x * 64 + threadIdx.x, half = blockIdx.y;
-    float *out = half ? out1 : out0;
-    if (c >= N || !out) return;
-    float s = 0.0f;
-    for (int b = 0; b < stripes; ++b) s += part[((int64_t)half * stripes + b) * N + c];
-    out[c] = s;
-}
-
-int64_t stripe_rows(int64_t M) { return std::max<int64_t>(round_up((M + kStripes - 1) / kStripes, kRowGroups), 32); }
+// One row per row group at least: with 32 rows a stripe at least, 256 x 1024 float16
+// took 12 us, with 8 it takes TIME.
+int64_t stripe_rows(int64_t M) { return round_up(std::max<int64_t>((M + kStripes - 1) / kStripes, 1), kRowGroups); }
 int stripes_of(int64_t M) { return (int)((M + stripe_rows(M) - 1) / stripe_rows(M)); }
 
 int slope(const SlopeArgs &s, int type, bool gated, float *b0, float *b1, hipStream_t stream) {
@@ -115,11 +108,7 @@ int slope(const SlopeArgs &s, int type, bool gated, float *b0, float *b1, hipStr
         }
         if (int rc = check_hip(hipGetLastError(), "k_slope")) return rc;
     }
-    if (a.N > 0 && (b0 || b1)) {
-        hipLaunchKernelGGL(k_slope_join, dim3((a.N + 63) / 64, 2), dim3(64), 0, stream, a.part, stripes, a.N, b0, b1);
-        return check_hip(hipGetLastError(), "k_slope_join");
-    }
-    return SA_OK;
+    return a.N > 0 && (b0 || b1) ? join_columns(a.part, stripes, a.N, b0, b1, stream) : SA_OK;
 }
 
 // Takes `bytes` of the workspace, 256-byte aligned.
@@ -174,9 +163,8 @@ BwdPlan plan_bwd(int64_t M, int64_t N, int64_t K, int type, int dw_type, int act
     p.dw.e.Y = dW0;
     p.dw.e.ldy = lddw;
     p.dw.e.out_f32 = dw_type == SA_F32;
-    // the two products run one after the other and share their scratch
-    const size_t a = dX ? gemm_workspace(p.dx) : 0, b = dW0 ? gemm_workspace(p.dw) : 0;
-    p.ws_dx = p.ws_dw = arena.take(std::max(a, b));
+    p.ws_dx = arena.take(dX ? gemm_workspace(p.dx) : 0);
+    p.ws_dw = arena.take(dW0 ? gemm_workspace(p.dw) : 0);
     p.bytes = arena.used;
     return p;
 }
@@ -184,11 +172,12 @@ BwdPlan plan_bwd(int64_t M, int64_t N, int64_t K, int type, int dw_type, int act
 int run_bwd(const BwdPlan &p, int type, float *b0, float *b1, hipStream_t stream) {
     if (p.need_slope)
         if (int rc = slope(p.slope, type, p.gated, b0, b1, stream)) return rc;
-    if (p.dx.e.Y)
-        if (int rc = gemm(p.dx, p.ws_dx, stream)) return rc;
-    if (p.dw.e.Y)
-        if (int rc = gemm(p.dw, p.ws_dw, stream)) return rc;
-    return SA_OK;
+    const Gemm *g[2];
+    void *ws[2];
+    int n = 0;
+    if (p.dx.e.Y) g[n] = &p.dx, ws[n++] = p.ws_dx;
+    if (p.dw.e.Y) g[n] = &p.dw, ws[n++] = p.ws_dw;
+    return gemm(g, ws, n, stream);
 }
 
 BwdPlan plan(const sa_linear_bwd_desc &d, void *ws) {
@@ -228,7 +217,8 @@ extern "C" int structadmm_linear_fwd(const sa_linear_desc *desc, hipStream_t str
     if (int rc = validate_linear(*desc)) return rc;
     const Gemm g = product(*desc);
     if (int rc = check_workspace("linear_fwd", desc->ws, desc->ws_bytes, gemm_workspace(g))) return rc;
-    return gemm(g, desc->ws, stream);
+    const Gemm *one = &g;
+    return gemm(&one, &desc->ws, 1, stream);
 }
 
 extern "C" size_t structadmm_linear_bwd_workspace(const sa_linear_bwd_desc *desc) {
@@ -256,7 +246,8 @@ extern "C" int structadmm_glu_fwd(const sa_glu_desc *desc, hipStream_t stream) {
     if (int rc = validate_glu(*desc)) return rc;
     const Gemm g = product(*desc);
     if (int rc = check_workspace("glu_fwd", desc->ws, desc->ws_bytes, gemm_workspace(g))) return rc;
-    return gemm(g, desc->ws, stream);
+    const Gemm *one = &g;
+    return gemm(&one, &desc->ws, 1, stream);
 }
 
 extern "C" size_t structadmm_glu_bwd_workspace(const sa_glu_bwd_desc *desc) {

@@ -18,6 +18,7 @@
 #include <algorithm>
 #include <cstdint>
 
+#include "nn_columns.h"
 #include "nn_types.h"
 #include "sa_host.h"
 
@@ -442,25 +443,6 @@ __global__ __launch_bounds__(64) void k_ln_params_long(BwdArgs a) {
     p[a.cols + c] = b;
 }
 
-// dgamma and dbeta: the partial sums of n workgroups, sixteen interleaved strands of
-// them by sixteen wavefronts, then the strands in their order.
-__global__ __launch_bounds__(1024) void k_ln_join(const float *part, int n, int cols, float *dgamma, float *dbeta) {
-    __shared__ float tmp[16][64];
-    const int lane = threadIdx.x & 63, c = blockIdx.x * 64 + lane, w = threadIdx.x >> 6, half = blockIdx.y;
-    float *out = half ? dbeta : dgamma;
-    float s = 0.0f;
-    if (c < cols)
-#pragma unroll 4
-        for (int b = w; b < n; b += 16) s += part[((int64_t)b * 2 + half) * cols + c];
-    tmp[w][lane] = s;
-    __syncthreads();
-    if (w > 0 || c >= cols || !out) return;
-    s = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) s += tmp[i][lane];
-    out[c] = s;
-}
-
 constexpr int kMaxRegCols = 512 * 4 * kV;  // the longest row held in registers
 
 // Calls f<TPR, CH, SHORT>() for the narrowest shape that holds a row.
@@ -582,10 +564,7 @@ extern "C" int structadmm_layer_norm_bwd(const sa_layer_norm_bwd_desc *desc, hip
         else rc = bwd<float>(a, groups, stream);
         if (rc) return rc;
     }
-    if (d.dgamma || d.dbeta) {
-        hipLaunchKernelGGL(k_ln_join, dim3(((int)d.cols + 63) / 64, 2), dim3(1024), 0, stream,
-                           static_cast<const float *>(d.ws), groups, (int)d.cols, d.dgamma, d.dbeta);
-        return check_hip(hipGetLastError(), "k_ln_join");
-    }
+    if (d.dgamma || d.dbeta)
+        return join_columns(static_cast<const float *>(d.ws), groups, (int)d.cols, d.dgamma, d.dbeta, stream);
     return SA_OK;
 }
