@@ -51,9 +51,7 @@ __device__ inline void finish(const Epilogue &e, void *Y, int64_t m, int64_t n, 
     };
     if (e.bias) add(e.bias + n, z);
     if (e.Z) put(reinterpret_cast<T *>(e.Z) + m * e.ldz + n, z);
-    if (e.act != SA_ACT_NONE)
-#pragma unroll
-        for (int i = 0; i < V; ++i) z[i] = act_value(e.act, z[i]);
+    if (e.act != SA_ACT_NONE) activate<false, V>(e.act, z, z, z);
     if constexpr (GATED) {
         if (e.bias2) add(e.bias2 + n, u);
         if (e.Z2) put(reinterpret_cast<T *>(e.Z2) + m * e.ldz + n, u);
@@ -88,7 +86,8 @@ __global__ __launch_bounds__(256) void k_join(Gemm g, Partial q) {
     const int64_t chunks = q.pitch / 8;
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= g.M * chunks) return;
-    const int64_t m = i / chunks, n = (i - m * chunks) * 8;
+    // the long division only where the short one does not do
+    const int64_t m = i >> 32 ? i / chunks : (uint32_t)i / (uint32_t)chunks, n = (i - m * chunks) * 8;
     const int z = blockIdx.y;
     float s[8] = {}, u[8] = {}, t[8];
     for (int c = 0; c < q.split; ++c) {

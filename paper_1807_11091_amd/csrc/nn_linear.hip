@@ -56,16 +56,18 @@ __global__ __launch_bounds__(256) void k_slope(SlopeArgs a) {
             load(a.dY, r * a.ldd + c, d);
             if (a.Z) load(a.Z, r * a.ldz + c, z);
             if constexpr (GATED) load(a.U, r * a.ldu + c, u);
+            float v[kV], slope[kV];
+#pragma unroll
+            for (int i = 0; i < kV; ++i) v[i] = slope[i] = 1.0f;
+            if (a.Z) activate<true, kV>(a.act, z, v, slope);
 #pragma unroll
             for (int i = 0; i < kV; ++i) {
-                float v = 1.0f, slope = 1.0f;
-                if (a.Z) act_both(a.act, z[i], v, slope);
                 if constexpr (GATED) {
-                    z[i] = d[i] * v;             // du
-                    d[i] = d[i] * u[i] * slope;  // dg
+                    z[i] = d[i] * v[i];             // du
+                    d[i] = d[i] * u[i] * slope[i];  // dg
                     s[GATED][i] += z[i];
                 } else {
-                    d[i] *= slope;
+                    d[i] *= slope[i];
                 }
                 s[0][i] += d[i];
             }

@@ -57,64 +57,69 @@ __device__ inline float wave_sum_f32(float x) {
     return x;
 }
 
-__device__ inline float sigmoid(float z) { return 1.0f / (1.0f + __expf(-z)); }
+// 1 / (1 + exp(-z)) with the hardware's reciprocal, which is within an ulp; a value
+// below the smallest normal number becomes 0.
+__device__ inline float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
 
 constexpr float kSqrtHalf = 0.70710678118654752f;
 constexpr float kInvSqrt2Pi = 0.39894228040143268f;
 constexpr float kTwoSqrt2OverPi = 1.5957691216057308f;  // 2 sqrt(2 / pi)
 constexpr float kGeluCubic = 0.044715f;
 
-// act(z); the tanh form uses z/2 (1 + tanh q) = z / (1 + exp(-2q)).
-__device__ inline float act_value(int act, float z) {
-    switch (act) {
-    case SA_ACT_RELU: return z <= 0.0f ? 0.0f : z;
-    case SA_ACT_SIGMOID: return sigmoid(z);
-    case SA_ACT_SILU: return z / (1.0f + __expf(-z));
-    case SA_ACT_GELU: return 0.5f * z * (1.0f + erff(z * kSqrtHalf));
-    case SA_ACT_GELU_TANH: return z / (1.0f + __expf(-kTwoSqrt2OverPi * (z + kGeluCubic * z * z * z)));
-    default: return z;
-    }
-}
-
-// act(z) and act'(z)
-__device__ inline void act_both(int act, float z, float &value, float &slope) {
+// act(z) and, if asked for, act'(z).  The tanh form uses z/2 (1 + tanh q) = z sigmoid(2q).
+// The choice of the activation stands outside the loop over the values, so that their
+// chains of exponential and reciprocal run side by side.
+template <bool SLOPE, int V>
+__device__ inline void activate(int act, const float (&z)[V], float (&value)[V], float (&slope)[V]) {
+    auto each = [&](auto f) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) f(z[i], value[i], slope[i]);
+    };
     switch (act) {
     case SA_ACT_RELU:
-        value = z <= 0.0f ? 0.0f : z;
-        slope = z <= 0.0f ? 0.0f : (z > 0.0f ? 1.0f : z);
+        each([](float x, float &v, float &s) {
+            v = x <= 0.0f ? 0.0f : x;
+            if (SLOPE) s = x <= 0.0f ? 0.0f : (x > 0.0f ? 1.0f : x);
+        });
         return;
-    case SA_ACT_SIGMOID: {
-        const float p = sigmoid(z);
-        value = p;
-        slope = p * (1.0f - p);
+    case SA_ACT_SIGMOID:
+        each([](float x, float &v, float &s) {
+            v = sigmoid(x);
+            if (SLOPE) s = v * (1.0f - v);
+        });
         return;
-    }
-    case SA_ACT_SILU: {
-        const float p = sigmoid(z);
-        value = z * p;
-        slope = p * (1.0f + z * (1.0f - p));
+    case SA_ACT_SILU:
+        each([](float x, float &v, float &s) {
+            const float p = sigmoid(x);
+            v = x * p;
+            if (SLOPE) s = p * (1.0f + x * (1.0f - p));
+        });
         return;
-    }
-    case SA_ACT_GELU: {
-        const float p = 0.5f * (1.0f + erff(z * kSqrtHalf));
-        value = z * p;
-        slope = p + z * (kInvSqrt2Pi * __expf(-0.5f * z * z));
+    case SA_ACT_GELU:
+        each([](float x, float &v, float &s) {
+            const float p = 0.5f * (1.0f + erff(x * kSqrtHalf));
+            v = x * p;
+            if (SLOPE) s = p + x * (kInvSqrt2Pi * __expf(-0.5f * x * x));
+        });
         return;
-    }
-    case SA_ACT_GELU_TANH: {
-        if (fabsf(z) > 30.0f) {  // the limits; z * z overflows further out
-            value = z > 0.0f ? z : 0.0f;
-            slope = z > 0.0f ? 1.0f : 0.0f;
-            return;
-        }
-        const float p = sigmoid(kTwoSqrt2OverPi * (z + kGeluCubic * z * z * z));
-        value = z * p;
-        slope = p + z * (p * (1.0f - p)) * (kTwoSqrt2OverPi * (1.0f + 3.0f * kGeluCubic * z * z));
+    case SA_ACT_GELU_TANH:
+        each([](float x, float &v, float &s) {
+            const float p = sigmoid(kTwoSqrt2OverPi * (x + kGeluCubic * x * x * x));
+            v = x * p;
+            if (SLOPE) {
+                s = p + x * (p * (1.0f - p)) * (kTwoSqrt2OverPi * (1.0f + 3.0f * kGeluCubic * x * x));
+                if (fabsf(x) > 30.0f) {  // the limits; x * x overflows further out
+                    v = x > 0.0f ? x : 0.0f;
+                    s = x > 0.0f ? 1.0f : 0.0f;
+                }
+            }
+        });
         return;
-    }
     default:
-        value = z;
-        slope = 1.0f;
+        each([](float x, float &v, float &s) {
+            v = x;
+            if (SLOPE) s = 1.0f;
+        });
     }
 }
 
