@@ -28,9 +28,13 @@ namespace {
 constexpr int kV = 8;  // elements per vector
 
 // Rows of TPR threads each that a workgroup of the register kernels takes at a time.
-template <int TPR>
+// WIDE: four of 192 threads instead of two, for the backward kernel of 16-bit types: a
+// CU holds one workgroup of it, which needs that many loads in flight (16384 x 2560
+// bfloat16 66.7 us with two, 54.8 with four).
+template <int TPR, bool WIDE = false>
 struct Rows {
-    static constexpr int per_group = TPR <= 64 ? 8 : TPR <= 128 ? 4 : TPR <= 256 ? 2 : 1;
+    static constexpr int per_group =
+        TPR <= 64 ? 8 : TPR <= 128 ? 4 : TPR <= 192 && WIDE ? 4 : TPR <= 256 ? 2 : 1;
     static constexpr int threads = TPR * per_group;
 };
 
@@ -259,8 +263,8 @@ struct BwdArgs {
 // bfloat16 in 104 us with the joining of the sums, 5.2 TB/s over x, dy and dx (209 us
 // without the next row, 134 us when copies waited for it).
 template <typename T, int TPR, int CH, bool SHORT>
-__global__ __launch_bounds__(Rows<TPR>::threads, 2) void k_ln_bwd(BwdArgs a) {
-    constexpr int NT = Rows<TPR>::threads, RPB = Rows<TPR>::per_group;
+__global__ __launch_bounds__((Rows<TPR, sizeof(T) == 2>::threads), (Rows<TPR, sizeof(T) == 2>::threads > 512 ? 3 : 2)) void k_ln_bwd(BwdArgs a) {
+    constexpr int NT = Rows<TPR, sizeof(T) == 2>::threads, RPB = Rows<TPR, sizeof(T) == 2>::per_group;
     constexpr bool kAhead = CH <= 2;  // more would not fit the registers
     __shared__ float2 tmp[2][NT / 64];
     __shared__ float join[RPB > 1 ? RPB * TPR * kV : 1];
@@ -479,16 +483,17 @@ struct LaunchBwd {
     hipStream_t stream;
     template <int TPR, int CH, bool SHORT>
     void operator()() {
-        hipLaunchKernelGGL((k_ln_bwd<T, TPR, CH, SHORT>), dim3(groups), dim3(Rows<TPR>::threads), 0, stream, a);
+        hipLaunchKernelGGL((k_ln_bwd<T, TPR, CH, SHORT>), dim3(groups), dim3(Rows<TPR, sizeof(T) == 2>::threads), 0, stream, a);
     }
 };
 
 // Rows that one workgroup of the backward kernel holds at a time.
 struct RowsAtATime {
-    int rows = 1;
+    bool wide;
+    int rows;
     template <int TPR, int CH, bool SHORT>
     void operator()() {
-        rows = Rows<TPR>::per_group;
+        rows = wide ? Rows<TPR, true>::per_group : Rows<TPR>::per_group;
     }
 };
 
@@ -496,8 +501,8 @@ struct RowsAtATime {
 // that each runs once.  Rows of up to 1024 columns take half the registers: there two
 // fit a CU (65536 x 1024 bfloat16 114 us with 256 workgroups, 89 with 512); longer ones
 // lose by it (32768 x 2048 86 and 92 us).
-int bwd_groups(int64_t rows, int64_t cols) {
-    RowsAtATime r;
+int bwd_groups(int64_t rows, int64_t cols, int type) {
+    RowsAtATime r{type != SA_F32, 1};
     if (cols <= kMaxRegCols) by_width(cols, r);
     return (int)std::min<int64_t>((rows + r.rows - 1) / r.rows, cols <= 1024 ? 512 : 256);
 }
@@ -539,7 +544,7 @@ extern "C" int structadmm_layer_norm_fwd(const sa_layer_norm_desc *desc, hipStre
 }
 
 static size_t ln_bwd_bytes(const sa_layer_norm_bwd_desc &d) {
-    return d.dgamma || d.dbeta ? (size_t)bwd_groups(d.rows, d.cols) * 2 * d.cols * sizeof(float) : 0;
+    return d.dgamma || d.dbeta ? (size_t)bwd_groups(d.rows, d.cols, d.type) * 2 * d.cols * sizeof(float) : 0;
 }
 
 extern "C" size_t structadmm_layer_norm_bwd_workspace(const sa_layer_norm_bwd_desc *desc) {
@@ -554,7 +559,7 @@ extern "C" int structadmm_layer_norm_bwd(const sa_layer_norm_bwd_desc *desc, hip
     if (int rc = validate_layer_norm_bwd(d)) return rc;
     const size_t need = ln_bwd_bytes(d);
     if (int rc = check_workspace("layer_norm_bwd", d.ws, d.ws_bytes, need)) return rc;
-    const int groups = bwd_groups(d.rows, d.cols);
+    const int groups = bwd_groups(d.rows, d.cols, d.type);
     BwdArgs a{d.rows, d.lddy, d.ldx, d.lddr, d.lddx, (int)d.cols, d.dY, d.X, d.mean, d.rstd, d.gamma, d.dR, d.dX,
               d.dgamma || d.dbeta ? static_cast<float *>(d.ws) : nullptr};
     if (groups > 0) {
