@@ -247,10 +247,19 @@ def _ptr(t) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
+_raw_stream = None
+
+
 def _stream(stream) -> Optional[int]:
+    """The handle of a stream (None: torch's current one)."""
+    global _raw_stream
     if stream is None:
         import torch
-        return torch.cuda.current_stream().cuda_stream
+        if _raw_stream is None:
+            # the handle alone: torch.cuda.current_stream() takes 2.6 us to wrap it
+            _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+                lambda device: torch.cuda.current_stream(device).cuda_stream)
+        return _raw_stream(torch.cuda.current_device())
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
@@ -586,7 +595,7 @@ def _type_code(t, what: str) -> int:
 
 def _matrix(t, rows: int, cols: int, code: int, dev, what: str) -> int:
     """Checks a [rows, cols] matrix argument with unit column stride; its row pitch."""
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+    if t.shape != (rows, cols):
         raise StructAdmmError(f"{what} must be [{rows}, {cols}], got {tuple(t.shape)}")
     if t.device != dev:
         raise StructAdmmError(f"{what} is on {t.device}, not {dev}")
@@ -604,8 +613,7 @@ def _vector(t, n: int, dev, what: str):
     """Checks an optional float32 vector of n entries; its pointer."""
     if t is None:
         return None
-    if t.numel() != n or t.dim() != 1 or (n > 1 and t.stride(0) != 1) or t.device != dev \
-            or _type_code(t, what) != F32:
+    if t.shape != (n,) or _type_codes.get(t.dtype) != F32 or t.device != dev or (n > 1 and t.stride(0) != 1):
         raise StructAdmmError(f"{what} must be float32 [{n}] on {dev}, contiguous")
     return t.data_ptr()
 
