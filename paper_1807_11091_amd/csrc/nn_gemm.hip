@@ -17,6 +17,7 @@ namespace sa {
 namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 __device__ inline f32x4 mfma(Vec8<__bf16>::type a, Vec8<__bf16>::type b, f32x4 c) {
@@ -33,38 +34,73 @@ __device__ inline f32x16 mfma(Vec8<_Float16>::type a, Vec8<_Float16>::type b, f3
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
 }
 
+// What the outputs' sums are joined with, loaded ahead of them.
+template <typename T, int V>
+struct Addends {
+    typedef T vec __attribute__((ext_vector_type(V)));
+    float bias[V], bias2[V];  // if the epilogue has them
+    vec r;                    // if has_r (whole vectors of the operands' type only)
+    bool has_r;
+
+    __device__ void load_bias(const Epilogue &e, int64_t n, int cnt) {
+        if (e.bias) {
+            if (cnt == V) load_vec<float, V>(e.bias + n, bias);
+            else load_part<float, V>(e.bias + n, cnt, bias);
+        }
+        if (e.bias2) {
+            if (cnt == V) load_vec<float, V>(e.bias2 + n, bias2);
+            else load_part<float, V>(e.bias2 + n, cnt, bias2);
+        }
+    }
+};
+
 // V (cnt < V at a row's end) consecutive outputs from their sums z (and u).
 template <typename T, bool GATED, int V>
-__device__ inline void finish(const Epilogue &e, void *Y, int64_t m, int64_t n, int cnt, float (&z)[V], float (&u)[V]) {
-    auto add = [&](const auto *p, float (&v)[V]) {
-        using E = typename std::remove_cv<typename std::remove_reference<decltype(*p)>::type>::type;
-        float t[V];
-        if (cnt == V) load_vec<E, V>(p, t);
-        else load_part<E, V>(p, cnt, t);
-#pragma unroll
-        for (int i = 0; i < V; ++i) v[i] += t[i];
-    };
+__device__ inline void finish(const Epilogue &e, void *Y, int64_t m, int64_t n, int cnt, float (&z)[V], float (&u)[V],
+                              const Addends<T, V> &with) {
     auto put = [&](auto *p, const float (&v)[V]) {
         using E = typename std::remove_reference<decltype(*p)>::type;
         if (cnt == V) store_vec<E, V>(p, v);
         else store_part<E, V>(p, cnt, v);
     };
-    if (e.bias) add(e.bias + n, z);
+    auto add = [&](const auto *p) {
+        using E = typename std::remove_cv<typename std::remove_reference<decltype(*p)>::type>::type;
+        float t[V];
+        if (cnt == V) load_vec<E, V>(p, t);
+        else load_part<E, V>(p, cnt, t);
+#pragma unroll
+        for (int i = 0; i < V; ++i) z[i] += t[i];
+    };
+    if (e.bias)
+#pragma unroll
+        for (int i = 0; i < V; ++i) z[i] += with.bias[i];
     if (e.Z) put(reinterpret_cast<T *>(e.Z) + m * e.ldz + n, z);
     if (e.act != SA_ACT_NONE) activate<false, V>(e.act, z, z, z);
     if constexpr (GATED) {
-        if (e.bias2) add(e.bias2 + n, u);
+        if (e.bias2)
+#pragma unroll
+            for (int i = 0; i < V; ++i) u[i] += with.bias2[i];
         if (e.Z2) put(reinterpret_cast<T *>(e.Z2) + m * e.ldz + n, u);
 #pragma unroll
         for (int i = 0; i < V; ++i) z[i] *= u[i];
     }
-    if (e.out_f32) {
-        if (e.R) add(reinterpret_cast<const float *>(e.R) + m * e.ldr + n, z);
-        put(reinterpret_cast<float *>(Y) + m * e.ldy + n, z);
-    } else {
-        if (e.R) add(reinterpret_cast<const T *>(e.R) + m * e.ldr + n, z);
-        put(reinterpret_cast<T *>(Y) + m * e.ldy + n, z);
+    if (with.has_r)
+#pragma unroll
+        for (int i = 0; i < V; ++i) z[i] += (float)with.r[i];
+    else if (e.R) {
+        if (e.out_f32) add(reinterpret_cast<const float *>(e.R) + m * e.ldr + n);
+        else add(reinterpret_cast<const T *>(e.R) + m * e.ldr + n);
     }
+    if (e.out_f32) put(reinterpret_cast<float *>(Y) + m * e.ldy + n, z);
+    else put(reinterpret_cast<T *>(Y) + m * e.ldy + n, z);
+}
+
+template <typename T, bool GATED, int V>
+__device__ inline void finish(const Epilogue &e, void *Y, int64_t m, int64_t n, int cnt, float (&z)[V], float (&u)[V]) {
+    Addends<T, V> with;
+    with.has_r = false;
+    with.load_bias(e, n, cnt);
+    finish<T, GATED, V>(e, Y, m, n, cnt, z, u, with);
 }
 
 // Where binary32 partial sums of a product go when k is split over workgroups:
@@ -643,93 +679,129 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_gemm(TileArgs a) {
         constexpr int H = GATED ? 2 : 1, F = MI == 16 ? 2 : 1;  // fragments of a projection taken together
         static_assert(TNG % F == 0, "pairs of fragments");
         const int nl = MI == 16 ? ((lane >> 4) & 1) * 16 + (lane >> 5) * 8 : (lane >> 5) * 8;
+        // A row of fragments shares its bias; where there is an R, it is read before the
+        // first of them is stored, so that there is one wait for memory and not one for
+        // each (8192 x 4096 x 9830 bfloat16 545 and 520 us).  Without one that would cost
+        // instructions for nothing: 6144 x 11264 x 512 108 and 118 us.
+        auto results = [&](auto ahead) {
+            constexpr bool AHEAD = decltype(ahead)::value;
+            constexpr int RV = F * MI * MI / 512;  // vectors of 8 of a fragment
+            Addends<T, 8> with[RV];
+            u32x4 rest[TM][RV];
 #pragma unroll 1
-        for (int f = 0; f < TNG / F * TM; ++f) {
-            Acc t[H][F];
-            pick<TNG / F * TM>(f, [&](auto fc) {
-                constexpr int i = decltype(fc)::value / TM * F, j = decltype(fc)::value % TM;
+            for (int f = 0; f < TNG / F * TM; ++f) {
+                if (AHEAD && f % TM == 0)
+#pragma unroll
+                    for (int r = 0; r < RV; ++r) {
+                        const int64_t n = q.n0 + nrow + f / TM * F * MI + nl + r * 16;
+                        if (n < g.N) with[r].load_bias(g.e, n, (int)min((int64_t)8, g.N - n));
+                        if (n + 8 <= g.N)
+#pragma unroll
+                            for (int j = 0; j < TM; ++j) {
+                                const int64_t m = q.m0 + mrow + j * MI + (lane & (MI - 1));
+                                if (m < g.M)
+                                    __builtin_memcpy(&rest[j][r], reinterpret_cast<const T *>(g.e.R) + m * g.e.ldr + n, 16);
+                            }
+                    }
+                Acc t[H][F];
+                pick<TNG / F * TM>(f, [&](auto fc) {
+                    constexpr int i = decltype(fc)::value / TM * F, j = decltype(fc)::value % TM;
+#pragma unroll
+                    for (int h = 0; h < H; ++h)
+#pragma unroll
+                        for (int k = 0; k < F; ++k) t[h][k] = acc[h * TNG + i + k][j];
+                });
+                const int64_t m = q.m0 + mrow + f % TM * MI + (lane & (MI - 1));
+                const int64_t nb = q.n0 + nrow + f / TM * F * MI + nl;
 #pragma unroll
                 for (int h = 0; h < H; ++h)
 #pragma unroll
-                    for (int k = 0; k < F; ++k) t[h][k] = acc[h * TNG + i + k][j];
-            });
-            const int64_t m = q.m0 + mrow + f % TM * MI + (lane & (MI - 1));
-            const int64_t nb = q.n0 + nrow + f / TM * F * MI + nl;
+                    for (int e = 0; e < 4; ++e) {
+                        if constexpr (MI == 16) {
+                            const auto w = __builtin_amdgcn_permlane16_swap(__float_as_uint(t[h][0][e]), __float_as_uint(t[h][F - 1][e]),
+                                                                            false, false);
+                            t[h][0][e] = __uint_as_float(w[0]);
+                            t[h][F - 1][e] = __uint_as_float(w[1]);
+                        } else {
 #pragma unroll
-            for (int h = 0; h < H; ++h)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if constexpr (MI == 16) {
-                        const auto w = __builtin_amdgcn_permlane16_swap(__float_as_uint(t[h][0][e]), __float_as_uint(t[h][F - 1][e]),
-                                                                        false, false);
-                        t[h][0][e] = __uint_as_float(w[0]);
-                        t[h][F - 1][e] = __uint_as_float(w[1]);
-                    } else {
-#pragma unroll
-                        for (int r = 0; r < 16; r += 8) {
-                            const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(t[h][0][r + e]),
-                                                                            __float_as_uint(t[h][0][r + e + 4]), false, false);
-                            t[h][0][r + e] = __uint_as_float(w[0]);
-                            t[h][0][r + e + 4] = __uint_as_float(w[1]);
+                            for (int r = 0; r < 16; r += 8) {
+                                const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(t[h][0][r + e]),
+                                                                                __float_as_uint(t[h][0][r + e + 4]), false, false);
+                                t[h][0][r + e] = __uint_as_float(w[0]);
+                                t[h][0][r + e + 4] = __uint_as_float(w[1]);
+                            }
                         }
                     }
-                }
-            if (m >= g.M) continue;
+                if (m >= g.M) continue;
 #pragma unroll
-            for (int r = 0; r < F * MI * MI / 64; r += 8) {
-                const int64_t n = nb + r * 2;
-                float z[8], u[8];
+                for (int r = 0; r < F * MI * MI / 64; r += 8) {
+                    const int64_t n = nb + r * 2;
+                    float z[8], u[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    z[e] = MI == 16 ? t[0][e / 4 * (F - 1)][e % 4] : t[0][0][(r + e) % (MI * MI / 64)];
-                    if constexpr (GATED) u[e] = MI == 16 ? t[GATED][e / 4 * (F - 1)][e % 4] : t[GATED][0][(r + e) % (MI * MI / 64)];
-                }
-                if (n >= g.N) continue;
-                if (a.part.split > 1) {
-                    store_vec<float, 8>(partial_at(a.part, g, q.chunk, q.z, 0, m, n), z);
-                    if constexpr (GATED) store_vec<float, 8>(partial_at(a.part, g, q.chunk, q.z, 1, m, n), u);
-                } else {
-                    finish<T, GATED, 8>(g.e, Y, m, n, (int)min((int64_t)8, g.N - n), z, u);
+                    for (int e = 0; e < 8; ++e) {
+                        z[e] = MI == 16 ? t[0][e / 4 * (F - 1)][e % 4] : t[0][0][(r + e) % (MI * MI / 64)];
+                        if constexpr (GATED) u[e] = MI == 16 ? t[GATED][e / 4 * (F - 1)][e % 4] : t[GATED][0][(r + e) % (MI * MI / 64)];
+                    }
+                    if (n >= g.N) continue;
+                    if (a.part.split > 1) {
+                        store_vec<float, 8>(partial_at(a.part, g, q.chunk, q.z, 0, m, n), z);
+                        if constexpr (GATED) store_vec<float, 8>(partial_at(a.part, g, q.chunk, q.z, 1, m, n), u);
+                    } else if constexpr (AHEAD) {
+                        Addends<T, 8> w = with[r / 8];
+                        w.has_r = n + 8 <= g.N;
+                        u32x4 x = {};
+#pragma unroll
+                        for (int j = 0; j < TM; ++j) {
+                            const u32x4 y = rest[j][r / 8];
+                            x = f % TM == j ? y : x;
+                        }
+                        __builtin_memcpy(&w.r, &x, sizeof x);
+                        finish<T, GATED, 8>(g.e, Y, m, n, (int)min((int64_t)8, g.N - n), z, u, w);
+                    } else {
+                        finish<T, GATED, 8>(g.e, Y, m, n, (int)min((int64_t)8, g.N - n), z, u);
+                    }
                 }
             }
+        };
+        if constexpr (!NA && !GATED) {
+            if (g.e.R && !g.e.out_f32 && a.part.split == 1) results(std::true_type{});
+            else results(std::false_type{});
+        } else {
+            results(std::false_type{});
         }
     }
     wait_vm<0>();  // the loads past the last stage still write to LDS
 }
 
-// Matrices to copy to rows of whole 16-byte chunks, one after the other in `rows`.
+// Matrices to copy to rows of whole 16-byte chunks.
 struct Copies {
     static constexpr int kMax = kMaxProducts * 4;
-    int n;
     struct {
         const uint16_t *p;
         uint16_t *out;
-        int64_t ld, ldo, end;  // end: the rows of this matrix and those before it
+        int64_t ld, ldo, chunks;
         int cols;
     } m[kMax];
 };
 
-// One wavefront a row at a time; the elements' type does not matter to a copy.
+// Workgroups (x, y): matrix y, a chunk per thread; the elements' type does not matter.
 __global__ __launch_bounds__(256) void k_align_rows(Copies a) {
     typedef uint16_t vec __attribute__((ext_vector_type(8)));
-    const int lane = threadIdx.x & 63;
-    int64_t row = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), first = 0;
-    for (int i = 0; i < a.n; first = a.m[i++].end)
-        for (; row < a.m[i].end; row += (int64_t)gridDim.x * 4) {
-            const uint16_t *p = a.m[i].p + (row - first) * a.m[i].ld;
-            uint16_t *out = a.m[i].out + (row - first) * a.m[i].ldo;
-            const int cols = a.m[i].cols;
-#pragma unroll 2
-            for (int k = lane * 8; k < cols; k += 512) {
-                vec v = {};
-                if (k + 8 <= cols) __builtin_memcpy(&v, p + k, 16);
-                else
+    const auto &q = a.m[blockIdx.y];
+    const uint32_t across = (uint32_t)(q.ldo / 8);
+    for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; c < q.chunks; c += (int64_t)gridDim.x * 256) {
+        // the long division only where the short one does not do
+        const int64_t row = c >> 32 ? c / across : (uint32_t)c / across;
+        const int k = (int)(c - row * across) * 8;
+        const uint16_t *p = q.p + row * q.ld + k;
+        vec v = {};
+        if (k + 8 <= q.cols) __builtin_memcpy(&v, p, 16);
+        else
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (k + e < cols) v[e] = p[k + e];
-                *reinterpret_cast<vec *>(out + k) = v;
-            }
-        }
+            for (int e = 0; e < 8; ++e)
+                if (k + e < q.cols) v[e] = p[e];
+        *reinterpret_cast<vec *>(q.out + c * 8) = v;
+    }
 }
 
 // ---------------------------------------------------------------- host side
@@ -953,7 +1025,8 @@ int gemm(const Gemm *const *gs, void *const *ws, int n, hipStream_t stream) {
     Plan plans[kMaxProducts];
     Partial partials[kMaxProducts];
     Copies copies{};
-    int64_t rows = 0;
+    int ncopies = 0;
+    int64_t most = 0;
     for (int i = 0; i < n; ++i) {
         Gemm &g = gemms[i] = *gs[i];
         if (g.M == 0 || g.N == 0) continue;
@@ -964,9 +1037,11 @@ int gemm(const Gemm *const *gs, void *const *ws, int n, hipStream_t stream) {
         if (!any_rows(p))
             each_copied(g, [&](Operand &o, const Shape &s) {
                 const int64_t ldo = aligned_pitch(s);
-                rows += s.rows;
-                copies.m[copies.n++] = {static_cast<const uint16_t *>(o.p), reinterpret_cast<uint16_t *>(at), o.ld, ldo, rows,
-                                        (int)s.cols};
+                const int64_t chunks = s.rows * (ldo / 8);
+                if (chunks > 0)
+                    copies.m[ncopies++] = {static_cast<const uint16_t *>(o.p), reinterpret_cast<uint16_t *>(at), o.ld, ldo,
+                                           chunks, (int)s.cols};
+                most = std::max(most, chunks);
                 o.p = at;
                 o.ld = ldo;
                 at += round_up(s.rows * ldo * 2, 256);
@@ -978,8 +1053,9 @@ int gemm(const Gemm *const *gs, void *const *ws, int n, hipStream_t stream) {
             if (nr <= 1) g.n[j].ld = round_up(g.n[0].across ? g.N : g.K, 8);
         }
     }
-    if (rows > 0) {
-        hipLaunchKernelGGL(k_align_rows, dim3((unsigned)std::min<int64_t>((rows + 3) / 4, 4096)), dim3(256), 0, stream, copies);
+    if (ncopies > 0) {
+        hipLaunchKernelGGL(k_align_rows, dim3((unsigned)std::min<int64_t>((most + 255) / 256, 4096), ncopies), dim3(256), 0, stream,
+                           copies);
         if (int rc = check_hip(hipGetLastError(), "k_align_rows")) return rc;
     }
     for (int i = 0; i < n; ++i) {
