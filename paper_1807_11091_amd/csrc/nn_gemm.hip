@@ -836,7 +836,8 @@ int resident(const void *kern, int nt, int lds, int *groups) {
 enum Path { kRows16, kRows32, kRows64, kTile64, kTile128, kTile256, kRows64x2 };
 struct Plan {
     Path path;
-    int split;  // chunks of k
+    int split;   // chunks of k
+    float time;  // of the model, microseconds
 };
 
 // Time models, microseconds, fitted to 364 products (40 to 2048 rows and fewer, 512 to
@@ -897,13 +898,9 @@ float rows_time(const RowsModel &m, const Gemm &g, int split) {
 
 Plan plan_of(const Gemm &g) {
     const int64_t nn = g.N * (g.gated ? 2 : 1), stages = (g.K + 63) / 64 * g.parts;
-    Plan best{kTile64, 1};
-    float least = 3e38f;
+    Plan best{kTile64, 1, 3e38f};
     const auto consider = [&](Path path, int split, float t) {
-        if (t < least) {
-            least = t;
-            best = {path, split};
-        }
+        if (t < best.time) best = {path, split, t};
     };
     if (!g.n[0].across)
         for (const RowsModel &m : kRowsModel) {
@@ -921,6 +918,70 @@ Plan plan_of(const Gemm &g) {
             consider((Path)(kTile64 + i), split, tile_time(m, g, split));
     }
     return best;
+}
+
+// A product in one piece or in two: whole rounds of 256 x 256 tiles, which fill the GPU,
+// and what is left of M or N, which would fill part of a round, by a plan of its own
+// (in one piece and in two: float16 gradients of 6000 x 5000 x 4000 519 and 460 us, gated
+// 2500 x 4096 x 2048 94.7 and 86.2, bfloat16 dW of 8192 x 4096 x 9830 672 and 635).
+struct Pieces {
+    int n;
+    bool cut_m;
+    int64_t at;  // where M, or else N, is cut
+    Plan plan[2];
+};
+
+// The part of a product from m0 and n0 on, M by N.
+Gemm part_of(const Gemm &g, int64_t m0, int64_t n0, int64_t M, int64_t N) {
+    Gemm p = g;
+    p.M = M;
+    p.N = N;
+    const auto move = [](auto *&q, int64_t elements, int size) {
+        if (q) q = reinterpret_cast<std::remove_reference_t<decltype(q)>>(reinterpret_cast<uintptr_t>(q) + elements * size);
+    };
+    for (int i = 0; i < 2; ++i) {
+        move(p.m[i].p, g.m[i].across ? m0 : m0 * g.m[i].ld, 2);
+        move(p.n[i].p, g.n[i].across ? n0 : n0 * g.n[i].ld, 2);
+    }
+    const int out = g.e.out_f32 ? 4 : 2;
+    move(p.e.bias, n0, 4);
+    move(p.e.bias2, n0, 4);
+    move(p.e.R, m0 * g.e.ldr + n0, out);
+    move(p.e.Y, m0 * g.e.ldy + n0, out);
+    move(p.y1, m0 * g.e.ldy + n0, out);
+    move(p.e.Z, m0 * g.e.ldz + n0, 2);
+    move(p.e.Z2, m0 * g.e.ldz + n0, 2);
+    return p;
+}
+
+Pieces pieces_of(const Gemm &g) {
+    Pieces best{1, false, 0, {plan_of(g), {}}};
+    const TileModel &m = kTileModel[kTile256 - kTile64];
+    const int64_t bn = g.gated ? m.bn / 2 : m.bn, mt = (g.M + m.bm - 1) / m.bm, nt = (g.N + bn - 1) / bn;
+    const int64_t rounds = mt * nt * g.batch / m.slots;
+    if (rounds == 0) return best;
+    float least = best.plan[0].time;
+    for (int cut_m = 0; cut_m < 2; ++cut_m) {
+        const int64_t across = (cut_m ? nt : mt) * g.batch, tiles = rounds * m.slots / across;
+        if (tiles < 1 || tiles >= (cut_m ? mt : nt)) continue;
+        const int64_t at = tiles * (cut_m ? m.bm : bn);
+        Gemm first = g, rest = g;
+        (cut_m ? first.M : first.N) = at;
+        (cut_m ? rest.M : rest.N) -= at;
+        const Plan one{kTile256, 1, tile_time(m, first, 1)}, two = plan_of(rest);
+        if (one.time + two.time < least) {
+            least = one.time + two.time;
+            best = {2, cut_m == 1, at, {one, two}};
+        }
+    }
+    return best;
+}
+
+// The pieces' products: the parts of g, whose operands may have been moved.
+int parts_of(const Gemm &g, const Pieces &p, Gemm (&parts)[2]) {
+    parts[0] = p.n == 1 ? g : part_of(g, 0, 0, p.cut_m ? p.at : g.M, p.cut_m ? g.N : p.at);
+    if (p.n == 2) parts[1] = part_of(g, p.cut_m ? p.at : 0, p.cut_m ? 0 : p.at, g.M - (p.cut_m ? p.at : 0), g.N - (p.cut_m ? 0 : p.at));
+    return p.n;
 }
 
 size_t partial_bytes(const Gemm &g, int split) {
@@ -991,8 +1052,11 @@ Shape shape_of(const Operand &o, int64_t r, int64_t K) { return o.across ? Shape
 // Do the rows start on 16-byte boundaries (a single row needs no pitch)?
 bool rows_aligned(const Operand &o, const Shape &s) { return aligned(o.p, 16) && (s.rows <= 1 || o.ld % 8 == 0); }
 
-// Does the product's path read rows of any alignment?
-bool any_rows(const Plan &p) { return p.path <= kRows64 || p.path == kRows64x2; }
+// Do the product's paths read rows of any alignment?
+bool any_rows(const Pieces &p) {
+    const Path path = p.plan[0].path;
+    return p.n == 1 && (path <= kRows64 || path == kRows64x2);
+}
 
 // Visits the operands that have to be copied to aligned rows.
 template <typename F>
@@ -1013,8 +1077,10 @@ int64_t aligned_pitch(const Shape &s) { return round_up(s.cols, 8); }
 size_t gemm_workspace(const Gemm &g0) {
     Gemm g = g0;
     if (g.M == 0 || g.N == 0) return 0;
-    const Plan p = plan_of(g);
-    size_t need = round_up(partial_bytes(g, p.split), 256);
+    const Pieces p = pieces_of(g);
+    Gemm parts[2];
+    size_t need = 0;
+    for (int i = 0, k = parts_of(g, p, parts); i < k; ++i) need += round_up(partial_bytes(parts[i], p.plan[i].split), 256);
     if (!any_rows(p))
         each_copied(g, [&](Operand &, const Shape &s) { need += (size_t)round_up(s.rows * aligned_pitch(s) * 2, 256); });
     return need;
@@ -1022,19 +1088,17 @@ size_t gemm_workspace(const Gemm &g0) {
 
 int gemm(const Gemm *const *gs, void *const *ws, int n, hipStream_t stream) {
     Gemm gemms[kMaxProducts];
-    Plan plans[kMaxProducts];
-    Partial partials[kMaxProducts];
+    Pieces pieces[kMaxProducts];
+    uint8_t *free[kMaxProducts];  // of the workspaces, behind the copies
     Copies copies{};
     int ncopies = 0;
     int64_t most = 0;
     for (int i = 0; i < n; ++i) {
         Gemm &g = gemms[i] = *gs[i];
         if (g.M == 0 || g.N == 0) continue;
-        const Plan &p = plans[i] = plan_of(g);
-        uint8_t *at = static_cast<uint8_t *>(ws[i]);
-        partials[i] = Partial{reinterpret_cast<float *>(at), round_up(g.N, 8), p.split};
-        at += round_up(partial_bytes(g, p.split), 256);
-        if (!any_rows(p))
+        pieces[i] = pieces_of(g);
+        uint8_t *&at = free[i] = static_cast<uint8_t *>(ws[i]);
+        if (!any_rows(pieces[i]))
             each_copied(g, [&](Operand &o, const Shape &s) {
                 const int64_t ldo = aligned_pitch(s);
                 const int64_t chunks = s.rows * (ldo / 8);
@@ -1061,9 +1125,14 @@ int gemm(const Gemm *const *gs, void *const *ws, int n, hipStream_t stream) {
     for (int i = 0; i < n; ++i) {
         const Gemm &g = gemms[i];
         if (g.M == 0 || g.N == 0) continue;
-        const int rc = g.type == SA_BF16 ? run<__bf16>(g, plans[i], partials[i], stream)
-                                         : run<_Float16>(g, plans[i], partials[i], stream);
-        if (rc) return rc;
+        Gemm parts[2];
+        for (int j = 0, k = parts_of(g, pieces[i], parts); j < k; ++j) {
+            const Plan &p = pieces[i].plan[j];
+            const Partial q{reinterpret_cast<float *>(free[i]), round_up(parts[j].N, 8), p.split};
+            free[i] += round_up(partial_bytes(parts[j], p.split), 256);
+            const int rc = g.type == SA_BF16 ? run<__bf16>(parts[j], p, q, stream) : run<_Float16>(parts[j], p, q, stream);
+            if (rc) return rc;
+        }
     }
     return SA_OK;
 }

@@ -312,6 +312,13 @@ def test_large_products(M, N, K, dtype, pitch):
     check(dWu, rwu, (M + 4) * E * (du.t() @ x.abs()) + 1.01 * (ru.t() @ x.abs()) + rounded(rwu, dt), "dWu")
 
 
+# More than one round of the largest tiles and part of another: run in two pieces.
+@pytest.mark.parametrize("M,N,K,dtype,pitch", [(4400, 3900, 2000, "bf16", "padded"), (2500, 4096, 2048, "f16", "packed"),
+                                               (7680, 2430, 1664, "f16", "packed"), (6001, 5001, 4001, "bf16", "packed")])
+def test_products_in_pieces(M, N, K, dtype, pitch):
+    test_large_products(M, N, K, dtype, pitch)
+
+
 # ------------------------------------------------------- empty sizes, specials
 def test_empty_sizes():
     bf = dict(dtype=T.bfloat16, device=DEV)
