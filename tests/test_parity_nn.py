@@ -458,3 +458,32 @@ def test_gradients_against_differences(a):
         + (u * dy * Z.double().abs() * dir_).sum()
     assert (got - want).abs() <= tol, (got.item(), want.item(), tol.item())
     assert tol < 0.25 * (dy * dir_).sum()  # the bound says something
+
+
+def test_offsets_past_32_bits():
+    """Matrices of more than 2^32 bytes and 2^31 elements: the last rows are right, each operator over all rows."""
+    rows, cols, n = 2 ** 20 + 70, 2112, 72
+    g = gen(77)
+    X = T.randn(rows, cols, generator=g, device=DEV, dtype=T.bfloat16)
+    last = slice(rows - 150, rows)
+    gamma = vec(g, cols, 0.2, 1.0)
+    Y, mean, rstd = sa.layer_norm_fwd(X, gamma)
+    alone = sa.layer_norm_fwd(X[last].clone(), gamma)
+    assert T.equal(Y[last], alone[0]) and T.equal(mean[last], alone[1]) and T.equal(rstd[last], alone[2])
+    dX = sa.layer_norm_bwd(Y, X, mean, rstd, gamma, dX=Y, params=False)[0]
+    assert T.equal(dX[last], sa.layer_norm_bwd(alone[0], X[last].clone(), alone[1], alone[2], gamma, params=False)[0])
+    del Y, dX
+    W = T.randn(n, cols, generator=g, device=DEV).bfloat16()
+    out = sa.linear_fwd(X, W)
+    x = X[last].double()
+    y = x @ W.double().t()
+    check(out[last], y, (cols + 4) * E * (x.abs() @ W.double().abs().t()) + rounded(y, T.bfloat16), "Y")
+    dY = T.zeros_like(out)  # only the last rows count
+    dY[last] = T.randn(150, n, generator=g, device=DEV).bfloat16()
+    dX, dW, db = sa.linear_bwd(dY, X, W, grads="xwb")
+    dy = dY[last].double()
+    rx, rw = dy @ W.double(), dy.t() @ x
+    check(dX[last], rx, (n + 4) * E * (dy.abs() @ W.double().abs()) + rounded(rx, T.bfloat16), "dX")
+    # the zeros add exactly
+    check(dW, rw, (150 + 4) * E * (dy.abs().t() @ x.abs()) + rounded(rw, T.float32), "dW")
+    check(db, dy.sum(0), (150 + 4) * E * dy.abs().sum(0), "dbias")
