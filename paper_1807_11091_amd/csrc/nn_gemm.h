@@ -52,8 +52,9 @@ size_t gemm_workspace(const Gemm &g);
 
 constexpr int kMaxProducts = 2;
 
-// Launches n <= kMaxProducts products one after the other, each with a workspace of its
-// own; the operands that they need copied are copied by one launch before them.
+// Launches n <= kMaxProducts products that do not read each other's results, each with a
+// workspace of its own; the operands that they need copied are copied by one launch before
+// them.  The small products of a gradient (dX first) share a launch.
 int gemm(const Gemm *const *g, void *const *ws, int n, hipStream_t stream);
 
 }  // namespace sa

@@ -468,8 +468,9 @@ struct TileArgs {
     int mtiles, ntiles, tiles, groups;  // tiles: of all batches and chunks; groups: workgroups
 };
 
+// Workgroup `block` of a.groups.
 template <typename T, bool NA, bool MA, bool GATED, int BN, int BM, int WN, int WM, int BK, int S, int MI>
-__global__ __launch_bounds__(WN *WM * 64, 2) void k_gemm(TileArgs a) {
+__device__ __forceinline__ void tile_product(const TileArgs &a, int block) {
     using Cfg = TileCfg<BN, BM, WN, WM, BK, S, MI>;
     constexpr int NROWS = GATED ? BN / 2 : BN;  // n of a tile; gated: one half of the N side per projection
     using NSide = Side<T, NA, NROWS, BK, Cfg::NW, MI>;
@@ -488,7 +489,7 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_gemm(TileArgs a) {
 
     // Workgroup b runs on XCD b mod 8, which walks one contiguous range of tiles
     // (its own L2); its workgroups take the range's tiles in turn.
-    const int xcd = blockIdx.x & 7, local = blockIdx.x >> 3;
+    const int xcd = block & 7, local = block >> 3;
     const int per = a.tiles >> 3, extra = a.tiles & 7;
     const int first = uni(xcd * per + min(xcd, extra) + local);
     const int end = uni((xcd + 1) * per + min(xcd + 1, extra));
@@ -782,6 +783,24 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_gemm(TileArgs a) {
     wait_vm<0>();  // the loads past the last stage still write to LDS
 }
 
+template <typename T, bool NA, bool MA, bool GATED, int BN, int BM, int WN, int WM, int BK, int S, int MI>
+__global__ __launch_bounds__(WN *WM * 64, 2) void k_gemm(TileArgs a) {
+    tile_product<T, NA, MA, GATED, BN, BM, WN, WM, BK, S, MI>(a, blockIdx.x);
+}
+
+// The two products of a gradient, dX (a) and dW (b), in one launch.  Alone, small ones
+// leave half of a CU's LDS and most of its matrix cores idle, waiting for a stage's loads;
+// together, each waits while the other works: gradients of 512 x 2048 x 2048 bfloat16 36
+// us in two launches and 28 in one, of 256 x 1024 x 1229 float16 29.7 and 23.4.
+template <typename T, int BM, int S>
+__global__ __launch_bounds__(256, 2) void k_gemm_pair(TileArgs a, TileArgs b, int first_b) {
+    if ((int)blockIdx.x < first_b) {
+        if ((int)blockIdx.x < a.groups) tile_product<T, true, false, false, 128, BM, 2, 2, 64, S, 32>(a, blockIdx.x);
+    } else {
+        tile_product<T, true, true, false, 128, BM, 2, 2, 64, S, 32>(b, (int)blockIdx.x - first_b);
+    }
+}
+
 // Matrices to copy to rows of whole 16-byte chunks.
 struct Copies {
     static constexpr int kMax = kMaxProducts * 4;
@@ -1004,22 +1023,68 @@ int join(const Gemm &g, const Partial &q, hipStream_t stream) {
     return check_hip(hipGetLastError(), "k_join");
 }
 
+// The tiles of a product; groups: at most that many workgroups.
+int tile_args(TileArgs &a, const Gemm &g, const Partial &q, int bn, int bm, int groups) {
+    const int64_t mt = (g.M + bm - 1) / bm, rows = g.gated ? bn / 2 : bn, nt = (g.N + rows - 1) / rows;
+    if (mt * nt >= (int64_t(1) << 28)) return fail(SA_E_UNSUPPORTED, "matrix product of more than 2^28 tiles");
+    a = TileArgs{g, q, (int)mt, (int)nt, (int)(mt * nt) * g.batch * q.split, 0};
+    a.groups = std::min(a.tiles, groups);
+    return SA_OK;
+}
+
 template <typename T, bool NA, bool MA, bool GATED, int BN, int BM, int WN, int WM, int BK, int S, int MI>
 int launch(const Gemm &g, const Partial &q, hipStream_t stream) {
     using Cfg = TileCfg<BN, BM, WN, WM, BK, S, MI>;
-    TileArgs a{g, q, 0, 0, 0, 0};
-    const int64_t mt = (g.M + BM - 1) / BM, nt = (g.N + (GATED ? BN / 2 : BN) - 1) / (GATED ? BN / 2 : BN);
-    if (mt * nt >= (int64_t(1) << 28)) return fail(SA_E_UNSUPPORTED, "matrix product of more than 2^28 tiles");
-    a.mtiles = (int)mt;
-    a.ntiles = (int)nt;
-    a.tiles = (int)(mt * nt) * g.batch * q.split;
     auto kern = k_gemm<T, NA, MA, GATED, BN, BM, WN, WM, BK, S, MI>;
     int groups = 0;
     if (int rc = resident(reinterpret_cast<const void *>(kern), Cfg::NT, Cfg::lds, &groups)) return rc;
-    a.groups = std::min(a.tiles, groups);
+    TileArgs a;
+    if (int rc = tile_args(a, g, q, BN, BM, groups)) return rc;
     hipLaunchKernelGGL(kern, dim3(a.groups), dim3(Cfg::NT), Cfg::lds, stream, a);
     if (int rc = check_hip(hipGetLastError(), "k_gemm")) return rc;
     return q.split > 1 ? join<T, GATED>(g, q, stream) : SA_OK;
+}
+
+template <typename T, int BM, int S>
+int launch_pair(const Gemm *g, const Partial *q, hipStream_t stream) {
+    constexpr int lds = TileCfg<128, BM, 2, 2, 64, S, 32>::lds;
+    auto kern = k_gemm_pair<T, BM, S>;
+    int groups = 0;
+    if (int rc = resident(reinterpret_cast<const void *>(kern), 256, lds, &groups)) return rc;
+    TileArgs a, b;
+    if (int rc = tile_args(a, g[0], q[0], 128, BM, groups)) return rc;
+    if (int rc = tile_args(b, g[1], q[1], 128, BM, groups)) return rc;
+    const int first_b = (int)round_up(a.groups, 8);  // workgroup b of the second runs on XCD b mod 8 too
+    hipLaunchKernelGGL(kern, dim3(first_b + b.groups), dim3(256), lds, stream, a, b, first_b);
+    if (int rc = check_hip(hipGetLastError(), "k_gemm_pair")) return rc;
+    for (int i = 0; i < 2; ++i)
+        if (q[i].split > 1)
+            if (int rc = join<T, false>(g[i], q[i], stream)) return rc;
+    return SA_OK;
+}
+
+// Do the products of a gradient run in one launch?  Those of up to three rounds of small
+// tiles do (gated 300 x 5504 x 2048, 1376 tiles, 70 us in two launches and 61 in one);
+// 5409 x 8064 from 77, whose 2709 tiles fill the GPU without help, takes 108 us
+// by itself with the other after it and 115 with the other beside it.
+bool is_pair(const Gemm *g, const Pieces *p) {
+    if (!g[0].n[0].across || g[0].m[0].across || !g[1].m[0].across) return false;
+    for (int i = 0; i < 2; ++i) {
+        const Plan &plan = p[i].plan[0];
+        if (g[i].M == 0 || g[i].N == 0 || p[i].n != 1 || (plan.path != kTile64 && plan.path != kTile128)) return false;
+        const TileModel &m = kTileModel[plan.path - kTile64];
+        if (((g[i].M + m.bm - 1) / m.bm) * ((g[i].N + m.bn - 1) / m.bn) * g[i].batch * plan.split > 3 * m.slots) return false;
+    }
+    return true;
+}
+
+// Tiles of one shape for both, the smaller where the plans differ: with one of each shape
+// gradients of 1000 x 2458 x 1024 (gated) take 60 us, as in two launches, with the smaller
+// 55.
+template <typename T>
+int run_pair(const Gemm *g, const Pieces *p, const Partial *q, hipStream_t stream) {
+    if (p[0].plan[0].path == kTile128 && p[1].plan[0].path == kTile128) return launch_pair<T, 128, 2>(g, q, stream);
+    return launch_pair<T, 64, 3>(g, q, stream);
 }
 
 template <typename T, bool GATED, int NF, int MF, int U>
@@ -1130,6 +1195,11 @@ int gemm(const Gemm *const *gs, void *const *ws, int n, hipStream_t stream) {
         hipLaunchKernelGGL(k_align_rows, dim3((unsigned)std::min<int64_t>((most + 255) / 256, 4096), ncopies), dim3(256), 0, stream,
                            copies);
         if (int rc = check_hip(hipGetLastError(), "k_align_rows")) return rc;
+    }
+    if (n == 2 && is_pair(gemms, pieces)) {
+        Partial q[2];
+        for (int i = 0; i < 2; ++i) q[i] = Partial{reinterpret_cast<float *>(free[i]), round_up(gemms[i].N, 8), pieces[i].plan[0].split};
+        return gemms[0].type == SA_BF16 ? run_pair<__bf16>(gemms, pieces, q, stream) : run_pair<_Float16>(gemms, pieces, q, stream);
     }
     for (int i = 0; i < n; ++i) {
         const Gemm &g = gemms[i];
