@@ -3,6 +3,7 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <exception>
 #include <map>
 #include <mutex>
 #include <type_traits>
@@ -835,7 +836,7 @@ __global__ __launch_bounds__(256) void k_align_rows(Copies a) {
 // ---------------------------------------------------------------- host side
 // Workgroups of `kern` (nt threads, lds bytes) that the GPU holds at once; raises
 // the kernel's LDS limit on the first call per device.
-int resident(const void *kern, int nt, int lds, int *groups) {
+int resident(const void *kern, int nt, int lds, int *groups) try {
     static std::mutex mu;
     static std::map<std::pair<const void *, int>, int> known;
     int dev = 0;
@@ -856,6 +857,8 @@ int resident(const void *kern, int nt, int lds, int *groups) {
     *groups = std::max(1, per_cu) * std::max(1, cus);
     known[{kern, dev}] = *groups;
     return SA_OK;
+} catch (const std::exception &) {  // no exception leaves a C entry
+    return fail(SA_E_HIP, "matrix product: out of host memory");
 }
 
 // How a product runs: k_rows with 16, 32 or 64 rows of M per workgroup (kRows64x2: 32
