@@ -17,6 +17,7 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <type_traits>
 
 #include "nn_columns.h"
 #include "nn_types.h"
@@ -464,15 +465,59 @@ void by_width(int64_t cols, F &&f) {
     else f.template operator()<512, 4, false>();
 }
 
+// HIP counts a launch's threads along x in 32 bits: calls f(at, n) for rows [at, at + n)
+// of at most kLaunchThreads / (threads a row) rows, a launch each.  2^28 threads keep the
+// GPU busy for 100 us and more, so that the launches follow each other without a gap.
+constexpr int64_t kLaunchThreads = int64_t(1) << 28;
+template <typename F>
+int by_rows(const char *who, int64_t rows, int threads, F &&f) {
+    const int64_t most = kLaunchThreads / threads;
+    for (int64_t at = 0; at < rows; at += most) {
+        f(at, std::min(most, rows - at));
+        if (int rc = check_hip(hipGetLastError(), who)) return rc;
+    }
+    return SA_OK;
+}
+
+// The n rows of a call from row `at` on.
+template <typename T, typename P>
+void skip_rows(P *&p, int64_t at, int64_t ld) {
+    using E = std::conditional_t<std::is_const_v<P>, const T, T>;
+    if (p) p = static_cast<E *>(p) + at * ld;
+}
+template <typename T>
+FwdArgs rows_from(FwdArgs a, int64_t at, int64_t n) {
+    a.rows = n;
+    skip_rows<T>(a.X, at, a.ldx);
+    skip_rows<T>(a.Y, at, a.ldy);
+    skip_rows<float>(a.mean, at, 1);
+    skip_rows<float>(a.rstd, at, 1);
+    return a;
+}
+template <typename T>
+BwdArgs rows_from(BwdArgs a, int64_t at, int64_t n) {
+    a.rows = n;
+    skip_rows<T>(a.dY, at, a.lddy);
+    skip_rows<T>(a.X, at, a.ldx);
+    skip_rows<T>(a.dR, at, a.lddr);
+    skip_rows<T>(a.dX, at, a.lddx);
+    skip_rows<float>(a.mean, at, 1);
+    skip_rows<float>(a.rstd, at, 1);
+    return a;
+}
+
 template <typename T>
 struct LaunchFwd {
     const FwdArgs &a;
     hipStream_t stream;
+    int rc;
     template <int TPR, int CH, bool SHORT>
     void operator()() {
-        constexpr int RPB = Rows<TPR>::per_group;
-        hipLaunchKernelGGL((k_ln_fwd<T, TPR, CH, SHORT>), dim3((unsigned)((a.rows + RPB - 1) / RPB)), dim3(Rows<TPR>::threads), 0, stream,
-                           a);
+        rc = by_rows("k_ln_fwd", a.rows, TPR, [&](int64_t at, int64_t n) {
+            constexpr int RPB = Rows<TPR>::per_group;
+            hipLaunchKernelGGL((k_ln_fwd<T, TPR, CH, SHORT>), dim3((unsigned)((n + RPB - 1) / RPB)), dim3(Rows<TPR>::threads), 0,
+                               stream, rows_from<T>(a, at, n));
+        });
     }
 };
 
@@ -509,9 +554,14 @@ int bwd_groups(int64_t rows, int64_t cols, int type) {
 
 template <typename T>
 int fwd(const FwdArgs &a, hipStream_t stream) {
-    if (a.cols <= kMaxRegCols) by_width(a.cols, LaunchFwd<T>{a, stream});
-    else hipLaunchKernelGGL(k_ln_fwd_long<T>, dim3((unsigned)a.rows), dim3(1024), 0, stream, a);
-    return check_hip(hipGetLastError(), "k_ln_fwd");
+    if (a.cols <= kMaxRegCols) {
+        LaunchFwd<T> launch{a, stream, SA_OK};
+        by_width(a.cols, launch);
+        return launch.rc;
+    }
+    return by_rows("k_ln_fwd_long", a.rows, 1024, [&](int64_t at, int64_t n) {
+        hipLaunchKernelGGL(k_ln_fwd_long<T>, dim3((unsigned)n), dim3(1024), 0, stream, rows_from<T>(a, at, n));
+    });
 }
 
 template <typename T>
@@ -520,10 +570,14 @@ int bwd(const BwdArgs &a, int groups, hipStream_t stream) {
         by_width(a.cols, LaunchBwd<T>{a, groups, stream});
         return check_hip(hipGetLastError(), "k_ln_bwd");
     }
-    if (a.part)  // first: dX may overwrite dY
+    if (a.part) {  // first: dX may overwrite dY
         hipLaunchKernelGGL(k_ln_params_long<T>, dim3((a.cols + 63) / 64, groups), dim3(64), 0, stream, a);
-    if (a.dX) hipLaunchKernelGGL(k_ln_bwd_long<T>, dim3((unsigned)a.rows), dim3(1024), 0, stream, a);
-    return check_hip(hipGetLastError(), "k_ln_bwd_long");
+        if (int rc = check_hip(hipGetLastError(), "k_ln_params_long")) return rc;
+    }
+    if (!a.dX) return SA_OK;
+    return by_rows("k_ln_bwd_long", a.rows, 1024, [&](int64_t at, int64_t n) {
+        hipLaunchKernelGGL(k_ln_bwd_long<T>, dim3((unsigned)n), dim3(1024), 0, stream, rows_from<T>(a, at, n));
+    });
 }
 
 }  // namespace
