@@ -263,17 +263,21 @@ def _stream(stream) -> Optional[int]:
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
-def _keep_for_stream(stream, *tensors):
-    """Temporaries this module allocates come from torch's caching allocator on
-    the current stream; when the launch goes to another torch stream, mark them
-    in use there, so their memory is not handed out again before that stream's
-    work has finished (a raw stream handle gets no such tracking: the caller
-    must keep such calls on the current stream or pass its own buffers)."""
-    if stream is None or isinstance(stream, int):
-        return
-    for t in tensors:
-        if t is not None:
-            t.record_stream(stream)
+def _empty(stream, shape, dtype, device):
+    """Uninitialised memory for a call on ``stream`` (a torch stream, a raw handle
+    or None for the current one).  It comes from that stream's own pool: a block
+    of the current stream's pool may still be in use by work that waits there and
+    that ``stream`` does not wait for.  The current stream is marked as a user,
+    so that a result which it reads may be dropped right after."""
+    import torch
+    if stream is None or isinstance(stream, int) and stream == _stream(None):
+        return torch.empty(shape, dtype=dtype, device=device)
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream(device))
+    return t
 
 
 @dataclass
@@ -367,20 +371,19 @@ def compact(Z, groups: int = 1, row_mask=None, col_mask=None, chan_mask=None, in
     dev = Z.device
     K = B * C * D
     if out is None:
-        Wc = torch.empty(A * ((K + 63) // 64 * 64), dtype=torch.uint16, device=dev)
-        row_idx = torch.empty(A, dtype=torch.int32, device=dev)
-        col_ch = torch.empty(groups * K, dtype=torch.int32, device=dev)
-        col_tap = torch.empty(groups * K, dtype=torch.int32, device=dev)
+        Wc = _empty(stream, A * ((K + 63) // 64 * 64), torch.uint16, dev)
+        row_idx = _empty(stream, A, torch.int32, dev)
+        col_ch = _empty(stream, groups * K, torch.int32, dev)
+        col_tap = _empty(stream, groups * K, torch.int32, dev)
     else:
         Wc, row_idx, col_ch, col_tap = out
     if ws is None:
-        ws = torch.empty(COMPACT_WS_BYTES, dtype=torch.uint8, device=dev)
+        ws = _empty(stream, COMPACT_WS_BYTES, torch.uint8, dev)
     desc = CompactDesc(A, B, C, D, groups, _ptr(Z), _ptr(row_mask), _ptr(col_mask), _ptr(chan_mask),
                        _ptr(in_ch_mask), 1 if in_compacted else 0, _ptr(Wc), _ptr(row_idx), _ptr(col_ch),
                        _ptr(col_tap), _ptr(ws))
     sizes = CompactSizes()
     _check(lib().structadmm_compact(ctypes.byref(desc), ctypes.byref(sizes), _stream(stream)), "structadmm_compact")
-    _keep_for_stream(stream, ws, *(() if out is not None else (Wc, row_idx, col_ch, col_tap)))
     return Wc, row_idx, col_ch, col_tap, sizes
 
 
@@ -396,23 +399,22 @@ def compact_many(items, ws=None, stream=None):
         return []
     dev = items[0]["Z"].device
     if ws is None:
-        ws = torch.empty(n * COMPACT_WS_BYTES, dtype=torch.uint8, device=dev)
+        ws = _empty(stream, n * COMPACT_WS_BYTES, torch.uint8, dev)
     elif ws.numel() * ws.element_size() < n * COMPACT_WS_BYTES:
         raise StructAdmmError(f"compact_many: ws must hold {n} x {COMPACT_WS_BYTES} bytes")
     descs = (CompactDesc * n)()
     sizes = (CompactSizes * n)()
-    outs, made = [], []
+    outs = []
     for i, it in enumerate(items):
         Z = it["Z"]
         A, B, C, D = Z.shape
         groups = it.get("groups", 1)
         K = B * C * D
         if it.get("out") is None:
-            o = (torch.empty(A * ((K + 63) // 64 * 64), dtype=torch.uint16, device=dev),
-                 torch.empty(A, dtype=torch.int32, device=dev),
-                 torch.empty(groups * K, dtype=torch.int32, device=dev),
-                 torch.empty(groups * K, dtype=torch.int32, device=dev))
-            made.extend(o)
+            o = (_empty(stream, A * ((K + 63) // 64 * 64), torch.uint16, dev),
+                 _empty(stream, A, torch.int32, dev),
+                 _empty(stream, groups * K, torch.int32, dev),
+                 _empty(stream, groups * K, torch.int32, dev))
         else:
             o = tuple(it["out"])
         outs.append(o)
@@ -421,7 +423,6 @@ def compact_many(items, ws=None, stream=None):
                                1 if it.get("in_compacted") else 0, _ptr(o[0]), _ptr(o[1]), _ptr(o[2]), _ptr(o[3]),
                                ws.data_ptr() + i * COMPACT_WS_BYTES)
     _check(lib().structadmm_compact_many(descs, n, sizes, _stream(stream)), "structadmm_compact_many")
-    _keep_for_stream(stream, ws, *made)
     return [outs[i] + (CompactSizes.from_buffer_copy(sizes[i]),) for i in range(n)]
 
 
@@ -431,11 +432,9 @@ def pack_nhwc(X, keep=None, Cx: Optional[int] = None, out=None, stream=None):
     N, Cin, H, W = X.shape
     if Cx is None:
         Cx = Cin if keep is None else int(keep.count_nonzero().item())
-    Xp = out if out is not None else torch.empty((N, H, W, Cx), dtype=torch.uint16, device=X.device)
+    Xp = out if out is not None else _empty(stream, (N, H, W, Cx), torch.uint16, X.device)
     _check(lib().structadmm_pack_nhwc(_ptr(X), N, Cin, H, W, _ptr(keep), Cx, _ptr(Xp), _stream(stream)),
            "structadmm_pack_nhwc")
-    if out is None:
-        _keep_for_stream(stream, Xp)
     return Xp
 
 
@@ -492,7 +491,6 @@ def conv_fwd(Xp, Wc, col_ch, col_tap, sizes: CompactSizes, C: int, D: int, strid
     the last dimension of a given 4-d Y, else Cy.  Y is then [N, P, Q, ldy] whose
     channels [Cy, ldy) are padding (left unchanged or set to +0)."""
     import torch
-    temps = []
     if desc is None:
         N, H, W, Cx = Xp.shape
         shape = conv_out_shape(N, H, W, C, D, stride, pad, sizes)
@@ -502,17 +500,14 @@ def conv_fwd(Xp, Wc, col_ch, col_tap, sizes: CompactSizes, C: int, D: int, strid
         if ldy < Cy:
             raise StructAdmmError(f"conv_fwd: ldy={ldy} is below the {Cy} output channels")
         if Y is None:
-            Y = torch.empty(shape[:3] + (ldy,), dtype=torch.uint16, device=Xp.device)
-            temps.append(Y)
+            Y = _empty(stream, shape[:3] + (ldy,), torch.uint16, Xp.device)
         elif Y.numel() < shape[0] * shape[1] * shape[2] * ldy or Y.dtype != torch.uint16:
             raise StructAdmmError(f"conv_fwd: Y must be uint16 with room for {shape[:3]} rows of {ldy}")
         if ws is None:
             need = conv_workspace(Xp, sizes, C, D, stride, pad)
-            ws = torch.empty(need, dtype=torch.uint8, device=Xp.device) if need else None
-            temps.append(ws)
+            ws = _empty(stream, need, torch.uint8, Xp.device) if need else None
         desc = conv_desc(Xp, Wc, col_ch, col_tap, sizes, C, D, stride, pad, Y, ws, 0 if ldy == Cy else ldy)
     _check(lib().structadmm_conv_fwd(ctypes.byref(desc), _stream(stream)), "structadmm_conv_fwd")
-    _keep_for_stream(stream, *temps)
     return Y
 
 
@@ -525,15 +520,17 @@ def csr(Z, kept_idx, nnz: Optional[int] = None, row_ptr=None, col=None, val=None
     nnz = int(kept_idx.numel()) if nnz is None else int(nnz)
     dev = Z.device
     if row_ptr is None:
-        row_ptr = torch.empty(A + 1, dtype=torch.int32, device=dev)
+        row_ptr = _empty(stream, A + 1, torch.int32, dev)
     if col is None:
-        col = torch.empty(max(nnz, 1), dtype=torch.int32, device=dev)
+        col = _empty(stream, max(nnz, 1), torch.int32, dev)
     if val is None:
-        val = torch.empty(max(nnz, 1), dtype=torch.uint16, device=dev)
+        val = _empty(stream, max(nnz, 1), torch.uint16, dev)
     d = CsrDesc(A, B, C, D, nnz, _ptr(Z), _ptr(kept_idx) if nnz else None, _ptr(row_ptr),
                 _ptr(col) if nnz else None, _ptr(val) if nnz else None)
     _check(lib().structadmm_csr(ctypes.byref(d), _stream(stream)), "structadmm_csr")
-    _keep_for_stream(stream, row_ptr, col, val)
+    for t in (row_ptr, col, val):  # given ones too stay until the stream has written them
+        if stream is not None and not isinstance(stream, int):
+            t.record_stream(stream)
     return row_ptr, col, val
 
 
@@ -559,22 +556,18 @@ def conv_sparse_fwd(Xp, row_ptr, col, val, shape, groups: int, stride: int, pad:
     [N, P, Q, A] (uint16).  reuse_ws: ws holds the padded entries an earlier
     call with the same CSR and geometry built."""
     import torch
-    temps = []
     if desc is None:
         N, H, W, Cx = Xp.shape
         A, B, C, D = shape
         if Y is None:
             P = (H + 2 * pad - C) // stride + 1
             Q = (W + 2 * pad - D) // stride + 1
-            Y = torch.empty((N, P, Q, A), dtype=torch.uint16, device=Xp.device)
-            temps.append(Y)
+            Y = _empty(stream, (N, P, Q, A), torch.uint16, Xp.device)
         if ws is None:
             need = conv_sparse_workspace(Xp, shape, groups, stride, pad, nnz)
-            ws = torch.empty(max(need, 256), dtype=torch.uint8, device=Xp.device)
-            temps.append(ws)
+            ws = _empty(stream, max(need, 256), torch.uint8, Xp.device)
         desc = sparse_conv_desc(Xp, row_ptr, col, val, shape, groups, stride, pad, nnz, Y, ws, reuse_ws)
     _check(lib().structadmm_conv_sparse_fwd(ctypes.byref(desc), _stream(stream)), "structadmm_conv_sparse_fwd")
-    _keep_for_stream(stream, *temps)
     return Y
 
 
@@ -629,25 +622,23 @@ def _optional(t, rows, cols, code, dev, what):
     return (None, cols) if t is None else (t.data_ptr(), _matrix(t, rows, cols, code, dev, what))
 
 
-def _new(like, rows: int, cols: int, dtype=None):
+def _new(stream, like, rows: int, cols: int, dtype=None):
     import torch
     dtype = dtype or like.dtype
-    return torch.empty((rows, cols), dtype=torch.bfloat16 if dtype == torch.uint16 else dtype, device=like.device)
+    return _empty(stream, (rows, cols), torch.bfloat16 if dtype == torch.uint16 else dtype, like.device)
 
 
-def _run(desc, name: str, ws_fn, ws, like, stream, made):
+def _run(desc, name: str, ws_fn, ws, like, stream):
     """Gives the descriptor its workspace and makes the call."""
     if ws_fn is not None:
         if ws is None:
             need = ws_fn(ctypes.byref(desc))
             if need:
                 import torch
-                ws = torch.empty(need, dtype=torch.uint8, device=like.device)
-                made.append(ws)
+                ws = _empty(stream, need, torch.uint8, like.device)
         if ws is not None:
             desc.ws, desc.ws_bytes = ws.data_ptr(), ws.numel() * ws.element_size()
     _check(getattr(lib(), name)(ctypes.byref(desc), _stream(stream)), name)
-    _keep_for_stream(stream, *made)
 
 
 def compacted_matrix(Wc, sizes: CompactSizes, group: int = 0):
@@ -667,23 +658,20 @@ def layer_norm_fwd(X, gamma=None, beta=None, eps: float = 1e-5, Y=None, mean=Non
     reads, are None with stats=False."""
     import torch
     rows, cols = _rows_of(X, "layer_norm_fwd: X")
-    dev, code, made = X.device, _type_code(X, "layer_norm_fwd: X"), []
+    dev, code = X.device, _type_code(X, "layer_norm_fwd: X")
     ldx = _matrix(X, rows, cols, code, dev, "layer_norm_fwd: X")
     if Y is None:
-        Y = _new(X, rows, cols)
-        made.append(Y)
+        Y = _new(stream, X, rows, cols)
     if stats and mean is None:
-        mean = torch.empty(rows, dtype=torch.float32, device=dev)
-        made.append(mean)
+        mean = _empty(stream, rows, torch.float32, dev)
     if stats and rstd is None:
-        rstd = torch.empty(rows, dtype=torch.float32, device=dev)
-        made.append(rstd)
+        rstd = _empty(stream, rows, torch.float32, dev)
     d = LayerNormDesc(rows, cols, code, eps, X.data_ptr(), ldx, _vector(gamma, cols, dev, "layer_norm_fwd: gamma"),
                       _vector(beta, cols, dev, "layer_norm_fwd: beta"), Y.data_ptr(),
                       _matrix(Y, rows, cols, code, dev, "layer_norm_fwd: Y"),
                       _vector(mean, rows, dev, "layer_norm_fwd: mean"),
                       _vector(rstd, rows, dev, "layer_norm_fwd: rstd"))
-    _run(d, "structadmm_layer_norm_fwd", None, None, X, stream, made)
+    _run(d, "structadmm_layer_norm_fwd", None, None, X, stream)
     return Y, mean, rstd
 
 
@@ -694,25 +682,22 @@ def layer_norm_bwd(dY, X, mean, rstd, gamma=None, dR=None, dX=None, dgamma=None,
     params=False (unless given)."""
     import torch
     rows, cols = _rows_of(X, "layer_norm_bwd: X")
-    dev, code, made, w = X.device, _type_code(X, "layer_norm_bwd: X"), [], "layer_norm_bwd: "
+    dev, code, w = X.device, _type_code(X, "layer_norm_bwd: X"), "layer_norm_bwd: "
     if mean is None or rstd is None:
         raise StructAdmmError(w + "mean and rstd of the forward pass are required")
     if dX is None:
-        dX = _new(X, rows, cols)
-        made.append(dX)
+        dX = _new(stream, X, rows, cols)
     if params and dgamma is None:
-        dgamma = torch.empty(cols, dtype=torch.float32, device=dev)
-        made.append(dgamma)
+        dgamma = _empty(stream, cols, torch.float32, dev)
     if params and dbeta is None:
-        dbeta = torch.empty(cols, dtype=torch.float32, device=dev)
-        made.append(dbeta)
+        dbeta = _empty(stream, cols, torch.float32, dev)
     r, ldr = _optional(dR, rows, cols, code, dev, w + "dR")
     d = LayerNormBwdDesc(rows, cols, code, dY.data_ptr(), _matrix(dY, rows, cols, code, dev, w + "dY"), X.data_ptr(),
                          _matrix(X, rows, cols, code, dev, w + "X"), _vector(mean, rows, dev, w + "mean"),
                          _vector(rstd, rows, dev, w + "rstd"), _vector(gamma, cols, dev, w + "gamma"), r, ldr,
                          dX.data_ptr(), _matrix(dX, rows, cols, code, dev, w + "dX"),
                          _vector(dgamma, cols, dev, w + "dgamma"), _vector(dbeta, cols, dev, w + "dbeta"), None, 0)
-    _run(d, "structadmm_layer_norm_bwd", lib().structadmm_layer_norm_bwd_workspace, ws, X, stream, made)
+    _run(d, "structadmm_layer_norm_bwd", lib().structadmm_layer_norm_bwd_workspace, ws, X, stream)
     return dX, dgamma, dbeta
 
 
@@ -723,17 +708,16 @@ def linear_fwd(X, W, bias=None, R=None, act: int = ACT_NONE, Y=None, Z=None, out
     pre-activations, which linear_bwd reads."""
     M, K = _rows_of(X, "linear_fwd: X")
     N, _ = _rows_of(W, "linear_fwd: W")
-    dev, code, made, w = X.device, _type_code(X, "linear_fwd: X"), [], "linear_fwd: "
+    dev, code, w = X.device, _type_code(X, "linear_fwd: X"), "linear_fwd: "
     if Y is None:
-        Y = _new(X, M, N, out_dtype)
-        made.append(Y)
+        Y = _new(stream, X, M, N, out_dtype)
     out = _type_code(Y, w + "Y")
     r, ldr = _optional(R, M, N, out, dev, w + "R")
     z, ldz = _optional(Z, M, N, code, dev, w + "Z")
     d = LinearDesc(M, N, K, code, out, act, X.data_ptr(), _matrix(X, M, K, code, dev, w + "X"), W.data_ptr(),
                    _matrix(W, N, K, code, dev, w + "W"), _vector(bias, N, dev, w + "bias"), r, ldr, Y.data_ptr(),
                    _matrix(Y, M, N, out, dev, w + "Y"), z, ldz, None, 0)
-    _run(d, "structadmm_linear_fwd", lib().structadmm_linear_workspace, ws, X, stream, made)
+    _run(d, "structadmm_linear_fwd", lib().structadmm_linear_workspace, ws, X, stream)
     return Y
 
 
@@ -746,16 +730,13 @@ def linear_bwd(dY, X, W, Z=None, act: int = ACT_NONE, dX=None, dW=None, dbias=No
     import torch
     M, K = _rows_of(X, "linear_bwd: X")
     N, _ = _rows_of(W, "linear_bwd: W")
-    dev, code, made, w = X.device, _type_code(X, "linear_bwd: X"), [], "linear_bwd: "
+    dev, code, w = X.device, _type_code(X, "linear_bwd: X"), "linear_bwd: "
     if dX is None and "x" in grads:
-        dX = _new(X, M, K)
-        made.append(dX)
+        dX = _new(stream, X, M, K)
     if dW is None and "w" in grads:
-        dW = _new(X, N, K, dw_dtype or torch.float32)
-        made.append(dW)
+        dW = _new(stream, X, N, K, dw_dtype or torch.float32)
     if dbias is None and "b" in grads:
-        dbias = torch.empty(N, dtype=torch.float32, device=dev)
-        made.append(dbias)
+        dbias = _empty(stream, N, torch.float32, dev)
     wcode = code if dW is None else _type_code(dW, w + "dW")
     z, ldz = _optional(Z, M, N, code, dev, w + "Z")
     dx, lddx = _optional(dX, M, K, code, dev, w + "dX")
@@ -764,7 +745,7 @@ def linear_bwd(dY, X, W, Z=None, act: int = ACT_NONE, dX=None, dW=None, dbias=No
                       X.data_ptr(), _matrix(X, M, K, code, dev, w + "X"), W.data_ptr(),
                       _matrix(W, N, K, code, dev, w + "W"), dx, lddx, dw, lddw, _vector(dbias, N, dev, w + "dbias"),
                       None, 0)
-    _run(d, "structadmm_linear_bwd", lib().structadmm_linear_bwd_workspace, ws, X, stream, made)
+    _run(d, "structadmm_linear_bwd", lib().structadmm_linear_bwd_workspace, ws, X, stream)
     return dX, dW, dbias
 
 
@@ -782,18 +763,17 @@ def glu_fwd(X, Wg, Wu, bg=None, bu=None, act: int = ACT_SILU, H=None, G=None, U=
     (both or neither) receive the two projections, which glu_bwd reads."""
     M, K = _rows_of(X, "glu_fwd: X")
     N, _ = _rows_of(Wg, "glu_fwd: Wg")
-    dev, code, made, w = X.device, _type_code(X, "glu_fwd: X"), [], "glu_fwd: "
+    dev, code, w = X.device, _type_code(X, "glu_fwd: X"), "glu_fwd: "
     if (G is None) != (U is None):
         raise StructAdmmError(w + "give both G and U or neither")
     if H is None:
-        H = _new(X, M, N)
-        made.append(H)
+        H = _new(stream, X, M, N)
     ldgu = N if G is None else _pair(G, U, M, N, code, dev, (w + "G", w + "U"))
     d = GluDesc(M, N, K, code, act, X.data_ptr(), _matrix(X, M, K, code, dev, w + "X"), Wg.data_ptr(), Wu.data_ptr(),
                 _pair(Wg, Wu, N, K, code, dev, (w + "Wg", w + "Wu")), _vector(bg, N, dev, w + "bg"),
                 _vector(bu, N, dev, w + "bu"), H.data_ptr(), _matrix(H, M, N, code, dev, w + "H"), _ptr(G), _ptr(U),
                 ldgu, None, 0)
-    _run(d, "structadmm_glu_fwd", lib().structadmm_glu_workspace, ws, X, stream, made)
+    _run(d, "structadmm_glu_fwd", lib().structadmm_glu_workspace, ws, X, stream)
     return H
 
 
@@ -806,22 +786,18 @@ def glu_bwd(dH, X, Wg, Wu, G, U, act: int = ACT_SILU, dX=None, dWg=None, dWu=Non
     import torch
     M, K = _rows_of(X, "glu_bwd: X")
     N, _ = _rows_of(Wg, "glu_bwd: Wg")
-    dev, code, made, w = X.device, _type_code(X, "glu_bwd: X"), [], "glu_bwd: "
+    dev, code, w = X.device, _type_code(X, "glu_bwd: X"), "glu_bwd: "
     if (dWg is None) != (dWu is None):
         raise StructAdmmError(w + "give both dWg and dWu or neither")
     if dX is None and "x" in grads:
-        dX = _new(X, M, K)
-        made.append(dX)
+        dX = _new(stream, X, M, K)
     if dWg is None and "w" in grads:
-        dW = _new(X, N, 2 * K, dw_dtype or torch.float32)
-        made.append(dW)
+        dW = _new(stream, X, N, 2 * K, dw_dtype or torch.float32)
         dWg, dWu = dW[:, :K], dW[:, K:]
     if dbg is None and "b" in grads:
-        dbg = torch.empty(N, dtype=torch.float32, device=dev)
-        made.append(dbg)
+        dbg = _empty(stream, N, torch.float32, dev)
     if dbu is None and "b" in grads:
-        dbu = torch.empty(N, dtype=torch.float32, device=dev)
-        made.append(dbu)
+        dbu = _empty(stream, N, torch.float32, dev)
     wcode = code if dWg is None else _type_code(dWg, w + "dWg")
     dx, lddx = _optional(dX, M, K, code, dev, w + "dX")
     lddw = K if dWg is None else _pair(dWg, dWu, N, K, wcode, dev, (w + "dWg", w + "dWu"))
@@ -830,7 +806,7 @@ def glu_bwd(dH, X, Wg, Wu, G, U, act: int = ACT_SILU, dX=None, dWg=None, dWu=Non
                    _matrix(X, M, K, code, dev, w + "X"), Wg.data_ptr(), Wu.data_ptr(),
                    _pair(Wg, Wu, N, K, code, dev, (w + "Wg", w + "Wu")), dx, lddx, _ptr(dWg), _ptr(dWu), lddw,
                    _vector(dbg, N, dev, w + "dbg"), _vector(dbu, N, dev, w + "dbu"), None, 0)
-    _run(d, "structadmm_glu_bwd", lib().structadmm_glu_bwd_workspace, ws, X, stream, made)
+    _run(d, "structadmm_glu_bwd", lib().structadmm_glu_bwd_workspace, ws, X, stream)
     return dX, dWg, dWu, dbg, dbu
 
 
