@@ -476,6 +476,13 @@ int structadmm_conv_sparse_fwd(const sa_sparse_conv_desc *desc, hipStream_t stre
  * an empty sum is 0.  Infinities and NaN of the inputs reach the outputs that
  * depend on them and no others.  Outputs may not overlap inputs or each other,
  * except where stated.
+ *
+ * A workspace size depends on the sizes, the types, which outputs are given and
+ * whether the operands' rows start on 16-byte boundaries.  It holds for calls with
+ * these outputs, or fewer of them, and with pointers aligned like those in the
+ * descriptor.  A query may come before the buffers: an operand that is NULL may
+ * start anywhere later, and while the first matrix of a backward descriptor (dY or
+ * dH) is NULL the size is for every output.  The query reads no buffer.
  */
 typedef enum {
     SA_BF16 = 0, /* bfloat16 */
@@ -547,7 +554,7 @@ typedef struct sa_layer_norm_bwd_desc {
     size_t ws_bytes;
 } sa_layer_norm_bwd_desc;
 
-/* Workspace bytes (0 if none, and for an invalid descriptor; the pointers are not read). */
+/* Workspace bytes (0 if none, and for an invalid descriptor). */
 size_t structadmm_layer_norm_bwd_workspace(const sa_layer_norm_bwd_desc *desc);
 int structadmm_layer_norm_bwd(const sa_layer_norm_bwd_desc *desc, hipStream_t stream);
 

@@ -207,6 +207,54 @@ Gemm product(const sa_glu_desc &d) {
                 Epilogue{d.act, 0, d.bg, d.bu, nullptr, 0, d.H, d.ldh, d.G, d.U, d.ldgu}, nullptr};
 }
 
+// A size query may come before the buffers.  An operand that is NULL then counts as one
+// whose rows start anywhere, and a backward descriptor without its first matrix as one of
+// every output, so that the size covers each call that may follow.
+template <typename P>
+void assume(P *&p) {
+    if (!p) p = reinterpret_cast<P *>(alignof(uint16_t));
+}
+
+size_t workspace(sa_linear_desc d) {
+    assume(d.X);
+    assume(d.W);
+    return gemm_workspace(product(d));
+}
+
+size_t workspace(sa_glu_desc d) {
+    assume(d.X);
+    assume(d.Wg);
+    assume(d.Wu);
+    return gemm_workspace(product(d));
+}
+
+size_t workspace(sa_linear_bwd_desc d) {
+    if (!d.dY && d.M > 0 && d.N > 0) {
+        assume(d.dY);
+        assume(d.dX);
+        assume(d.dW);
+        assume(d.dbias);
+    }
+    assume(d.X);
+    assume(d.W);
+    return plan(d, nullptr).bytes;
+}
+
+size_t workspace(sa_glu_bwd_desc d) {
+    if (!d.dH && d.M > 0 && d.N > 0) {
+        assume(d.dH);
+        assume(d.dX);
+        assume(d.dWg);
+        assume(d.dWu);
+        assume(d.dbg);
+        assume(d.dbu);
+    }
+    assume(d.X);
+    assume(d.Wg);
+    assume(d.Wu);
+    return plan(d, nullptr).bytes;
+}
+
 }  // namespace
 }  // namespace sa
 
@@ -214,7 +262,7 @@ using namespace sa;
 
 extern "C" size_t structadmm_linear_workspace(const sa_linear_desc *desc) {
     if (!desc || validate_linear_sizes(*desc) != SA_OK) return 0;
-    return gemm_workspace(product(*desc));
+    return workspace(*desc);
 }
 
 extern "C" int structadmm_linear_fwd(const sa_linear_desc *desc, hipStream_t stream) {
@@ -229,7 +277,7 @@ extern "C" int structadmm_linear_fwd(const sa_linear_desc *desc, hipStream_t str
 
 extern "C" size_t structadmm_linear_bwd_workspace(const sa_linear_bwd_desc *desc) {
     if (!desc || validate_linear_bwd_sizes(*desc) != SA_OK) return 0;
-    return plan(*desc, nullptr).bytes;
+    return workspace(*desc);
 }
 
 extern "C" int structadmm_linear_bwd(const sa_linear_bwd_desc *desc, hipStream_t stream) {
@@ -243,7 +291,7 @@ extern "C" int structadmm_linear_bwd(const sa_linear_bwd_desc *desc, hipStream_t
 
 extern "C" size_t structadmm_glu_workspace(const sa_glu_desc *desc) {
     if (!desc || validate_glu_sizes(*desc) != SA_OK) return 0;
-    return gemm_workspace(product(*desc));
+    return workspace(*desc);
 }
 
 extern "C" int structadmm_glu_fwd(const sa_glu_desc *desc, hipStream_t stream) {
@@ -258,7 +306,7 @@ extern "C" int structadmm_glu_fwd(const sa_glu_desc *desc, hipStream_t stream) {
 
 extern "C" size_t structadmm_glu_bwd_workspace(const sa_glu_bwd_desc *desc) {
     if (!desc || validate_glu_bwd_sizes(*desc) != SA_OK) return 0;
-    return plan(*desc, nullptr).bytes;
+    return workspace(*desc);
 }
 
 extern "C" int structadmm_glu_bwd(const sa_glu_bwd_desc *desc, hipStream_t stream) {

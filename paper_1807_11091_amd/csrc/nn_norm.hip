@@ -603,7 +603,10 @@ static size_t ln_bwd_bytes(const sa_layer_norm_bwd_desc &d) {
 
 extern "C" size_t structadmm_layer_norm_bwd_workspace(const sa_layer_norm_bwd_desc *desc) {
     if (!desc || validate_layer_norm_bwd_sizes(*desc) != SA_OK) return 0;
-    return ln_bwd_bytes(*desc);
+    sa_layer_norm_bwd_desc d = *desc;
+    float any;
+    if (!d.dY && d.rows > 0) d.dgamma = &any;  // before the buffers: as for every output
+    return ln_bwd_bytes(d);
 }
 
 extern "C" int structadmm_layer_norm_bwd(const sa_layer_norm_bwd_desc *desc, hipStream_t stream) {
