@@ -61,8 +61,36 @@ __device__ inline float wave_sum_f32(float x) {
 // below the smallest normal number becomes 0.
 __device__ inline float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
 
-constexpr float kSqrtHalf = 0.70710678118654752f;
 constexpr float kInvSqrt2Pi = 0.39894228040143268f;
+
+// The normal distribution's Phi(x) = P(X <= x), without the difference 1 - erf of its
+// lower tail.  With a = |x| and e = exp(-x^2 / 4), Phi(-a) = e^2 h(a), where
+// h(a) = exp(a^2 / 2) Phi(-a) falls smoothly from 1/2 to 1 / (a sqrt(2 pi)): t = 1 / (1 + a/4)
+// times a polynomial in t of degree 9, fitted for the least relative error (3.4e-8; 4e-7 with
+// the roundings of its evaluation).  e and not e^2, so that products with e * e keep their
+// bits down to the smallest normal number (x = -13.1).  A product of 8192 x 4096 x 1024
+// bfloat16 with it takes 105 us, with erff 118.
+struct NormalTail {
+    float e, h, xe;  // xe: x e, and 0 at +infinity
+    __device__ explicit NormalTail(float x) {
+        e = __expf(x * x * -0.25f);
+        xe = fminf(x, 64.0f) * e;
+        const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(x), 0.25f, 1.0f));
+        constexpr float c[] = {0.0997355655f, 0.0997364298f, 0.0934663564f, 0.0816031024f,  0.0589751787f,
+                               0.0636990219f, -0.03171736f,  0.0955969095f, -0.0808772147f, 0.0197819863f};
+        float s = c[9];
+#pragma unroll
+        for (int k = 8; k >= 0; --k) s = fmaf(s, t, c[k]);
+        h = s * t;
+    }
+    // x Phi(x) = max(x, 0) - |x| Phi(-|x|), and its derivative; no branch
+    __device__ float value(float x) const { return fmaxf(x, 0.0f) - fabsf(xe * (e * h)); }
+    __device__ float slope(float x) const {
+        const float tail = e * e * h;
+        return fmaf(xe, e * kInvSqrt2Pi, x < 0.0f ? tail : 1.0f - tail);
+    }
+};
+
 constexpr float kTwoSqrt2OverPi = 1.5957691216057308f;  // 2 sqrt(2 / pi)
 constexpr float kGeluCubic = 0.044715f;
 
@@ -97,9 +125,9 @@ __device__ inline void activate(int act, const float (&z)[V], float (&value)[V],
         return;
     case SA_ACT_GELU:
         each([](float x, float &v, float &s) {
-            const float p = 0.5f * (1.0f + erff(x * kSqrtHalf));
-            v = x * p;
-            if (SLOPE) s = p + x * (kInvSqrt2Pi * __expf(-0.5f * x * x));
+            const NormalTail tail(x);
+            v = tail.value(x);
+            if (SLOPE) s = tail.slope(x);
         });
         return;
     case SA_ACT_GELU_TANH:
