@@ -508,7 +508,9 @@ typedef enum {
  * mean[r] = sum_c X[r][c] / cols, rstd[r] = 1 / sqrt(sum_c (X[r][c] - mean[r])^2 / cols + eps).
  * gamma NULL stands for ones, beta NULL for zeros.  mean and rstd may be NULL
  * (a forward pass without a backward one).  Y may be X itself with the same
- * pitch.  A row of equal values gives rstd = 1 / sqrt(eps) and Y = beta.
+ * pitch.  With eps > 0 a row of equal values gives Y = beta, the values as their
+ * mean and rstd = 1 / sqrt(eps) up to rounding (rows of up to 16384 columns; longer
+ * ones to within the rounding of their sums).
  */
 typedef struct sa_layer_norm_desc {
     int64_t rows, cols;   /* rows >= 0, cols >= 1 */
