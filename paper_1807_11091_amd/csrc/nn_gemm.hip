@@ -498,8 +498,8 @@ __device__ __forceinline__ void tile_product(const TileArgs &a, int block) {
     if (first >= end) return;
     const int mine = (end - first + stride - 1) / stride;  // tiles of this workgroup
 
-    const int K = uni((int)g.K);
-    const int sp = (K + BK - 1) / BK, ns = NA && !MA ? sp * uni(g.parts) : sp;  // stages of a part, of a tile
+    const int K = uni((int)g.K);  // a sum over rows may have 2^31 - 1 terms: nothing is added to K
+    const int sp = K / BK + (K % BK != 0), ns = NA && !MA ? sp * uni(g.parts) : sp;  // stages of a part, of a tile
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)smem;
     const int64_t nld = g.n[0].ld, mld = g.m[0].ld;  // parts and batches share their pitch
 
@@ -566,8 +566,8 @@ __device__ __forceinline__ void tile_product(const TileArgs &a, int block) {
         mc = MSide::open(reinterpret_cast<const T *>(second || (MA && q.z) ? g.m[1].p : g.m[0].p) + mo, mld, mrows, K, k0);
         nside.limit(K - k0);
         mside.limit(K - k0);
-        if (k0 + BK > K && (K & 7) != 0) cuts |= 1 << lslot;
-        run = uni(k0 + BK <= K ? min(K / BK - st, lend - lstage) : 1);
+        if (BK > K - k0 && (K & 7) != 0) cuts |= 1 << lslot;
+        run = uni(BK <= K - k0 ? min(K / BK - st, lend - lstage) : 1);
         lstage += run;
     };
     // The stage that is loaded next: begin, its loads 0 .. L - 1, end.
