@@ -637,6 +637,8 @@ def _run(desc, name: str, ws_fn, ws, like, stream):
                 import torch
                 ws = _empty(stream, need, torch.uint8, like.device)
         if ws is not None:
+            if ws.device != like.device or not ws.is_contiguous():
+                raise StructAdmmError(f"{name}: ws must be contiguous and on {like.device}, not {ws.device}")
             desc.ws, desc.ws_bytes = ws.data_ptr(), ws.numel() * ws.element_size()
     _check(getattr(lib(), name)(ctypes.byref(desc), _stream(stream)), name)
 

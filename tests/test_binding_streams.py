@@ -134,6 +134,25 @@ def test_memory_on_the_current_stream(pools, name, handle):
     assert pools and all(pool == "current" and not t.users for pool, t in pools)
 
 
+@pytest.mark.parametrize("name", ["layer_norm_bwd", "linear_fwd", "linear_bwd", "glu_fwd", "glu_bwd"])
+def test_workspaces_that_are_refused(pools, name):
+    """A workspace in host memory, or a view whose elements lie apart, is not handed to
+    the kernels."""
+    import torch
+    bf, f32 = torch.bfloat16, torch.float32
+    X, Y, W, V, m = Stand((6, 8), bf), Stand((6, 10), bf), Stand((10, 8), bf), Stand((10, 8), bf), Stand(6, f32)
+    args = {"layer_norm_bwd": (X, X, m, m), "linear_fwd": (X, W), "linear_bwd": (Y, X, W), "glu_fwd": (X, W, V),
+            "glu_bwd": (Y, X, W, V, Y, Y)}[name]
+    call = getattr(sa, name)
+    call(*args, ws=Stand(4096, torch.uint8))
+    with pytest.raises(sa.StructAdmmError, match="ws must be contiguous and on cuda:0"):
+        call(*args, ws=torch.zeros(4096, dtype=torch.uint8))
+    apart = Stand(4096, torch.uint8)
+    apart.is_contiguous = lambda: False
+    with pytest.raises(sa.StructAdmmError, match="contiguous"):
+        call(*args, ws=apart)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("raw", [False, True])
 def test_a_busy_block_is_not_taken(raw):
