@@ -871,9 +871,10 @@ struct Plan {
     float time;  // of the model, microseconds
 };
 
-// Time models, microseconds, fitted to 364 products (40 to 2048 rows and fewer, 512 to
-// 19712 by 512 to 9856, forward and both gradients, k in 1 to 32 chunks: 3600 launches;
-// median error 5%).  The model's choice takes 1.012 of the best one's time on average.
+// Time models, microseconds, fitted to 364 products (4 to 2048 rows, 512 to 19712 by 512
+// to 9856, forward and both gradients, k in 1 to 32 chunks: 4382 launches; median error 3
+// to 7% a kernel).  The model's choice takes 1.012 of the best one's time on average, 1.34
+// at most.
 struct TileModel {
     int bn, bm, slots;    // tile; workgroups that the 256 CUs hold
     float launch, round;  // a launch; a round of tiles

@@ -6,7 +6,12 @@
 //             dWg = dg^T x, dWu = du^T x, dbg and dbu their column sums
 //
 // dz (dg and du) go to the workspace in the operands' type, as the matrix cores
-// read them; the bias gradients are summed from the binary32 values.
+// read them; the bias gradients are summed from the binary32 values.  That rounding is
+// the price of the 16-bit products: binary32 values would have to go in as sums of two
+// 16-bit ones, for twice the products.  Against binary64 it takes the error of dX and
+// dW from 2.1e-4 to 2.9e-4 of their size in binary16 and from 1.7e-3 to 2.3e-3 in
+// bfloat16, whatever dW's type; without an activation dz is dY itself and nothing is
+// rounded.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

@@ -31,7 +31,8 @@ constexpr int kV = 8;  // elements per vector
 // Rows of TPR threads each that a workgroup of the register kernels takes at a time.
 // WIDE: four of 192 threads instead of two, for the backward kernel of 16-bit types: a
 // CU holds one workgroup of it, which needs that many loads in flight (16384 x 2560
-// bfloat16 66.7 us with two, 54.8 with four).
+// bfloat16 66.7 us with two, 54.8 with four).  Rows of 384 threads, one a
+// workgroup, were not tried in pairs.
 template <int TPR, bool WIDE = false>
 struct Rows {
     static constexpr int per_group =
@@ -286,7 +287,7 @@ struct BwdArgs {
 // what hides the memory's latency is the next row's x and dy, read while this row is
 // worked on: into a second set of registers, the loop unrolled by two, since a copy
 // from one set to the other would wait for them.  Bound by memory: 16384 x 4096
-// bfloat16 in 104 us with the joining of the sums, 5.2 TB/s over x, dy and dx (209 us
+// bfloat16 in 104 us with the joining of the sums, 5.2 TB/s over x, dy, dr and dx (209 us
 // without the next row, 134 us when copies waited for it).
 template <typename T, int TPR, int CH, bool SHORT>
 __global__ __launch_bounds__((Rows<TPR, sizeof(T) == 2>::threads), (Rows<TPR, sizeof(T) == 2>::threads > 512 ? 3 : 2)) void k_ln_bwd(BwdArgs a) {
