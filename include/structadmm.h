@@ -689,6 +689,183 @@ typedef struct sa_glu_bwd_desc {
 size_t structadmm_glu_bwd_workspace(const sa_glu_bwd_desc *desc);
 int structadmm_glu_bwd(const sa_glu_bwd_desc *desc, hipStream_t stream);
 
+/* ---- 8-bit feed-forward operators ------------------------------------ */
+/*
+ * The block around a pruned matrix in 8-bit floating point: the root-mean-square
+ * norm with the residual's addition, the quantisation of weights, activations and
+ * gradients, the linear layer and the gated pair.  What is said above of matrices,
+ * sizes of 0, infinities, overlap and workspaces holds here too.
+ *
+ * An 8-bit matrix has codes in e4m3 (sign, 4 bits of exponent, 3 of mantissa;
+ * largest 448, smallest 2^-9, no infinity) and a binary32 scale for each block of
+ * SA_BLOCK columns of a row ("row blocks": activations and gradients), or of
+ * SA_BLOCK rows by SA_BLOCK columns ("square blocks": weights; the last blocks of a
+ * side may be smaller).  Element (r, c) stands for
+ *   codes[r * ld + c] * scales[rb * scale_row + c / SA_BLOCK * scale_col],
+ * rb = r or r / SA_BLOCK.  Rows of codes start on 16-byte boundaries: codes is
+ * 16-byte aligned and ld a multiple of 16 (at most SA_MAX_LD).  scale_row is at
+ * most SA_MAX_LD; the strides of an operand may be 0 (one scale for several blocks).
+ * The products read scales fastest where those of one block column lie side by side
+ * (scale_row = 1).
+ *
+ * Written by these calls, a block has
+ *   scale = max(largest |v| / 448, 2^-126), code = v * (1 / scale) to nearest even,
+ * of the binary32 values v.  The scale leaves NaN out of account and a NaN has a NaN
+ * code; in a block with an infinity the scale is infinite, the infinities' codes are
+ * NaN and the others 0, so that a product with the block gives NaN.
+ */
+#define SA_BLOCK 128
+
+typedef struct sa_matrix8 {
+    uint8_t *codes;
+    int64_t ld;          /* row pitch of codes, in bytes */
+    float *scales;
+    int64_t scale_row;   /* strides of scales, in elements: to the next block row ... */
+    int64_t scale_col;   /* ... and block column */
+} sa_matrix8;
+
+/* ---- root-mean-square norm: structadmm_rms_norm_fwd / _bwd ----------- */
+/*
+ * S = X + R, rounded to its type (S = X where R is NULL),
+ * Y[r][c] = S[r][c] * rstd[r] * gamma[c], rstd[r] = 1 / sqrt(sum_c S[r][c]^2 / cols + eps).
+ * gamma NULL stands for ones.  S, Y, Q and rstd may each be left out (NULL; at least
+ * one of S, Y and Q is given): Y receives the result in the inputs' type, Q in 8 bits
+ * with row blocks, both from the same binary32 values.  S may be X or R itself, and Y
+ * one of them that S is not, with the same pitch.
+ */
+typedef struct sa_rms_norm_desc {
+    int64_t rows, cols;   /* rows >= 0, cols >= 1 */
+    int32_t type;         /* sa_type of X, R, S and Y */
+    float eps;            /* >= 0 */
+    const void *X;
+    int64_t ldx;
+    const void *R;        /* or NULL */
+    int64_t ldr;
+    const float *gamma;   /* [cols] or NULL */
+    void *S;              /* out or NULL */
+    int64_t lds;
+    void *Y;              /* out or NULL */
+    int64_t ldy;
+    sa_matrix8 Q;         /* out [rows, cols], row blocks; codes NULL: none */
+    float *rstd;          /* out [rows] or NULL */
+} sa_rms_norm_desc;
+
+int structadmm_rms_norm_fwd(const sa_rms_norm_desc *desc, hipStream_t stream);
+
+/*
+ * With xn = S * rstd and t = dY * gamma:
+ *   dX     = rstd * (t - xn * sum_c(t * xn) / cols) + dR
+ *   dgamma = sum over rows of dY * xn.
+ * dX is the gradient of X and of R.  dR is the gradient that reaches S past the
+ * norm, NULL for none; dX may be dR or dY itself with the same pitch.  dX and dgamma
+ * may each be NULL (at least one is given).
+ */
+typedef struct sa_rms_norm_bwd_desc {
+    int64_t rows, cols;
+    int32_t type;         /* sa_type of dY, S, dR and dX */
+    const void *dY;
+    int64_t lddy;
+    const void *S;        /* as the forward pass wrote it (X where there was no R) */
+    int64_t lds;
+    const float *rstd;    /* [rows], as the forward pass wrote it */
+    const float *gamma;   /* [cols] or NULL */
+    const void *dR;       /* or NULL */
+    int64_t lddr;
+    void *dX;             /* out or NULL */
+    int64_t lddx;
+    float *dgamma;        /* out [cols] or NULL */
+    void *ws;             /* structadmm_rms_norm_bwd_workspace() bytes, 256-byte aligned */
+    size_t ws_bytes;
+} sa_rms_norm_bwd_desc;
+
+size_t structadmm_rms_norm_bwd_workspace(const sa_rms_norm_bwd_desc *desc);
+int structadmm_rms_norm_bwd(const sa_rms_norm_bwd_desc *desc, hipStream_t stream);
+
+/* ---- quantisation: structadmm_quantize8 ------------------------------ */
+/*
+ * X in 8 bits, with row blocks (block_rows 1) or square blocks (block_rows SA_BLOCK):
+ * Q [rows, cols] as it stands, QT [cols, rows] transposed (each may be left out, codes
+ * NULL).  The row blocks of QT run along X's rows, and so have scales of their own;
+ * with square blocks QT holds the codes and scales of Q transposed.
+ *
+ * A product's gradients are products of such operands: with dY's row blocks Q and QT,
+ * the square blocks QT of W and QT of X,
+ *   dX = linear8_fwd(dY.Q, W.QT), dW = linear8_fwd(dY.QT, X.QT) (out_type SA_F32).
+ */
+typedef struct sa_quantize8_desc {
+    int64_t rows, cols;   /* QT: rows at most SA_MAX_LD */
+    int32_t type;         /* sa_type of X */
+    int32_t block_rows;   /* 1 or SA_BLOCK */
+    const void *X;
+    int64_t ldx;
+    sa_matrix8 Q;         /* out */
+    sa_matrix8 QT;        /* out */
+} sa_quantize8_desc;
+
+int structadmm_quantize8(const sa_quantize8_desc *desc, hipStream_t stream);
+
+/* ---- 8-bit linear layer: structadmm_linear8_fwd ---------------------- */
+/*
+ * z = X W^T + bias, y = act(z) + R: X [M, K] with row blocks, W [N, K] with square
+ * blocks, bias [N], R [M, N].  The sum of a block's products is scaled in binary32 by
+ * both scales and added up.  Y receives y in out_type, Q in 8 bits with row blocks
+ * (at least one is given), Z, when given, z for the backward pass.  Y may be R itself
+ * with the same pitch.
+ */
+typedef struct sa_linear8_desc {
+    int64_t M, N, K;
+    int32_t type;        /* SA_BF16 or SA_F16: Z         */
+    int32_t out_type;    /* type or SA_F32: R and Y      */
+    int32_t act;         /* sa_act */
+    sa_matrix8 X;
+    sa_matrix8 W;
+    const float *bias;   /* [N] or NULL */
+    const void *R;       /* [M, N] or NULL */
+    int64_t ldr;
+    void *Y;             /* out [M, N] or NULL */
+    int64_t ldy;
+    void *Z;             /* out [M, N] or NULL */
+    int64_t ldz;
+    sa_matrix8 Q;        /* out [M, N]; codes NULL: none */
+    void *ws;            /* structadmm_linear8_workspace() bytes, 256-byte aligned */
+    size_t ws_bytes;
+} sa_linear8_desc;
+
+/* The query holds for calls with these outputs or fewer, whatever their pointers; before
+ * the outputs (Y and Q NULL) it is for all of them. */
+size_t structadmm_linear8_workspace(const sa_linear8_desc *desc);
+int structadmm_linear8_fwd(const sa_linear8_desc *desc, hipStream_t stream);
+
+/* ---- 8-bit gated pair of projections: structadmm_glu8_fwd ------------ */
+/*
+ * g = X Wg^T + bg, u = X Wu^T + bu, h = act(g) * u: X [M, K] with row blocks, Wg and
+ * Wu [N, K] with square blocks.  H receives h in 16 bits, Q in 8 bits with row blocks
+ * (at least one is given); G and U, when given (both or neither), g and u for
+ * structadmm_glu_bwd.  Everything is computed from the unrounded g and u.  Wg and Wu
+ * share their pitch and the strides of their scales.
+ */
+typedef struct sa_glu8_desc {
+    int64_t M, N, K;
+    int32_t type;        /* SA_BF16 or SA_F16: H, G and U */
+    int32_t act;         /* sa_act */
+    sa_matrix8 X;
+    sa_matrix8 Wg;
+    sa_matrix8 Wu;
+    const float *bg;     /* [N] or NULL */
+    const float *bu;     /* [N] or NULL */
+    void *H;             /* out or NULL */
+    int64_t ldh;
+    void *G;             /* out or NULL */
+    void *U;             /* out or NULL */
+    int64_t ldgu;        /* pitch of G and U */
+    sa_matrix8 Q;        /* out [M, N]; codes NULL: none */
+    void *ws;            /* structadmm_glu8_workspace() bytes, 256-byte aligned */
+    size_t ws_bytes;
+} sa_glu8_desc;
+
+size_t structadmm_glu8_workspace(const sa_glu8_desc *desc);
+int structadmm_glu8_fwd(const sa_glu8_desc *desc, hipStream_t stream);
+
 /* Message describing the last error on the calling thread ("" if none). */
 const char *structadmm_last_error(void);
 

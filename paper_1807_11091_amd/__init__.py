@@ -23,6 +23,12 @@ Entry points (same names as the C ABI):
   linear_bwd(dY, X, W, Z=None, act=ACT_NONE, ...) -> (dX, dW, dbias)
   glu_fwd(X, Wg, Wu, bg=None, bu=None, act=ACT_SILU, ...) -> H
   glu_bwd(dH, X, Wg, Wu, G, U, act=ACT_SILU, ...) -> (dX, dWg, dWu, dbg, dbu)
+  rms_norm_fwd(X, gamma=None, R=None, eps=1e-5, ...) -> (Y, S, rstd, Q)
+  rms_norm_bwd(dY, S, rstd, gamma=None, dR=None, ...) -> (dX, dgamma)
+  quantize8(X, block_rows=1, ...) -> (Q, QT)
+  linear8_fwd(X, W, bias=None, R=None, act=ACT_NONE, ...) -> (Y, Q)
+  glu8_fwd(X, Wg, Wu, bg=None, bu=None, act=ACT_SILU, ...) -> (H, Q)
+  matrix8(rows, cols, block_rows=1, ...) -> an uninitialised Matrix8
   compacted_matrix(Wc, sizes, group=0) -> the [M, K] matrix of a compacted layer
 """
 from __future__ import annotations
@@ -30,7 +36,7 @@ from __future__ import annotations
 import ctypes
 import os
 from dataclasses import dataclass
-from typing import List, Optional, Sequence
+from typing import List, NamedTuple, Optional, Sequence
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libstructadmm.so")
@@ -172,6 +178,42 @@ class GluBwdDesc(ctypes.Structure):
                 ("dbg", _vp), ("dbu", _vp), ("ws", _vp), ("ws_bytes", _sz)]
 
 
+BLOCK = 128  # columns (and rows, of a square block) that share a scale of an 8-bit matrix
+
+
+class Matrix8Arg(ctypes.Structure):
+    _fields_ = [("codes", _vp), ("ld", _i64), ("scales", _vp), ("scale_row", _i64), ("scale_col", _i64)]
+
+
+class RmsNormDesc(ctypes.Structure):
+    _fields_ = [("rows", _i64), ("cols", _i64), ("type", _i32), ("eps", ctypes.c_float), ("X", _vp), ("ldx", _i64),
+                ("R", _vp), ("ldr", _i64), ("gamma", _vp), ("S", _vp), ("lds", _i64), ("Y", _vp), ("ldy", _i64),
+                ("Q", Matrix8Arg), ("rstd", _vp)]
+
+
+class RmsNormBwdDesc(ctypes.Structure):
+    _fields_ = [("rows", _i64), ("cols", _i64), ("type", _i32), ("dY", _vp), ("lddy", _i64), ("S", _vp), ("lds", _i64),
+                ("rstd", _vp), ("gamma", _vp), ("dR", _vp), ("lddr", _i64), ("dX", _vp), ("lddx", _i64),
+                ("dgamma", _vp), ("ws", _vp), ("ws_bytes", _sz)]
+
+
+class Quantize8Desc(ctypes.Structure):
+    _fields_ = [("rows", _i64), ("cols", _i64), ("type", _i32), ("block_rows", _i32), ("X", _vp), ("ldx", _i64),
+                ("Q", Matrix8Arg), ("QT", Matrix8Arg)]
+
+
+class Linear8Desc(ctypes.Structure):
+    _fields_ = [("M", _i64), ("N", _i64), ("K", _i64), ("type", _i32), ("out_type", _i32), ("act", _i32),
+                ("X", Matrix8Arg), ("W", Matrix8Arg), ("bias", _vp), ("R", _vp), ("ldr", _i64), ("Y", _vp),
+                ("ldy", _i64), ("Z", _vp), ("ldz", _i64), ("Q", Matrix8Arg), ("ws", _vp), ("ws_bytes", _sz)]
+
+
+class Glu8Desc(ctypes.Structure):
+    _fields_ = [("M", _i64), ("N", _i64), ("K", _i64), ("type", _i32), ("act", _i32), ("X", Matrix8Arg),
+                ("Wg", Matrix8Arg), ("Wu", Matrix8Arg), ("bg", _vp), ("bu", _vp), ("H", _vp), ("ldh", _i64),
+                ("G", _vp), ("U", _vp), ("ldgu", _i64), ("Q", Matrix8Arg), ("ws", _vp), ("ws_bytes", _sz)]
+
+
 class StructAdmmError(RuntimeError):
     pass
 
@@ -220,12 +262,14 @@ def lib():
         L.structadmm_conv_sparse_fwd.restype = ctypes.c_int
         for name, cls in (("layer_norm_fwd", LayerNormDesc), ("layer_norm_bwd", LayerNormBwdDesc),
                           ("linear_fwd", LinearDesc), ("linear_bwd", LinearBwdDesc), ("glu_fwd", GluDesc),
-                          ("glu_bwd", GluBwdDesc)):
+                          ("glu_bwd", GluBwdDesc), ("rms_norm_fwd", RmsNormDesc), ("rms_norm_bwd", RmsNormBwdDesc),
+                          ("quantize8", Quantize8Desc), ("linear8_fwd", Linear8Desc), ("glu8_fwd", Glu8Desc)):
             f = getattr(L, f"structadmm_{name}")
             f.argtypes = [ctypes.POINTER(cls), _vp]
             f.restype = ctypes.c_int
         for name, cls in (("layer_norm_bwd", LayerNormBwdDesc), ("linear", LinearDesc), ("linear_bwd", LinearBwdDesc),
-                          ("glu", GluDesc), ("glu_bwd", GluBwdDesc)):
+                          ("glu", GluDesc), ("glu_bwd", GluBwdDesc), ("rms_norm_bwd", RmsNormBwdDesc),
+                          ("linear8", Linear8Desc), ("glu8", Glu8Desc)):
             f = getattr(L, f"structadmm_{name}_workspace")
             f.argtypes = [ctypes.POINTER(cls)]
             f.restype = ctypes.c_size_t
@@ -810,6 +854,199 @@ def glu_bwd(dH, X, Wg, Wu, G, U, act: int = ACT_SILU, dX=None, dWg=None, dWu=Non
                    _vector(dbg, N, dev, w + "dbg"), _vector(dbu, N, dev, w + "dbu"), None, 0)
     _run(d, "structadmm_glu_bwd", lib().structadmm_glu_bwd_workspace, ws, X, stream)
     return dX, dWg, dWu, dbg, dbu
+
+
+# ------------------------------------------------ 8-bit feed-forward operators
+class Matrix8(NamedTuple):
+    """An 8-bit matrix: codes [rows, cols] (float8_e4m3fn, or its bits as uint8) with rows
+    on 16-byte boundaries, and float32 scales, one for each block of 128 columns of a row
+    ([rows, ceil(cols / 128)]: "row blocks") or of 128 rows ([ceil(rows / 128), ..]: "square
+    blocks")."""
+    codes: "object"
+    scales: "object"
+
+
+def _blocks(n: int) -> int:
+    return (n + BLOCK - 1) // BLOCK
+
+
+def matrix8(rows: int, cols: int, block_rows: int = 1, device=None, stream=None) -> Matrix8:
+    """An uninitialised 8-bit matrix as the calls below make them: rows of codes a
+    multiple of 128 bytes apart, the scales of a block column side by side."""
+    import torch
+    if block_rows not in (1, BLOCK):
+        raise StructAdmmError(f"matrix8: block_rows must be 1 or {BLOCK}, got {block_rows}")
+    device = torch.device("cuda", torch.cuda.current_device()) if device is None else device
+    nc, nr = _blocks(cols), rows if block_rows == 1 else _blocks(rows)
+    codes = _empty(stream, (rows, nc * BLOCK), torch.uint8, device)
+    scales = _empty(stream, (nc, nr), torch.float32, device)
+    return Matrix8(codes.view(torch.float8_e4m3fn)[:, :cols], scales.t())
+
+
+_e4m3 = []
+
+
+def _matrix8(m, rows: int, cols: int, block_rows: int, dev, what: str) -> Matrix8Arg:
+    """Checks a [rows, cols] 8-bit matrix argument (None: left out)."""
+    if m is None:
+        return Matrix8Arg(None, (cols + 15) // 16 * 16, None, 1, 1)
+    if not _e4m3:
+        import torch
+        _e4m3.extend((torch.float8_e4m3fn, torch.uint8, torch.float32))
+    codes, scales = m
+    if codes.shape != (rows, cols) or codes.dtype not in _e4m3[:2]:
+        raise StructAdmmError(f"{what} must hold e4m3 codes [{rows}, {cols}], got {codes.dtype} {tuple(codes.shape)}")
+    nr, nc = rows if block_rows == 1 else _blocks(rows), _blocks(cols)
+    if scales.shape != (nr, nc) or scales.dtype != _e4m3[2]:
+        raise StructAdmmError(f"{what} must have float32 scales [{nr}, {nc}], got {scales.dtype} {tuple(scales.shape)}")
+    if codes.device != dev or scales.device != dev:
+        raise StructAdmmError(f"{what} is on {codes.device} and {scales.device}, not {dev}")
+    ld, step = codes.stride()
+    if step != 1 and cols > 1 and rows > 0:
+        raise StructAdmmError(f"{what} must have unit column stride")
+    if rows <= 1 and (ld < cols or ld % 16 or ld > MAX_LD):
+        ld = (cols + 15) // 16 * 16  # a single row has no pitch
+    row, col = scales.stride()
+    return Matrix8Arg(codes.data_ptr(), ld, scales.data_ptr(), row if nr > 1 else 1, col if nc > 1 else 1)
+
+
+def _codes_of(m, what: str):
+    """The [rows, cols] of an 8-bit operand in GPU memory."""
+    if not isinstance(m, (tuple, list)) or len(m) != 2 or m[0].dim() != 2 or not m[0].is_cuda:
+        raise StructAdmmError(f"{what} must be a Matrix8 in GPU memory")
+    _type_code(m[1], what)
+    return m[0].shape
+
+
+def rms_norm_fwd(X, gamma=None, R=None, eps: float = 1e-5, S=None, Y=None, Q=None, rstd=None, out: str = "ysr",
+                 stream=None):
+    """structadmm_rms_norm_fwd over the rows of S = X + R (X [rows, cols] bfloat16,
+    float16 or float32; R like it or None); returns (Y, S, rstd, Q).  out names the
+    outputs to make besides the buffers given: "y" (the result in X's type), "q" (in 8
+    bits with row blocks), "s" (the sum; X itself where there is no R) and "r" (rstd,
+    which the backward pass reads); the others are None."""
+    import torch
+    rows, cols = _rows_of(X, "rms_norm_fwd: X")
+    dev, code, w = X.device, _type_code(X, "rms_norm_fwd: X"), "rms_norm_fwd: "
+    if Y is None and "y" in out:
+        Y = _new(stream, X, rows, cols)
+    if S is None and R is not None and "s" in out:
+        S = _new(stream, X, rows, cols)
+    if Q is None and "q" in out:
+        Q = matrix8(rows, cols, 1, dev, stream)
+    if rstd is None and "r" in out:
+        rstd = _empty(stream, rows, torch.float32, dev)
+    r, ldr = _optional(R, rows, cols, code, dev, w + "R")
+    s, lds = _optional(S, rows, cols, code, dev, w + "S")
+    y, ldy = _optional(Y, rows, cols, code, dev, w + "Y")
+    d = RmsNormDesc(rows, cols, code, eps, X.data_ptr(), _matrix(X, rows, cols, code, dev, w + "X"), r, ldr,
+                    _vector(gamma, cols, dev, w + "gamma"), s, lds, y, ldy, _matrix8(Q, rows, cols, 1, dev, w + "Q"),
+                    _vector(rstd, rows, dev, w + "rstd"))
+    _run(d, "structadmm_rms_norm_fwd", None, None, X, stream)
+    return Y, (X if S is None and R is None and "s" in out else S), rstd, Q
+
+
+def rms_norm_bwd(dY, S, rstd, gamma=None, dR=None, dX=None, dgamma=None, params: bool = True, ws=None, stream=None):
+    """structadmm_rms_norm_bwd; returns (dX, dgamma): dX is the gradient of X and of R.
+    dR: the gradient that reaches S past the norm, added to dX.  dgamma is None with
+    params=False (unless given)."""
+    import torch
+    rows, cols = _rows_of(S, "rms_norm_bwd: S")
+    dev, code, w = S.device, _type_code(S, "rms_norm_bwd: S"), "rms_norm_bwd: "
+    if rstd is None:
+        raise StructAdmmError(w + "rstd of the forward pass is required")
+    if dX is None:
+        dX = _new(stream, S, rows, cols)
+    if params and dgamma is None:
+        dgamma = _empty(stream, cols, torch.float32, dev)
+    r, ldr = _optional(dR, rows, cols, code, dev, w + "dR")
+    d = RmsNormBwdDesc(rows, cols, code, dY.data_ptr(), _matrix(dY, rows, cols, code, dev, w + "dY"), S.data_ptr(),
+                       _matrix(S, rows, cols, code, dev, w + "S"), _vector(rstd, rows, dev, w + "rstd"),
+                       _vector(gamma, cols, dev, w + "gamma"), r, ldr, dX.data_ptr(),
+                       _matrix(dX, rows, cols, code, dev, w + "dX"), _vector(dgamma, cols, dev, w + "dgamma"), None, 0)
+    _run(d, "structadmm_rms_norm_bwd", lib().structadmm_rms_norm_bwd_workspace, ws, S, stream)
+    return dX, dgamma
+
+
+def quantize8(X, block_rows: int = 1, Q=None, QT=None, out: str = "q", stream=None):
+    """structadmm_quantize8: X [rows, cols] (bfloat16, float16 or float32) in 8 bits, with
+    row blocks (block_rows=1) or square blocks (128); returns (Q, QT).  out names what to
+    make besides the matrices given: "q" (Q, as X stands) and "t" (QT [cols, rows], X
+    transposed); the others are None."""
+    rows, cols = _rows_of(X, "quantize8: X")
+    dev, code, w = X.device, _type_code(X, "quantize8: X"), "quantize8: "
+    if block_rows not in (1, BLOCK):
+        raise StructAdmmError(f"{w}block_rows must be 1 or {BLOCK}, got {block_rows}")
+    if Q is None and "q" in out:
+        Q = matrix8(rows, cols, block_rows, dev, stream)
+    if QT is None and "t" in out:
+        QT = matrix8(cols, rows, block_rows, dev, stream)
+    d = Quantize8Desc(rows, cols, code, block_rows, X.data_ptr(), _matrix(X, rows, cols, code, dev, w + "X"),
+                      _matrix8(Q, rows, cols, block_rows, dev, w + "Q"),
+                      _matrix8(QT, cols, rows, block_rows, dev, w + "QT"))
+    _run(d, "structadmm_quantize8", None, None, X, stream)
+    return Q, QT
+
+
+def _type16(t, what: str) -> Optional[int]:
+    """bfloat16's or float16's code of an output that may be None or float32 (None)."""
+    code = None if t is None else _type_code(t, what)
+    return None if code == F32 else code
+
+
+def linear8_fwd(X, W, bias=None, R=None, act: int = ACT_NONE, Y=None, Z=None, Q=None, out_dtype=None, out: str = "y",
+                ws=None, stream=None):
+    """structadmm_linear8_fwd: act(X W^T + bias) + R for 8-bit X [M, K] (row blocks) and W
+    [N, K] (square blocks); returns (Y, Q).  out names the results to make besides the
+    buffers given: "y" (Y in out_dtype: R's type or else bfloat16 by default, float16 or
+    float32) and "q" (Q in 8 bits with row blocks); the others are None.  R has Y's type.
+    Z (bfloat16 or float16, Y's type unless that is float32): receives the
+    pre-activations."""
+    import torch
+    M, K = _codes_of(X, "linear8_fwd: X")
+    N, _ = _codes_of(W, "linear8_fwd: W")
+    dev, w = X[0].device, "linear8_fwd: "
+    if Y is None and "y" in out:
+        like = R.dtype if R is not None else torch.bfloat16 if Z is None else Z.dtype
+        Y = _new(stream, X[0], M, N, out_dtype or like)
+    if Q is None and "q" in out:
+        Q = matrix8(M, N, 1, dev, stream)
+    code = next((c for c in (_type16(Z, w + "Z"), _type16(Y, w + "Y"), _type16(R, w + "R")) if c is not None), BF16)
+    to = code if Y is None and R is None else _type_code(R if Y is None else Y, w + "Y")
+    r, ldr = _optional(R, M, N, to, dev, w + "R")
+    y, ldy = _optional(Y, M, N, to, dev, w + "Y")
+    z, ldz = _optional(Z, M, N, code, dev, w + "Z")
+    d = Linear8Desc(M, N, K, code, to, act, _matrix8(X, M, K, 1, dev, w + "X"), _matrix8(W, N, K, BLOCK, dev, w + "W"),
+                    _vector(bias, N, dev, w + "bias"), r, ldr, y, ldy, z, ldz, _matrix8(Q, M, N, 1, dev, w + "Q"), None, 0)
+    _run(d, "structadmm_linear8_fwd", lib().structadmm_linear8_workspace, ws, X[0], stream)
+    return Y, Q
+
+
+def glu8_fwd(X, Wg, Wu, bg=None, bu=None, act: int = ACT_SILU, H=None, Q=None, G=None, U=None, dtype=None,
+             out: str = "q", ws=None, stream=None):
+    """structadmm_glu8_fwd: act(X Wg^T + bg) * (X Wu^T + bu) for 8-bit X [M, K] (row blocks),
+    Wg and Wu [N, K] (square blocks; one pitch and one layout of scales); returns (H, Q).
+    out names the results to make besides the buffers given: "h" (H in dtype: G's type or
+    else bfloat16 by default, or float16) and "q" (Q in 8 bits with row blocks); the others
+    are None.  G and U (both or neither) receive the two projections, which glu_bwd reads."""
+    import torch
+    M, K = _codes_of(X, "glu8_fwd: X")
+    N, _ = _codes_of(Wg, "glu8_fwd: Wg")
+    dev, w = X[0].device, "glu8_fwd: "
+    if (G is None) != (U is None):
+        raise StructAdmmError(w + "give both G and U or neither")
+    if H is None and "h" in out:
+        H = _new(stream, X[0], M, N, dtype or (torch.bfloat16 if G is None else G.dtype))
+    if Q is None and "q" in out:
+        Q = matrix8(M, N, 1, dev, stream)
+    code = BF16 if H is None and G is None else _type_code(G if H is None else H, w + "H")
+    h, ldh = _optional(H, M, N, code, dev, w + "H")
+    ldgu = N if G is None else _pair(G, U, M, N, code, dev, (w + "G", w + "U"))
+    d = Glu8Desc(M, N, K, code, act, _matrix8(X, M, K, 1, dev, w + "X"), _matrix8(Wg, N, K, BLOCK, dev, w + "Wg"),
+                 _matrix8(Wu, N, K, BLOCK, dev, w + "Wu"), _vector(bg, N, dev, w + "bg"), _vector(bu, N, dev, w + "bu"),
+                 h, ldh, _ptr(G), _ptr(U), ldgu, _matrix8(Q, M, N, 1, dev, w + "Q"), None, 0)
+    _run(d, "structadmm_glu8_fwd", lib().structadmm_glu8_workspace, ws, X[0], stream)
+    return H, Q
 
 
 def version() -> str:

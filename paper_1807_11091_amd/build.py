@@ -10,7 +10,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libstructadmm.so")
 SOURCES = ["sa_host.cpp", "admm.hip", "compact.hip", "conv.hip", "conv_ig.hip", "conv_tile.hip", "sparse.hip",
-           "nn_norm.hip", "nn_gemm.hip", "nn_linear.hip"]
+           "nn_norm.hip", "nn_gemm.hip", "nn_linear.hip", "nn_quant.hip", "nn_gemm8.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

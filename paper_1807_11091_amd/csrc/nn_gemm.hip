@@ -3,23 +3,17 @@
 
 #include <algorithm>
 #include <cstdint>
-#include <exception>
-#include <map>
-#include <mutex>
 #include <type_traits>
-#include <utility>
 
+#include "nn_epilogue.h"
 #include "nn_gemm.h"
+#include "nn_tile.h"
 #include "nn_types.h"
 #include "sa_conv_device.h"
 #include "sa_host.h"
 
 namespace sa {
 namespace {
-
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 __device__ inline f32x4 mfma(Vec8<__bf16>::type a, Vec8<__bf16>::type b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
@@ -33,75 +27,6 @@ __device__ inline f32x16 mfma(Vec8<__bf16>::type a, Vec8<__bf16>::type b, f32x16
 }
 __device__ inline f32x16 mfma(Vec8<_Float16>::type a, Vec8<_Float16>::type b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
-}
-
-// What the outputs' sums are joined with, loaded ahead of them.
-template <typename T, int V>
-struct Addends {
-    typedef T vec __attribute__((ext_vector_type(V)));
-    float bias[V], bias2[V];  // if the epilogue has them
-    vec r;                    // if has_r (whole vectors of the operands' type only)
-    bool has_r;
-
-    __device__ void load_bias(const Epilogue &e, int64_t n, int cnt) {
-        if (e.bias) {
-            if (cnt == V) load_vec<float, V>(e.bias + n, bias);
-            else load_part<float, V>(e.bias + n, cnt, bias);
-        }
-        if (e.bias2) {
-            if (cnt == V) load_vec<float, V>(e.bias2 + n, bias2);
-            else load_part<float, V>(e.bias2 + n, cnt, bias2);
-        }
-    }
-};
-
-// V (cnt < V at a row's end) consecutive outputs from their sums z (and u).
-template <typename T, bool GATED, int V>
-__device__ inline void finish(const Epilogue &e, void *Y, int64_t m, int64_t n, int cnt, float (&z)[V], float (&u)[V],
-                              const Addends<T, V> &with) {
-    auto put = [&](auto *p, const float (&v)[V]) {
-        using E = typename std::remove_reference<decltype(*p)>::type;
-        if (cnt == V) store_vec<E, V>(p, v);
-        else store_part<E, V>(p, cnt, v);
-    };
-    auto add = [&](const auto *p) {
-        using E = typename std::remove_cv<typename std::remove_reference<decltype(*p)>::type>::type;
-        float t[V];
-        if (cnt == V) load_vec<E, V>(p, t);
-        else load_part<E, V>(p, cnt, t);
-#pragma unroll
-        for (int i = 0; i < V; ++i) z[i] += t[i];
-    };
-    if (e.bias)
-#pragma unroll
-        for (int i = 0; i < V; ++i) z[i] += with.bias[i];
-    if (e.Z) put(reinterpret_cast<T *>(e.Z) + m * e.ldz + n, z);
-    if (e.act != SA_ACT_NONE) activate<false, V>(e.act, z, z, z);
-    if constexpr (GATED) {
-        if (e.bias2)
-#pragma unroll
-            for (int i = 0; i < V; ++i) u[i] += with.bias2[i];
-        if (e.Z2) put(reinterpret_cast<T *>(e.Z2) + m * e.ldz + n, u);
-#pragma unroll
-        for (int i = 0; i < V; ++i) z[i] *= u[i];
-    }
-    if (with.has_r)
-#pragma unroll
-        for (int i = 0; i < V; ++i) z[i] += (float)with.r[i];
-    else if (e.R) {
-        if (e.out_f32) add(reinterpret_cast<const float *>(e.R) + m * e.ldr + n);
-        else add(reinterpret_cast<const T *>(e.R) + m * e.ldr + n);
-    }
-    if (e.out_f32) put(reinterpret_cast<float *>(Y) + m * e.ldy + n, z);
-    else put(reinterpret_cast<T *>(Y) + m * e.ldy + n, z);
-}
-
-template <typename T, bool GATED, int V>
-__device__ inline void finish(const Epilogue &e, void *Y, int64_t m, int64_t n, int cnt, float (&z)[V], float (&u)[V]) {
-    Addends<T, V> with;
-    with.has_r = false;
-    with.load_bias(e, n, cnt);
-    finish<T, GATED, V>(e, Y, m, n, cnt, z, u, with);
 }
 
 // Where binary32 partial sums of a product go when k is split over workgroups:
@@ -265,36 +190,7 @@ __global__ __launch_bounds__(512) void k_rows(Gemm g, Partial q) {
 // former.  A third stage in flight gained nothing in the largest tile (its loads land in
 // time) and nothing further in the smallest.
 
-typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-
-constexpr int kMaxLds = 160 * 1024;
-
-__device__ inline int uni(int x) { return __builtin_amdgcn_readfirstlane(x); }
-
-// a raw buffer of `bytes` at base, both wavefront-uniform
-__device__ inline i32x4 buffer_at(uint64_t base, uint32_t bytes) {
-    return i32x4{uni((int)(uint32_t)base), uni((int)((uint32_t)(base >> 32) & 0xffffu)), uni((int)bytes), kRsrcWord3};
-}
-
-// 16 bytes per lane straight from memory to LDS: lane i's land at lds + AT + 16 * i.
-// Inline asm: after the compiler's own LDS-DMA builtin every LDS read waits for
-// all loads in flight.  The statement has no outputs; the waits are wait_vm().
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-template <int AT>
-__device__ inline void dma16(i32x4 r, uint32_t voff, uint32_t soff, uint32_t lds) {
-    asm volatile("s_add_u32 m0, %0, %4\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(voff),
-                 "s"(r), "s"(soff), "n"(AT)
-                 : "memory", "scc", "m0");
-}
-#pragma clang diagnostic pop
-template <int N>
-__device__ inline void wait_vm() {
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-}
-// this wavefront's LDS accesses done, then the workgroup's barrier
-__device__ inline void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // One operand's part of a stage: B rows by BK k, NW wavefronts.
 template <typename T, bool ACROSS, int B, int BK, int NW, int MI>
@@ -444,24 +340,6 @@ struct TileCfg {
     static constexpr int lds = S * stage;
     static_assert(lds <= kMaxLds, "LDS");
 };
-
-// f(j) with j, below N, as a constant: registers cannot be indexed
-template <int N, typename F>
-__device__ inline void pick(int j, F &&f) {
-    if constexpr (N > 0) {
-        if (j == N - 1) f(std::integral_constant<int, N - 1>{});
-        else pick<N - 1>(j, f);
-    }
-}
-
-// f(0), .. f(N - 1) with constants
-template <int N, int I = 0, typename F>
-__device__ inline void each(F &&f) {
-    if constexpr (I < N) {
-        f(std::integral_constant<int, I>{});
-        each<N, I + 1>(f);
-    }
-}
 
 struct TileArgs {
     Gemm g;
@@ -834,33 +712,6 @@ __global__ __launch_bounds__(256) void k_align_rows(Copies a) {
 }
 
 // ---------------------------------------------------------------- host side
-// Workgroups of `kern` (nt threads, lds bytes) that the GPU holds at once; raises
-// the kernel's LDS limit on the first call per device.
-int resident(const void *kern, int nt, int lds, int *groups) try {
-    static std::mutex mu;
-    static std::map<std::pair<const void *, int>, int> known;
-    int dev = 0;
-    if (int rc = check_hip(hipGetDevice(&dev), "matrix product: current device")) return rc;
-    std::lock_guard<std::mutex> lock(mu);
-    const auto it = known.find({kern, dev});
-    if (it != known.end()) {
-        *groups = it->second;
-        return SA_OK;
-    }
-    if (int rc = check_hip(hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds), "matrix product: LDS"))
-        return rc;
-    int per_cu = 0, cus = 0;
-    if (int rc = check_hip(hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, kern, nt, lds), "matrix product: occupancy"))
-        return rc;
-    if (int rc = check_hip(hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev), "matrix product: CU count"))
-        return rc;
-    *groups = std::max(1, per_cu) * std::max(1, cus);
-    known[{kern, dev}] = *groups;
-    return SA_OK;
-} catch (const std::exception &) {  // no exception leaves a C entry
-    return fail(SA_E_HIP, "matrix product: out of host memory");
-}
-
 // How a product runs: k_rows with 16, 32 or 64 rows of M per workgroup (kRows64x2: 32
 // rows of the N side instead of 16), or k_gemm with tiles of 128 x 64, 128 x 128 or
 // 256 x 256 (N side by M side).

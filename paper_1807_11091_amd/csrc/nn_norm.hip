@@ -1,13 +1,15 @@
-// Layer norm over the rows of a matrix and its gradient.
+// Layer norm and root-mean-square norm over the rows of a matrix, and their gradients.
 //
 //   forward   mean = sum x / n, rstd = (sum (x - mean)^2 / n + eps)^-1/2,
 //             y = (x - mean) rstd gamma + beta
 //   backward  with xn = (x - mean) rstd and t = dy gamma:
 //             dx = rstd (t - sum t / n - xn sum(t xn) / n) + dr,
 //             dgamma = sum over rows of dy xn, dbeta = sum over rows of dy
+//   RMS       s = x + r, rstd = (sum s^2 / n + eps)^-1/2, y = s rstd gamma, also in 8 bits;
+//             with xn = s rstd: dx = rstd (t - xn sum(t xn) / n) + dr, dgamma as above
 //
-// Both are bound by HBM: the forward pass reads x and writes y, the backward pass
-// reads dy, x (and dr) and writes dx, each once.
+// All are bound by HBM: the forward passes read x (and r) and write y (and s), the backward
+// passes read dy, x (and dr) and write dx, each once.
 //
 // TPR threads hold one row in registers (CH vectors of 8 elements each), so the
 // row is read once and the variance is summed over x - mean, not as a difference
@@ -20,6 +22,7 @@
 #include <type_traits>
 
 #include "nn_columns.h"
+#include "nn_quant.h"
 #include "nn_types.h"
 #include "sa_host.h"
 
@@ -272,6 +275,120 @@ __global__ __launch_bounds__(1024) void k_ln_fwd_long(FwdArgs a) {
     }
 }
 
+struct RmsArgs {
+    int64_t rows, ldx, ldr, lds, ldy;
+    int cols;
+    float eps;
+    const void *X, *R;
+    const float *gamma;
+    void *S, *Y;
+    sa_matrix8 Q;
+    float *rstd;
+};
+
+// Eight columns of a row from c on, of which n are inside it, to Y and Q.  All sixteen
+// threads of a block call it.
+template <typename T>
+__device__ inline void rms_results(const RmsArgs &a, int64_t row, int c, const float (&y)[kV]) {
+    const int n = min(a.cols - c, kV);
+    if (a.Y && n > 0) store_chunk<T>(reinterpret_cast<T *>(a.Y) + row * a.ldy, c, a.cols, y);
+    if (a.Q.codes)
+        quantise_row(y, n, a.Q.codes + row * a.Q.ld + c, a.Q.scales + row * a.Q.scale_row + c / kBlock * a.Q.scale_col);
+}
+
+// x + r to nearest in their type, which is what S holds and the norm is of
+template <typename T>
+__device__ inline float rms_sum(float x, float r) {
+    return (float)(T)(x + r);
+}
+
+template <typename T, int TPR, int CH, bool SHORT>
+__global__ __launch_bounds__(Rows<TPR>::threads) void k_rms_fwd(RmsArgs a) {
+    constexpr int NT = Rows<TPR>::threads, RPB = Rows<TPR>::per_group;
+    __shared__ float2 tmp[2][NT / 64];
+    const int t = threadIdx.x % TPR;
+    const int64_t row = (int64_t)blockIdx.x * RPB + __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
+    const bool in = row < a.rows;  // threads of a row past the last one only keep the barriers
+    const T *x = reinterpret_cast<const T *>(a.X) + (in ? row : 0) * a.ldx;
+    Raw<T> raw[CH], res[CH];
+    float v[CH][kV];
+    float s = 0.0f, none = 0.0f;
+#pragma unroll
+    for (int k = 0; k < CH; ++k) raw[k].template load<SHORT>(x, (k * TPR + t) * kV, a.cols);
+    if (a.R) {
+        const T *r = reinterpret_cast<const T *>(a.R) + (in ? row : 0) * a.ldr;
+#pragma unroll
+        for (int k = 0; k < CH; ++k) res[k].template load<SHORT>(r, (k * TPR + t) * kV, a.cols);
+    }
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+        const int c = (k * TPR + t) * kV;
+        raw[k].template place<SHORT>(c, a.cols, a.cols);
+        if (a.R) res[k].template place<SHORT>(c, a.cols, a.cols);
+#pragma unroll
+        for (int i = 0; i < kV; ++i) {
+            v[k][i] = a.R ? rms_sum<T>(raw[k][i], res[k][i]) : raw[k][i];
+            s = fmaf(v[k][i], v[k][i], s);
+        }
+        if (a.S && in && c < a.cols) store_chunk<T>(reinterpret_cast<T *>(a.S) + row * a.lds, c, a.cols, v[k]);
+    }
+    row_sums<TPR, NT>(s, none, tmp, 0);
+    if (!in) return;
+    const float rstd = 1.0f / sqrtf(s / (float)a.cols + a.eps);
+    if (t == 0 && a.rstd) a.rstd[row] = rstd;
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+        const int c = (k * TPR + t) * kV;
+        float g[kV];
+        load_param(a.gamma, c, a.cols, 1.0f, g);
+#pragma unroll
+        for (int i = 0; i < kV; ++i) g[i] *= v[k][i] * rstd;
+        rms_results<T>(a, row, c, g);
+    }
+}
+
+// Rows longer than the registers hold: the row is read twice.  S may stand where X or R
+// does, so where it is written the second read is of S.
+template <typename T>
+__global__ __launch_bounds__(1024) void k_rms_fwd_long(RmsArgs a) {
+    constexpr int NT = 1024;
+    __shared__ float2 tmp[2][NT / 64];
+    const int64_t row = blockIdx.x;
+    const T *x = reinterpret_cast<const T *>(a.X) + row * a.ldx;
+    const T *r = reinterpret_cast<const T *>(a.R) + row * a.ldr;
+    T *sum = reinterpret_cast<T *>(a.S) + row * a.lds;
+    auto load_sum = [&](int c, float (&v)[kV]) {
+        load_chunk<T>(x, c, a.cols, v);
+        if (!a.R) return;
+        float o[kV];
+        load_chunk<T>(r, c, a.cols, o);
+#pragma unroll
+        for (int i = 0; i < kV; ++i) v[i] = rms_sum<T>(v[i], o[i]);
+    };
+    float s = 0.0f, none = 0.0f, v[kV];
+    for (int c = threadIdx.x * kV; c < a.cols; c += NT * kV) {
+        load_sum(c, v);
+#pragma unroll
+        for (int i = 0; i < kV; ++i) s = fmaf(v[i], v[i], s);
+        if (a.S) store_chunk<T>(sum, c, a.cols, v);
+    }
+    row_sums<NT, NT>(s, none, tmp, 0);
+    const float rstd = 1.0f / sqrtf(s / (float)a.cols + a.eps);
+    if (threadIdx.x == 0 && a.rstd) a.rstd[row] = rstd;
+    for (int base = 0; base < a.cols; base += NT * kV) {
+        const int c = base + threadIdx.x * kV;
+        float g[kV] = {};
+        if (c < a.cols) {
+            if (a.S) load_chunk<T>(sum, c, a.cols, v);  // what this thread wrote
+            else load_sum(c, v);
+            load_param(a.gamma, c, a.cols, 1.0f, g);
+#pragma unroll
+            for (int i = 0; i < kV; ++i) g[i] = c + i < a.cols ? g[i] * (v[i] * rstd) : 0.0f;
+        }
+        rms_results<T>(a, row, c, g);
+    }
+}
+
 struct BwdArgs {
     int64_t rows, lddy, ldx, lddr, lddx;
     int cols;
@@ -289,7 +406,8 @@ struct BwdArgs {
 // from one set to the other would wait for them.  Bound by memory: 16384 x 4096
 // bfloat16 in 104 us with the joining of the sums, 5.2 TB/s over x, dy, dr and dx (209 us
 // without the next row, 134 us when copies waited for it).
-template <typename T, int TPR, int CH, bool SHORT>
+// RMS: the root-mean-square norm's gradient, without means and dbeta.
+template <typename T, int TPR, int CH, bool SHORT, bool RMS>
 __global__ __launch_bounds__((Rows<TPR, sizeof(T) == 2>::threads), (Rows<TPR, sizeof(T) == 2>::threads > 512 ? 3 : 2)) void k_ln_bwd(BwdArgs a) {
     constexpr int NT = Rows<TPR, sizeof(T) == 2>::threads, RPB = Rows<TPR, sizeof(T) == 2>::per_group;
     constexpr bool kAhead = CH <= 2;  // more would not fit the registers
@@ -319,7 +437,7 @@ __global__ __launch_bounds__((Rows<TPR, sizeof(T) == 2>::threads), (Rows<TPR, si
             w.x[k].template load<SHORT>(x, c, a.cols);
             w.y[k].template load<SHORT>(dy, c, a.cols);
         }
-        w.mean = a.mean[row];
+        w.mean = RMS ? 0.0f : a.mean[row];
         w.rstd = a.rstd[row];
     };
     // Works on the row in w while next is read, after this row's dR.
@@ -344,8 +462,8 @@ __global__ __launch_bounds__((Rows<TPR, sizeof(T) == 2>::threads), (Rows<TPR, si
                 const float dy = w.y[k][i], d = dy * gamma[k][i];
                 const float xn = c + i < end ? (w.x[k][i] - w.mean) * w.rstd : 0.0f;
                 sg[k][i] = fmaf(dy, xn, sg[k][i]);
-                sb[k][i] += dy;
-                s1 += d;
+                if (!RMS) sb[k][i] += dy;
+                if (!RMS) s1 += d;
                 s2 = fmaf(d, xn, s2);
             }
         }
@@ -395,7 +513,7 @@ __global__ __launch_bounds__((Rows<TPR, sizeof(T) == 2>::threads), (Rows<TPR, si
     if (!a.part) return;
     float *pg = a.part + (int64_t)blockIdx.x * 2 * a.cols;
 #pragma unroll
-    for (int half = 0; half < 2; ++half)
+    for (int half = 0; half < (RMS ? 1 : 2); ++half)
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
             float v[kV];
@@ -418,7 +536,7 @@ __global__ __launch_bounds__((Rows<TPR, sizeof(T) == 2>::threads), (Rows<TPR, si
 }
 
 // Rows longer than the registers hold: dX in three reads of the row.
-template <typename T>
+template <typename T, bool RMS>
 __global__ __launch_bounds__(1024) void k_ln_bwd_long(BwdArgs a) {
     constexpr int NT = 1024;
     __shared__ float2 tmp[2][NT / 64];
@@ -428,7 +546,7 @@ __global__ __launch_bounds__(1024) void k_ln_bwd_long(BwdArgs a) {
     const T *dy = reinterpret_cast<const T *>(a.dY) + row * a.lddy;
     const T *dr = a.dR ? reinterpret_cast<const T *>(a.dR) + row * a.lddr : nullptr;
     T *dx = reinterpret_cast<T *>(a.dX) + row * a.lddx;
-    const float mean = a.mean[row], rstd = a.rstd[row];
+    const float mean = RMS ? 0.0f : a.mean[row], rstd = a.rstd[row];
     float s1 = 0.0f, s2 = 0.0f, v[kV], d[kV], g[kV], r[kV];
     for (int c = threadIdx.x * kV; c < a.cols; c += NT * kV) {
         load_chunk<T>(x, c, a.cols, v);
@@ -437,7 +555,7 @@ __global__ __launch_bounds__(1024) void k_ln_bwd_long(BwdArgs a) {
 #pragma unroll
         for (int i = 0; i < kV; ++i) {
             const float xn = c + i < a.cols ? (v[i] - mean) * rstd : 0.0f;
-            s1 += d[i] * g[i];
+            if (!RMS) s1 += d[i] * g[i];
             s2 = fmaf(d[i] * g[i], xn, s2);
         }
     }
@@ -458,7 +576,7 @@ __global__ __launch_bounds__(1024) void k_ln_bwd_long(BwdArgs a) {
 }
 
 // Their column sums: workgroup (x, y) takes 64 columns and every gridDim.y-th row.
-template <typename T>
+template <typename T, bool RMS>
 __global__ __launch_bounds__(64) void k_ln_params_long(BwdArgs a) {
     const int c = blockIdx.x * 64 + threadIdx.x;
     if (c >= a.cols) return;
@@ -466,12 +584,12 @@ __global__ __launch_bounds__(64) void k_ln_params_long(BwdArgs a) {
     for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
         const float x = (float)reinterpret_cast<const T *>(a.X)[row * a.ldx + c];
         const float dy = (float)reinterpret_cast<const T *>(a.dY)[row * a.lddy + c];
-        g = fmaf(dy, (x - a.mean[row]) * a.rstd[row], g);
+        g = fmaf(dy, (RMS ? x : x - a.mean[row]) * a.rstd[row], g);
         b += dy;
     }
     float *p = a.part + (int64_t)blockIdx.y * 2 * a.cols;
     p[c] = g;
-    p[a.cols + c] = b;
+    if (!RMS) p[a.cols + c] = b;
 }
 
 constexpr int kMaxRegCols = 512 * 4 * kV;  // the longest row held in registers
@@ -521,6 +639,20 @@ FwdArgs rows_from(FwdArgs a, int64_t at, int64_t n) {
     return a;
 }
 template <typename T>
+RmsArgs rows_from(RmsArgs a, int64_t at, int64_t n) {
+    a.rows = n;
+    skip_rows<T>(a.X, at, a.ldx);
+    skip_rows<T>(a.R, at, a.ldr);
+    skip_rows<T>(a.S, at, a.lds);
+    skip_rows<T>(a.Y, at, a.ldy);
+    skip_rows<float>(a.rstd, at, 1);
+    if (a.Q.codes) {
+        a.Q.codes += at * a.Q.ld;
+        a.Q.scales += at * a.Q.scale_row;
+    }
+    return a;
+}
+template <typename T>
 BwdArgs rows_from(BwdArgs a, int64_t at, int64_t n) {
     a.rows = n;
     skip_rows<T>(a.dY, at, a.lddy);
@@ -548,13 +680,28 @@ struct LaunchFwd {
 };
 
 template <typename T>
+struct LaunchRms {
+    const RmsArgs &a;
+    hipStream_t stream;
+    int rc;
+    template <int TPR, int CH, bool SHORT>
+    void operator()() {
+        rc = by_rows("k_rms_fwd", a.rows, TPR, [&](int64_t at, int64_t n) {
+            constexpr int RPB = Rows<TPR>::per_group;
+            hipLaunchKernelGGL((k_rms_fwd<T, TPR, CH, SHORT>), dim3((unsigned)((n + RPB - 1) / RPB)), dim3(Rows<TPR>::threads), 0,
+                               stream, rows_from<T>(a, at, n));
+        });
+    }
+};
+
+template <typename T, bool RMS>
 struct LaunchBwd {
     const BwdArgs &a;
     int groups;
     hipStream_t stream;
     template <int TPR, int CH, bool SHORT>
     void operator()() {
-        hipLaunchKernelGGL((k_ln_bwd<T, TPR, CH, SHORT>), dim3(groups), dim3(Rows<TPR, sizeof(T) == 2>::threads), 0, stream, a);
+        hipLaunchKernelGGL((k_ln_bwd<T, TPR, CH, SHORT, RMS>), dim3(groups), dim3(Rows<TPR, sizeof(T) == 2>::threads), 0, stream, a);
     }
 };
 
@@ -591,19 +738,45 @@ int fwd(const FwdArgs &a, hipStream_t stream) {
 }
 
 template <typename T>
+int rms(const RmsArgs &a, hipStream_t stream) {
+    if (a.cols <= kMaxRegCols) {
+        LaunchRms<T> launch{a, stream, SA_OK};
+        by_width(a.cols, launch);
+        return launch.rc;
+    }
+    return by_rows("k_rms_fwd_long", a.rows, 1024, [&](int64_t at, int64_t n) {
+        hipLaunchKernelGGL(k_rms_fwd_long<T>, dim3((unsigned)n), dim3(1024), 0, stream, rows_from<T>(a, at, n));
+    });
+}
+
+template <typename T, bool RMS>
 int bwd(const BwdArgs &a, int groups, hipStream_t stream) {
     if (a.cols <= kMaxRegCols) {
-        by_width(a.cols, LaunchBwd<T>{a, groups, stream});
+        by_width(a.cols, LaunchBwd<T, RMS>{a, groups, stream});
         return check_hip(hipGetLastError(), "k_ln_bwd");
     }
     if (a.part) {  // first: dX may overwrite dY
-        hipLaunchKernelGGL(k_ln_params_long<T>, dim3((a.cols + 63) / 64, groups), dim3(64), 0, stream, a);
+        hipLaunchKernelGGL((k_ln_params_long<T, RMS>), dim3((a.cols + 63) / 64, groups), dim3(64), 0, stream, a);
         if (int rc = check_hip(hipGetLastError(), "k_ln_params_long")) return rc;
     }
     if (!a.dX) return SA_OK;
     return by_rows("k_ln_bwd_long", a.rows, 1024, [&](int64_t at, int64_t n) {
-        hipLaunchKernelGGL(k_ln_bwd_long<T>, dim3((unsigned)n), dim3(1024), 0, stream, rows_from<T>(a, at, n));
+        hipLaunchKernelGGL((k_ln_bwd_long<T, RMS>), dim3((unsigned)n), dim3(1024), 0, stream, rows_from<T>(a, at, n));
     });
+}
+
+// The gradient of either norm; dbeta is the layer norm's.
+template <bool RMS>
+int norm_bwd(const BwdArgs &a, int type, float *dgamma, float *dbeta, hipStream_t stream) {
+    const int groups = bwd_groups(a.rows, a.cols, type);
+    if (groups > 0) {
+        int rc;
+        if (type == SA_BF16) rc = bwd<__bf16, RMS>(a, groups, stream);
+        else if (type == SA_F16) rc = bwd<_Float16, RMS>(a, groups, stream);
+        else rc = bwd<float, RMS>(a, groups, stream);
+        if (rc) return rc;
+    }
+    return dgamma || dbeta ? join_columns(a.part, groups, a.cols, dgamma, dbeta, stream) : SA_OK;
 }
 
 }  // namespace
@@ -642,17 +815,42 @@ extern "C" int structadmm_layer_norm_bwd(const sa_layer_norm_bwd_desc *desc, hip
     if (int rc = validate_layer_norm_bwd(d)) return rc;
     const size_t need = ln_bwd_bytes(d);
     if (int rc = check_workspace("layer_norm_bwd", d.ws, d.ws_bytes, need)) return rc;
-    const int groups = bwd_groups(d.rows, d.cols, d.type);
-    BwdArgs a{d.rows, d.lddy, d.ldx, d.lddr, d.lddx, (int)d.cols, d.dY, d.X, d.mean, d.rstd, d.gamma, d.dR, d.dX,
-              d.dgamma || d.dbeta ? static_cast<float *>(d.ws) : nullptr};
-    if (groups > 0) {
-        int rc;
-        if (d.type == SA_BF16) rc = bwd<__bf16>(a, groups, stream);
-        else if (d.type == SA_F16) rc = bwd<_Float16>(a, groups, stream);
-        else rc = bwd<float>(a, groups, stream);
-        if (rc) return rc;
-    }
-    if (d.dgamma || d.dbeta)
-        return join_columns(static_cast<const float *>(d.ws), groups, (int)d.cols, d.dgamma, d.dbeta, stream);
-    return SA_OK;
+    const BwdArgs a{d.rows, d.lddy, d.ldx, d.lddr, d.lddx, (int)d.cols, d.dY, d.X, d.mean, d.rstd, d.gamma, d.dR, d.dX,
+                    d.dgamma || d.dbeta ? static_cast<float *>(d.ws) : nullptr};
+    return norm_bwd<false>(a, d.type, d.dgamma, d.dbeta, stream);
+}
+
+extern "C" int structadmm_rms_norm_fwd(const sa_rms_norm_desc *desc, hipStream_t stream) {
+    clear_error();
+    if (!desc) return fail(SA_E_ARG, "rms_norm_fwd: desc is required");
+    const sa_rms_norm_desc &d = *desc;
+    if (int rc = validate_rms_norm(d)) return rc;
+    if (d.rows == 0) return SA_OK;
+    const RmsArgs a{d.rows, d.ldx, d.ldr, d.lds, d.ldy, (int)d.cols, d.eps, d.X, d.R, d.gamma, d.S, d.Y, d.Q, d.rstd};
+    if (d.type == SA_BF16) return rms<__bf16>(a, stream);
+    if (d.type == SA_F16) return rms<_Float16>(a, stream);
+    return rms<float>(a, stream);
+}
+
+static size_t rms_bwd_bytes(const sa_rms_norm_bwd_desc &d) {
+    return d.dgamma ? (size_t)bwd_groups(d.rows, d.cols, d.type) * 2 * d.cols * sizeof(float) : 0;
+}
+
+extern "C" size_t structadmm_rms_norm_bwd_workspace(const sa_rms_norm_bwd_desc *desc) {
+    if (!desc || validate_rms_norm_bwd_sizes(*desc) != SA_OK) return 0;
+    sa_rms_norm_bwd_desc d = *desc;
+    float any;
+    if (!d.dY && d.rows > 0) d.dgamma = &any;  // before the buffers: as for every output
+    return rms_bwd_bytes(d);
+}
+
+extern "C" int structadmm_rms_norm_bwd(const sa_rms_norm_bwd_desc *desc, hipStream_t stream) {
+    clear_error();
+    if (!desc) return fail(SA_E_ARG, "rms_norm_bwd: desc is required");
+    const sa_rms_norm_bwd_desc &d = *desc;
+    if (int rc = validate_rms_norm_bwd(d)) return rc;
+    if (int rc = check_workspace("rms_norm_bwd", d.ws, d.ws_bytes, rms_bwd_bytes(d))) return rc;
+    const BwdArgs a{d.rows, d.lddy, d.lds, d.lddr, d.lddx, (int)d.cols, d.dY, d.S, nullptr, d.rstd, d.gamma, d.dR, d.dX,
+                    d.dgamma ? static_cast<float *>(d.ws) : nullptr};
+    return norm_bwd<true>(a, d.type, d.dgamma, nullptr, stream);
 }

@@ -326,6 +326,123 @@ int check_norm_bwd(const sa_layer_norm_bwd_desc &d, bool ptrs) {
     return check_alias(w, "dX and dR with another pitch", d.dX, d.dR, d.lddx == d.lddr);
 }
 
+int64_t blocks_of(int64_t n) { return (n + SA_BLOCK - 1) / SA_BLOCK; }
+
+// An 8-bit matrix of blocks of block_rows rows.  `out`: its scales must not share memory.
+int check_matrix8(const char *who, const char *name, const sa_matrix8 &q, bool required, int64_t rows, int64_t cols,
+                  int64_t block_rows, bool out, bool pointers) {
+    if (!q.codes && !required) return SA_OK;  // left out
+    if (q.ld < cols || q.ld > SA_MAX_LD)
+        return fail(q.ld < cols ? SA_E_ARG : SA_E_UNSUPPORTED, "%s: the pitch %lld of %s must be in [%lld, %d]", who,
+                    (long long)q.ld, name, (long long)cols, SA_MAX_LD);
+    if (q.ld % 16) return fail(SA_E_ALIGN, "%s: the pitch %lld of %s must be a multiple of 16", who, (long long)q.ld, name);
+    const int64_t nr = block_rows == 1 ? rows : blocks_of(rows), nc = blocks_of(cols);
+    if (q.scale_row < 0 || q.scale_col < 0)
+        return fail(SA_E_ARG, "%s: the strides of %s's scales must not be negative", who, name);
+    if (q.scale_row > SA_MAX_LD || q.scale_col > kMaxElems)
+        return fail(SA_E_UNSUPPORTED, "%s: the strides %lld and %lld of %s's scales must be at most %d and 2^31 - 1", who,
+                    (long long)q.scale_row, (long long)q.scale_col, name, SA_MAX_LD);
+    if (out) {  // rows of block columns or the other way round
+        const int64_t r = nr > 1 ? q.scale_row : 1, c = nc > 1 ? q.scale_col : 1;
+        const bool by_row = nc <= 1 || (c >= 1 && (nr <= 1 || r >= c * (nc - 1) + 1));
+        const bool by_col = nr <= 1 || (r >= 1 && (nc <= 1 || c >= r * (nr - 1) + 1));
+        if (r < 1 || c < 1 || !(by_row || by_col))
+            return fail(SA_E_ARG, "%s: the strides of %s's scales let blocks share one", who, name);
+    }
+    if (pointers && rows > 0 && cols > 0 && (!q.codes || !q.scales))
+        return fail(SA_E_ARG, "%s: %s is required, codes and scales", who, name);
+    if (!aligned(q.codes, 16)) return fail(SA_E_ALIGN, "%s: the codes of %s must be 16-byte aligned", who, name);
+    if (!aligned(q.scales, 4)) return fail(SA_E_ALIGN, "%s: the scales of %s must be 4-byte aligned", who, name);
+    return SA_OK;
+}
+
+// an 8-bit output against an operand or another output
+int check_alias8(const char *who, const char *names, const sa_matrix8 &out, const void *in) {
+    SA_TRY(check_alias(who, names, out.codes, in));
+    return out.codes ? check_alias(who, names, out.scales, in) : SA_OK;
+}
+int check_alias8(const char *who, const char *names, const sa_matrix8 &out, const sa_matrix8 &in) {
+    SA_TRY(check_alias8(who, names, out, in.codes));
+    return in.codes ? check_alias8(who, names, out, in.scales) : SA_OK;
+}
+
+int check_rms_bwd(const sa_rms_norm_bwd_desc &d, bool ptrs) {
+    const char *w = "rms_norm_bwd";
+    SA_TRY(check_norm(w, d.rows, d.cols, d.type));
+    SA_TRY(check_matrix(w, "dY", d.dY, true, d.rows, d.cols, d.lddy, d.type, ptrs));
+    SA_TRY(check_matrix(w, "S", d.S, true, d.rows, d.cols, d.lds, d.type, ptrs));
+    SA_TRY(check_matrix(w, "dR", d.dR, false, d.rows, d.cols, d.lddr, d.type, ptrs));
+    SA_TRY(check_matrix(w, "dX", d.dX, false, d.rows, d.cols, d.lddx, d.type, ptrs));
+    SA_TRY(check_vector(w, "rstd", d.rstd));
+    SA_TRY(check_vector(w, "gamma", d.gamma));
+    SA_TRY(check_vector(w, "dgamma", d.dgamma));
+    if (!ptrs) return SA_OK;
+    if (d.rows > 0 && !d.rstd) return fail(SA_E_ARG, "%s: rstd is required", w);
+    if (!d.dX && !d.dgamma && d.rows > 0) return fail(SA_E_ARG, "%s: nothing to do (dX and dgamma are NULL)", w);
+    SA_TRY(check_alias(w, "dX and S", d.dX, d.S));
+    SA_TRY(check_alias(w, "dX and dY with another pitch", d.dX, d.dY, d.lddx == d.lddy));
+    return check_alias(w, "dX and dR with another pitch", d.dX, d.dR, d.lddx == d.lddr);
+}
+
+int check_linear8(const sa_linear8_desc &d, bool ptrs) {
+    const char *w = "linear8_fwd";
+    SA_TRY(check_product(w, d.M, d.N, d.K, d.type, d.out_type, d.act));
+    SA_TRY(check_matrix8(w, "X", d.X, true, d.M, d.K, 1, false, ptrs));
+    SA_TRY(check_matrix8(w, "W", d.W, true, d.N, d.K, SA_BLOCK, false, ptrs));
+    SA_TRY(check_matrix(w, "R", d.R, false, d.M, d.N, d.ldr, d.out_type, ptrs));
+    SA_TRY(check_matrix(w, "Y", d.Y, false, d.M, d.N, d.ldy, d.out_type, ptrs));
+    SA_TRY(check_matrix(w, "Z", d.Z, false, d.M, d.N, d.ldz, d.type, ptrs));
+    SA_TRY(check_matrix8(w, "Q", d.Q, false, d.M, d.N, 1, true, ptrs));
+    SA_TRY(check_vector(w, "bias", d.bias));
+    if (!ptrs) return SA_OK;
+    if (!d.Y && !d.Q.codes && d.M > 0 && d.N > 0) return fail(SA_E_ARG, "%s: Y or Q is required", w);
+    const void *in[] = {d.X.codes, d.X.scales, d.W.codes, d.W.scales};
+    for (const void *p : in) {
+        SA_TRY(check_alias(w, "Y and an operand", d.Y, p));
+        SA_TRY(check_alias(w, "Z and an operand", d.Z, p));
+        SA_TRY(check_alias8(w, "Q and an operand", d.Q, p));
+    }
+    SA_TRY(check_alias(w, "Y and R with another pitch", d.Y, d.R, d.ldy == d.ldr));
+    SA_TRY(check_alias(w, "Z and Y", d.Z, d.Y));
+    SA_TRY(check_alias(w, "Z and R", d.Z, d.R));
+    SA_TRY(check_alias8(w, "Q and Y", d.Q, d.Y));
+    SA_TRY(check_alias8(w, "Q and Z", d.Q, d.Z));
+    return check_alias8(w, "Q and R", d.Q, d.R);
+}
+
+int check_glu8(const sa_glu8_desc &d, bool ptrs) {
+    const char *w = "glu8_fwd";
+    SA_TRY(check_product(w, d.M, d.N, d.K, d.type, d.type, d.act));
+    SA_TRY(check_matrix8(w, "X", d.X, true, d.M, d.K, 1, false, ptrs));
+    SA_TRY(check_matrix8(w, "Wg", d.Wg, true, d.N, d.K, SA_BLOCK, false, ptrs));
+    SA_TRY(check_matrix8(w, "Wu", d.Wu, true, d.N, d.K, SA_BLOCK, false, ptrs));
+    if (d.N > 1 && d.Wg.ld != d.Wu.ld) return fail(SA_E_ARG, "%s: Wg and Wu must have one pitch", w);
+    if ((d.N > SA_BLOCK && d.Wg.scale_row != d.Wu.scale_row) || (d.K > SA_BLOCK && d.Wg.scale_col != d.Wu.scale_col))
+        return fail(SA_E_ARG, "%s: the scales of Wg and Wu must have the same strides", w);
+    SA_TRY(check_matrix(w, "H", d.H, false, d.M, d.N, d.ldh, d.type, ptrs));
+    SA_TRY(check_matrix(w, "G", d.G, false, d.M, d.N, d.ldgu, d.type, ptrs));
+    SA_TRY(check_matrix(w, "U", d.U, false, d.M, d.N, d.ldgu, d.type, ptrs));
+    SA_TRY(check_matrix8(w, "Q", d.Q, false, d.M, d.N, 1, true, ptrs));
+    SA_TRY(check_vector(w, "bg", d.bg));
+    SA_TRY(check_vector(w, "bu", d.bu));
+    if ((d.G == nullptr) != (d.U == nullptr)) return fail(SA_E_ARG, "%s: give both G and U or neither", w);
+    if (!ptrs) return SA_OK;
+    if (!d.H && !d.Q.codes && d.M > 0 && d.N > 0) return fail(SA_E_ARG, "%s: H or Q is required", w);
+    const void *in[] = {d.X.codes, d.X.scales, d.Wg.codes, d.Wg.scales, d.Wu.codes, d.Wu.scales};
+    for (const void *p : in) {
+        SA_TRY(check_alias(w, "H and an operand", d.H, p));
+        SA_TRY(check_alias(w, "G and an operand", d.G, p));
+        SA_TRY(check_alias(w, "U and an operand", d.U, p));
+        SA_TRY(check_alias8(w, "Q and an operand", d.Q, p));
+    }
+    SA_TRY(check_alias(w, "G and U", d.G, d.U));
+    SA_TRY(check_alias(w, "H and G", d.H, d.G));
+    SA_TRY(check_alias(w, "H and U", d.H, d.U));
+    SA_TRY(check_alias8(w, "Q and H", d.Q, d.H));
+    SA_TRY(check_alias8(w, "Q and G", d.Q, d.G));
+    return check_alias8(w, "Q and U", d.Q, d.U);
+}
+
 }  // namespace
 
 int validate_layer_norm(const sa_layer_norm_desc &d) {
@@ -351,6 +468,52 @@ int validate_glu_sizes(const sa_glu_desc &d) { return check_glu(d, false); }
 int validate_glu(const sa_glu_desc &d) { return check_glu(d, true); }
 int validate_glu_bwd_sizes(const sa_glu_bwd_desc &d) { return check_glu_bwd(d, false); }
 int validate_glu_bwd(const sa_glu_bwd_desc &d) { return check_glu_bwd(d, true); }
+int validate_rms_norm_bwd_sizes(const sa_rms_norm_bwd_desc &d) { return check_rms_bwd(d, false); }
+int validate_rms_norm_bwd(const sa_rms_norm_bwd_desc &d) { return check_rms_bwd(d, true); }
+int validate_linear8_sizes(const sa_linear8_desc &d) { return check_linear8(d, false); }
+int validate_linear8(const sa_linear8_desc &d) { return check_linear8(d, true); }
+int validate_glu8_sizes(const sa_glu8_desc &d) { return check_glu8(d, false); }
+int validate_glu8(const sa_glu8_desc &d) { return check_glu8(d, true); }
+
+int validate_rms_norm(const sa_rms_norm_desc &d) {
+    const char *w = "rms_norm_fwd";
+    SA_TRY(check_norm(w, d.rows, d.cols, d.type));
+    if (!(d.eps >= 0.0f)) return fail(SA_E_ARG, "%s: eps must be at least 0", w);
+    SA_TRY(check_matrix(w, "X", d.X, true, d.rows, d.cols, d.ldx, d.type, true));
+    SA_TRY(check_matrix(w, "R", d.R, false, d.rows, d.cols, d.ldr, d.type, true));
+    SA_TRY(check_matrix(w, "S", d.S, false, d.rows, d.cols, d.lds, d.type, true));
+    SA_TRY(check_matrix(w, "Y", d.Y, false, d.rows, d.cols, d.ldy, d.type, true));
+    SA_TRY(check_matrix8(w, "Q", d.Q, false, d.rows, d.cols, 1, true, true));
+    SA_TRY(check_vector(w, "gamma", d.gamma));
+    SA_TRY(check_vector(w, "rstd", d.rstd));
+    if (!d.S && !d.Y && !d.Q.codes && d.rows > 0) return fail(SA_E_ARG, "%s: nothing to do (S, Y and Q are NULL)", w);
+    SA_TRY(check_alias(w, "S and X with another pitch", d.S, d.X, d.lds == d.ldx));
+    SA_TRY(check_alias(w, "S and R with another pitch", d.S, d.R, d.lds == d.ldr));
+    SA_TRY(check_alias(w, "Y and X with another pitch", d.Y, d.X, d.ldy == d.ldx));
+    SA_TRY(check_alias(w, "Y and R with another pitch", d.Y, d.R, d.ldy == d.ldr));
+    SA_TRY(check_alias(w, "Y and S", d.Y, d.S));
+    const void *other[] = {d.X, d.R, d.S, d.Y};
+    for (const void *p : other) SA_TRY(check_alias8(w, "Q and another matrix", d.Q, p));
+    return SA_OK;
+}
+
+int validate_quantize8(const sa_quantize8_desc &d) {
+    const char *w = "quantize8";
+    if (d.rows < 0 || d.rows > kMaxElems || d.cols < 0)
+        return fail(SA_E_ARG, "%s: rows=%lld must be in [0, 2^31) and cols=%lld at least 0", w, (long long)d.rows,
+                    (long long)d.cols);
+    if (d.type != SA_BF16 && d.type != SA_F16 && d.type != SA_F32) return fail(SA_E_ARG, "%s: unknown type %d", w, d.type);
+    if (d.block_rows != 1 && d.block_rows != SA_BLOCK)
+        return fail(SA_E_ARG, "%s: block_rows=%d must be 1 or %d", w, d.block_rows, SA_BLOCK);
+    SA_TRY(check_matrix(w, "X", d.X, true, d.rows, d.cols, d.ldx, d.type, true));
+    SA_TRY(check_matrix8(w, "Q", d.Q, false, d.rows, d.cols, d.block_rows, true, true));
+    SA_TRY(check_matrix8(w, "QT", d.QT, false, d.cols, d.rows, d.block_rows, true, true));
+    if (!d.Q.codes && !d.QT.codes && d.rows > 0 && d.cols > 0)
+        return fail(SA_E_ARG, "%s: nothing to do (Q and QT are NULL)", w);
+    SA_TRY(check_alias8(w, "Q and X", d.Q, d.X));
+    SA_TRY(check_alias8(w, "QT and X", d.QT, d.X));
+    return check_alias8(w, "Q and QT", d.Q, d.QT);
+}
 
 #undef SA_TRY
 

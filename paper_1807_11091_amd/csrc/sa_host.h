@@ -48,6 +48,14 @@ int validate_glu_sizes(const sa_glu_desc &d);
 int validate_glu(const sa_glu_desc &d);
 int validate_glu_bwd_sizes(const sa_glu_bwd_desc &d);
 int validate_glu_bwd(const sa_glu_bwd_desc &d);
+int validate_rms_norm(const sa_rms_norm_desc &d);
+int validate_rms_norm_bwd_sizes(const sa_rms_norm_bwd_desc &d);
+int validate_rms_norm_bwd(const sa_rms_norm_bwd_desc &d);
+int validate_quantize8(const sa_quantize8_desc &d);
+int validate_linear8_sizes(const sa_linear8_desc &d);
+int validate_linear8(const sa_linear8_desc &d);
+int validate_glu8_sizes(const sa_glu8_desc &d);
+int validate_glu8(const sa_glu8_desc &d);
 // ws holds `need` bytes and is 256-byte aligned (when need > 0)
 int check_workspace(const char *who, const void *ws, size_t have, size_t need);
 

@@ -1,0 +1,265 @@
+"""GPU parity of the 8-bit feed-forward operators against the binary64 reference.
+
+Quantisation is compared bit for bit with its stated rule; results of norms and products
+within the bounds of nn8_reference (binary32 sums, then one rounding to the result's type:
+u |y| with u = 2^-8 bfloat16, 2^-11 binary16, 2^-24 binary32).
+"""
+import math
+
+import pytest
+
+import nn8_reference as ref8
+import paper_1807_11091_amd as sa
+from gpu_helpers import DEV, torch
+from test_parity_nn import E, LN_SIZES, PITCHES, TYPES, check, gen, matrix, out_matrix, padding_untouched, rounded, vec
+
+pytestmark = pytest.mark.gpu
+
+T = torch()
+
+
+def out8(rows, cols, block=1, layout="columns"):
+    """An 8-bit output inside buffers of sentinels: codes 0x7e, scales -1."""
+    ld = (cols + 15) // 16 * 16 + (16 if layout == "rows" else 0)
+    buf = T.full((rows * ld + 32,), 0x7e, dtype=T.uint8, device=DEV)
+    codes = buf[16:16 + rows * ld].view(rows, ld)[:, :cols].view(T.float8_e4m3fn)
+    nr, nc = rows if block == 1 else ref8.blocks(rows), ref8.blocks(cols)
+    if layout == "rows":
+        sb = T.full((nr, nc + 3), -1.0, device=DEV)
+        scales = sb[:, :nc]
+    else:
+        sb = T.full((nc, nr + 5), -1.0, device=DEV)
+        scales = sb[:, :nr].t()
+    return sa.Matrix8(codes, scales), (buf, sb)
+
+
+def untouched8(m, bufs):
+    """Nothing outside the codes and scales was written, and every scale was."""
+    buf, sb = bufs
+    inside = (m.codes.view(T.uint8) == 0x7e).sum().item()
+    codes = (buf == 0x7e).sum().item() - inside == buf.numel() - m.codes.numel()
+    return codes and (sb == -1.0).sum().item() == sb.numel() - m.scales.numel() and bool((m.scales > 0).all())
+
+
+def same_bits(a, b):
+    nan = a.float().isnan()
+    return T.equal(nan, b.float().isnan()) and T.equal(a.view(T.uint8)[~nan], b.view(T.uint8)[~nan])
+
+
+def operand(g, rows, cols, block, scale=1.0, layout="columns"):
+    """An 8-bit operand whose padding holds NaN codes."""
+    m, (buf, _) = out8(rows, cols, block, layout)
+    buf.fill_(0x7f)
+    q, s = ref8.quantise(T.randn(rows, cols, generator=g, device=DEV) * scale, block)
+    m.codes.view(T.uint8).copy_(q.view(T.uint8))
+    m.scales.copy_(s)
+    return m
+
+
+# ------------------------------------------------------------- quantisation
+Q_SIZES = [(1, 1), (1, 127), (2, 128), (17, 129), (16, 300), (127, 64), (128, 128), (129, 130), (300, 77), (5, 2458),
+           (257, 1000), (1000, 24), (3, 16500)]
+
+
+@pytest.mark.parametrize("rows,cols", Q_SIZES)
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("block", [1, 128])
+def test_quantize8(rows, cols, dtype, block):
+    g = gen(rows + 31 * cols)
+    X, _ = matrix(g, rows, cols, TYPES[dtype], PITCHES[(rows + cols) % 3], 2.0)
+    X.mul_(T.exp(T.randn(rows, 1, generator=g, device=DEV)).to(X.dtype))
+    X[rows // 2].zero_()  # a row without a value
+    for layout in ("columns", "rows"):
+        Q, bq = out8(rows, cols, block, layout)
+        QT, bt = out8(cols, rows, block, layout)
+        sa.quantize8(X, block, Q=Q, QT=QT, out="")
+        for m, v, b in ((Q, X, bq), (QT, X.t(), bt)):
+            q, s = ref8.quantise(v, block)
+            assert T.equal(m.scales, s) and same_bits(m.codes, q)
+            assert untouched8(m, b)
+    only, none = sa.quantize8(X, block)
+    assert none is None and same_bits(only.codes, Q.codes) and T.equal(only.scales, Q.scales)
+    none, only = sa.quantize8(X, block, out="t")
+    assert none is None and same_bits(only.codes, QT.codes) and T.equal(only.scales, QT.scales)
+    # independently of the rule's binary32 steps: a scale that uses the range, codes within half a step
+    v, w = X.double(), ref8.wide(Q.scales, rows, cols, block)
+    top = ref8.amax(v, block)
+    assert ((Q.scales.double() * 448 - top).abs() <= 2 * E * top + 448 * 2.0 ** -126).all()
+    assert ((Q.codes.double() * w - v).abs() <= 2.0 ** -4 * (1 + 4 * E) * v.abs() + 2.0 ** -10 * w).all()
+
+
+@pytest.mark.parametrize("block", [1, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_quantize8_special_values(block, dtype):
+    g = gen(5)
+    X, _ = matrix(g, 200, 300, TYPES[dtype], "packed")
+    nan, inf = float("nan"), float("inf")
+    X[3, 5], X[4, 130:260], X[7, 299], X[140, 2], X[141, 131], X[190, 290] = nan, nan, inf, -inf, 1e-39, 3e38
+    X[9].fill_(1e-38)
+    X[10, :128].fill_(-2.0 ** -133)
+    X[11].fill_(nan)
+    Q, QT = sa.quantize8(X, block, out="qt")
+    for m, v in ((Q, X), (QT, X.t())):
+        q, s = ref8.quantise(v, block)
+        assert T.equal(m.scales, s) and same_bits(m.codes, q)
+    if block == 1:
+        assert Q.scales[7, 2] == inf and Q.codes.float()[7, 299].isnan() and (Q.codes.float()[7, 256:299] == 0).all()
+        assert Q.codes.float()[3, 5].isnan() and not Q.codes.float()[3, 6:].isnan().any()
+        assert (Q.scales[11] == 2.0 ** -126).all() and Q.codes.float()[11].isnan().all()
+
+
+def test_quantize8_empty():
+    X = T.zeros(0, 40, dtype=T.bfloat16, device=DEV)
+    Q, QT = sa.quantize8(X, out="qt")
+    assert Q.codes.shape == (0, 40) and QT.codes.shape == (40, 0) and QT.scales.shape == (40, 0)
+    Q, _ = sa.quantize8(X.t())
+    assert Q.scales.shape == (40, 0)
+
+
+# ------------------------------------------------------------------ the norm
+@pytest.mark.parametrize("rows,cols", LN_SIZES)
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("pitch", PITCHES)
+def test_rms_norm(rows, cols, dtype, pitch):
+    dt, g, eps = TYPES[dtype], gen(rows * 5 + cols), 1e-5
+    X, _ = matrix(g, rows, cols, dt, pitch, 2.0)
+    R = matrix(g, rows, cols, dt, pitch)[0] if (rows + cols) % 2 else None
+    gamma = None if (rows + cols) % 3 == 0 else vec(g, cols, 0.2, 1.0)
+    S, sbuf = out_matrix(rows, cols, dt, pitch)
+    Y, ybuf = out_matrix(rows, cols, dt, pitch)
+    Q, qbufs = out8(rows, cols, 1, "rows" if rows % 2 else "columns")
+    rstd = T.full((rows,), -1.0, device=DEV)
+    got = sa.rms_norm_fwd(X, gamma, R=R, eps=eps, S=S, Y=Y, Q=Q, rstd=rstd, out="")
+    assert got[0] is Y and got[1] is S and got[2] is rstd and got[3] is Q
+    s = X if R is None else (X.float() + R.float()).to(dt)
+    assert T.equal(S, s)
+    d = lambda t: None if t is None else t.double()
+    y, r = ref8.rms_fwd(s.double(), d(gamma), eps)
+    er = (cols + 16) * E  # a sum of cols squares, half of its error in the root
+    check(rstd, r, er * r, "rstd")
+    tol = (er + 8 * E) * y.abs()
+    check(Y, y, tol + rounded(y, dt), "Y")
+    ref8.check_codes(Q, y, tol, "Q")
+    assert padding_untouched(S, sbuf) and padding_untouched(Y, ybuf) and untouched8(Q, qbufs)
+    # each output by itself, and in the places of the inputs
+    alone = sa.rms_norm_fwd(X, gamma, R=R, eps=eps, out="q")
+    assert alone[:3] == (None, None, None)
+    assert same_bits(alone[3].codes, Q.codes) and T.equal(alone[3].scales, Q.scales)
+    x2, r2 = X.clone(), None if R is None else R.clone()
+    sa.rms_norm_fwd(x2, gamma, R=r2, eps=eps, S=r2, Y=x2, out="")
+    assert T.equal(x2, Y) and (R is None or T.equal(r2, S))
+    x2, r2 = X.clone(), None if R is None else R.clone()
+    sa.rms_norm_fwd(x2, gamma, R=r2, eps=eps, S=x2, Y=r2, out="r")
+    assert T.equal(x2, S) and (R is None or T.equal(r2, Y))
+
+    dY, _ = matrix(g, rows, cols, dt, pitch)
+    dR = matrix(g, rows, cols, dt, pitch)[0] if cols % 2 else None
+    dX, buf = out_matrix(rows, cols, dt, pitch)
+    dg = T.full((cols,), 7.0, device=DEV)
+    sa.rms_norm_bwd(dY, S, rstd, gamma, dR=dR, dX=dX, dgamma=dg)
+    dy, r = dY.double(), rstd.double()
+    rx, rg = ref8.rms_bwd(dy, s.double(), r, d(gamma), d(dR))
+    xn = (s.double() * r[:, None]).abs()
+    t = dy.abs() * (1.0 if gamma is None else gamma.double().abs())
+    tol = r[:, None] * (t * 8 * E + xn * (t * xn).mean(1, keepdim=True) * (cols + 16) * E)
+    a = 0.0 if dR is None else dR.double().abs()
+    check(dX, rx, tol * 1.01 + 4 * E * a + rounded(rx, dt), "dX")
+    assert padding_untouched(dX, buf)
+    check(dg, rg, (rows + 16) * E * (dy.abs() * xn).sum(0) + 1e-30, "dgamma")
+    only = sa.rms_norm_bwd(dY, S, rstd, gamma, dR=dR, params=False)
+    assert only[1] is None and T.equal(only[0], dX)
+    over = dY.clone()  # dX in dY's place
+    assert T.equal(sa.rms_norm_bwd(over, S, rstd, gamma, dR=dR, dX=over)[1], dg) and T.equal(over, dX)
+
+
+def test_rms_norm_gradient_against_differences():
+    """Central differences of a scalar of the binary32 operator's own outputs."""
+    g = gen(3)
+    X, R, w = (T.randn(3, 37, generator=g, device=DEV) for _ in range(3))
+    gamma = vec(g, 37, 0.2, 1.0)
+    f = lambda x, p: (sa.rms_norm_fwd(x, p, R=R)[0].double() * w.double()).sum().item()
+    _, S, rstd, _ = sa.rms_norm_fwd(X, gamma, R=R)
+    dX, dg = sa.rms_norm_bwd(w, S, rstd, gamma)
+    h = 2.0 ** -7  # the third derivatives' part h^2 / 6, the results' rounding / h
+    for i, j in ((0, 0), (1, 20), (2, 36)):
+        x1, x2, p1, p2 = X.clone(), X.clone(), gamma.clone(), gamma.clone()
+        x1[i, j] += h
+        x2[i, j] -= h
+        p1[j] += h
+        p2[j] -= h
+        bound = 8 * h * h + 37 * 3 * 8 * E / h
+        assert abs((f(x1, gamma) - f(x2, gamma)) / (2 * h) - dX[i, j].item()) <= bound
+        assert abs((f(X, p1) - f(X, p2)) / (2 * h) - dg[j].item()) <= bound
+
+
+def test_rms_norm_no_rows():
+    none = T.zeros(0, 50, dtype=T.float16, device=DEV)
+    Y, S, rstd, Q = sa.rms_norm_fwd(none, R=none, out="ysrq")
+    assert Y.shape == S.shape == Q.codes.shape == (0, 50) and rstd.shape == (0,)
+    dX, dg = sa.rms_norm_bwd(none, none, rstd)
+    assert dX.shape == (0, 50) and (dg == 0).all()
+
+
+# --------------------------------------------------------------- the products
+M_SIZES = [(1, 1, 1), (1, 16, 128), (2, 17, 15), (1, 300, 1000), (5, 64, 129), (16, 129, 640), (17, 200, 257), (33, 128, 2500),
+           (64, 130, 511), (65, 384, 128), (100, 77, 1229), (128, 256, 256), (129, 257, 384), (200, 1000, 600),
+           (257, 129, 130), (300, 520, 1100), (700, 640, 96), (513, 1025, 2050), (1, 4096, 4096), (40, 2458, 1024)]
+ACTS = ["none", "relu", "sigmoid", "silu", "gelu", "gelu_tanh"]
+
+
+def check_out(Y, y, tol, dt, buf, what):
+    check(Y, y, tol + rounded(y, dt), what)
+    assert padding_untouched(Y, buf)
+
+
+@pytest.mark.parametrize("M,N,K", M_SIZES)
+@pytest.mark.parametrize("out", ["same", "f32", "q", "both"])
+def test_linear8(M, N, K, out):
+    i = M + N + K + len(out)
+    g, dt, act, pitch = gen(i), (T.bfloat16, T.float16)[i % 2], ACTS[i % 6], PITCHES[i % 3]
+    X = operand(g, M, K, 1, 1.0, ("columns", "rows")[i % 2])
+    W = operand(g, N, K, 128, 2 / math.sqrt(K), ("rows", "columns")[i % 2])
+    bias = vec(g, N) if i % 3 else None
+    to = T.float32 if out == "f32" else dt
+    R = matrix(g, M, N, to, pitch)[0] if i % 4 < 2 else None
+    Z, zbuf = out_matrix(M, N, dt, pitch) if i % 5 < 2 else (None, None)
+    Y, ybuf = out_matrix(M, N, to, pitch) if out != "q" else (None, None)
+    Q, qbufs = out8(M, N) if out in ("q", "both") else (None, None)
+    got = sa.linear8_fwd(X, W, bias, R=R, act=sa.ACTS[act], Y=Y, Z=Z, Q=Q, out="")
+    assert got[0] is Y and got[1] is Q
+    y, ty, z, tz = ref8.linear8(X, W, bias, R, act)
+    if Y is not None:
+        check_out(Y, y, ty, to, ybuf, "Y")
+    if Z is not None:
+        check_out(Z, z, tz, dt, zbuf, "Z")
+    if Q is not None:
+        ref8.check_codes(Q, y, ty, "Q")
+        assert untouched8(Q, qbufs)
+    if R is not None and Y is not None:  # Y in R's place
+        sa.linear8_fwd(X, W, bias, R=R, act=sa.ACTS[act], Y=R, out="")
+        assert T.equal(R, Y)
+
+
+@pytest.mark.parametrize("M,N,K", M_SIZES)
+@pytest.mark.parametrize("out", ["h", "q", "all"])
+def test_glu8(M, N, K, out):
+    i = M + N + K + len(out)
+    g, dt, act, pitch = gen(i), (T.float16, T.bfloat16)[i % 2], ACTS[i % 6], PITCHES[i % 3]
+    layout = ("columns", "rows")[i % 2]
+    X = operand(g, M, K, 1, 1.0, layout)
+    Wg, Wu = operand(g, N, K, 128, 2 / math.sqrt(K), layout), operand(g, N, K, 128, 2 / math.sqrt(K), layout)
+    bg, bu = (vec(g, N) if i % 3 else None), (vec(g, N) if i % 4 else None)
+    H, hbuf = out_matrix(M, N, dt, pitch) if out != "q" else (None, None)
+    G, gbuf = out_matrix(M, N, dt, pitch) if out == "all" else (None, None)
+    U, ubuf = out_matrix(M, N, dt, pitch) if out == "all" else (None, None)
+    Q, qbufs = out8(M, N, 1, layout) if out != "h" else (None, None)
+    sa.glu8_fwd(X, Wg, Wu, bg, bu, act=sa.ACTS[act], H=H, Q=Q, G=G, U=U, out="")
+    h, th, gg, tg, u, tu = ref8.glu8(X, Wg, Wu, bg, bu, act)
+    if H is not None:
+        check_out(H, h, th, dt, hbuf, "H")
+    if G is not None:
+        check_out(G, gg, tg, dt, gbuf, "G")
+        check_out(U, u, tu, dt, ubuf, "U")
+    if Q is not None:
+        ref8.check_codes(Q, h, th, "Q")
+        assert untouched8(Q, qbufs)
