@@ -195,13 +195,456 @@ __global__ __launch_bounds__(512) void k_rows8(Gemm8 g, Partial8 q) {
     }
 }
 
+// ------------------------------------------------------------ tiled product
+// k_tile8: BN x BM outputs (N side by M side) per workgroup of WN x WM wavefronts, a block
+// of 128 k a stage.  Stages go through a ring of two LDS buffers, written by buffer_load ..
+// lds: the codes, 128 bytes a row, the 16-byte chunks of a row XOR-swizzled so that the rows
+// of a fragment read hit distinct banks (the swizzle is applied to the source address); for
+// each wavefront the scales of its rows of X, and of its block row of W.  The weights are
+// the row operand of the matrix instructions, so a lane's four sums are consecutive in n and
+// share one scale.
+//
+// Workgroups are persistent and their loads run over the stages of all their tiles.
+template <bool GATED, int BN, int BM, int WN, int WM>
+struct TileCfg8 {
+    static constexpr int NW = WN * WM, NT = NW * 64;
+    static constexpr int TN = BN / WN / 16, TM = BM / WM / 16;  // fragments of a wavefront
+    static constexpr int scales_at = (BN + BM) * kBlock;
+    static constexpr int scales = GATED ? 768 : 512;            // bytes a wavefront: X's, W's (64 places each, 1 used)
+    static constexpr int stage = scales_at + NW * scales;
+    static constexpr int join_at = 2 * stage;                   // largest values of the results' rows
+    static constexpr int lds = join_at + WN * BM * 4;
+    static_assert(lds <= kMaxLds, "LDS");
+};
+
+struct TileArgs8 {
+    Gemm8 g;
+    Partial8 part;
+    int mtiles, ntiles, tiles, groups;  // tiles: of all parts of k; groups: workgroups
+};
+
+// One operand's part of a stage: B rows of 128 codes, NW wavefronts.
+template <int B, int NW>
+struct Side8 {
+    static constexpr int bytes = B * kBlock;
+    static constexpr int loads = bytes / 1024 / NW;  // per wavefront
+    static_assert(bytes % (1024 * NW) == 0, "whole loads per wavefront");
+
+    __device__ static int swz(int r) { return (r >> 1) & 7; }
+
+    uint32_t off[loads];  // byte offset of each load from the tile's origin
+    int kc;               // first k of this lane's chunks: the loads lie 8 rows apart or a multiple
+
+    __device__ void setup(int64_t ld, int wave, int lane) {
+#pragma unroll
+        for (int i = 0; i < loads; ++i) {
+            const int at = (i * NW + wave) * 64 + lane, row = at >> 3;
+            const int chunk = (at & 7) ^ swz(row);
+            off[i] = (uint32_t)row * (uint32_t)ld + chunk * 16u;
+            if (i == 0) kc = chunk * 16;
+        }
+        static_assert(NW % 2 == 0 || loads == 1, "one chunk per lane");
+    }
+
+    // Where the next stage's loads read.  Rows past the matrix and k past K read as 0; a
+    // chunk that K cuts is completed by mend().  The range is rounded up to whole chunks:
+    // the bytes past the matrix's end lie in the aligned 16 bytes that hold its last code.
+    struct Cursor {
+        i32x4 rs;
+        uint32_t so;
+    };
+    // at k0 of the rows at p (the tile's first row; `rows` of them in the matrix)
+    __device__ static Cursor open(const uint8_t *p, int64_t ld, int rows, int K, int k0) {
+        const uint32_t range = ((uint32_t)(min(rows, B) - 1) * (uint32_t)ld + (uint32_t)K + 15u) & ~15u;
+        return Cursor{buffer_at(reinterpret_cast<uint64_t>(p), range), (uint32_t)uni(k0)};
+    }
+    __device__ static void advance(Cursor &c) { c.so = uni(c.so + kBlock); }
+    // Lanes whose chunk begins at `k` or past it read zeros from here on (offsets are below
+    // 2^31, one with the top bit set lies past every range).
+    __device__ void limit(int k) {
+#pragma unroll
+        for (int i = 0; i < loads; ++i) off[i] = kc < k ? off[i] & ~kInvalidOffset : off[i] | kInvalidOffset;
+    }
+    template <int I>
+    __device__ void load(const Cursor &c, uint32_t lds) const {
+        dma16<I * NW * 1024>(c.rs, off[I], c.so, lds);
+    }
+
+    // The chunk that holds k = K - 1, in LDS: its codes past K become 0 (after this
+    // wavefront's loads have landed); n: k of K's last stage.
+    __device__ void mend(uint8_t *lds, int n, int wave, int lane) const {
+        if (kc != (n & ~15)) return;
+#pragma unroll
+        for (int i = 0; i < loads; ++i) {
+            i32x4 *q = reinterpret_cast<i32x4 *>(lds + (i * NW + wave) * 1024 + lane * 16);
+            i32x4 v = *q;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int have = (n & 15) - e * 4;
+                if (have < 4) v[e] = have <= 0 ? 0 : v[e] & ((1 << have * 8) - 1);
+            }
+            *q = v;
+        }
+    }
+};
+
+// A lane's 32 codes of a fragment of 16 rows from row0 on: chunks lane / 16 and 4 + lane / 16.
+struct Reads8 {
+    uint32_t fo[2];
+    __device__ explicit Reads8(int lane) {
+        const int r = lane & 15;
+#pragma unroll
+        for (int q = 0; q < 2; ++q) fo[q] = r * kBlock + (((q * 4 + (lane >> 4)) ^ (r >> 1)) & 7) * 16;
+    }
+    __device__ i32x8 operator()(const uint8_t *lds, int row0) const {
+        union {
+            i32x4 h[2];
+            i32x8 v;
+        } x;
+#pragma unroll
+        for (int q = 0; q < 2; ++q) x.h[q] = *reinterpret_cast<const i32x4 *>(lds + fo[q] + row0 * kBlock);
+        return x.v;
+    }
+};
+
+// A fragment's codes as the matrix instructions take them.
+struct Wide {
+    Vec8<__bf16>::type k[4];
+    __device__ explicit Wide(i32x8 v) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) k[q] = widen(v[2 * q], v[2 * q + 1]);
+    }
+    Wide() = default;
+};
+
+template <typename T, bool GATED, int BN, int BM, int WN, int WM>
+__global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8 a) {
+    using Cfg = TileCfg8<GATED, BN, BM, WN, WM>;
+    constexpr int NW = Cfg::NW, TN = Cfg::TN, TM = Cfg::TM, TNG = GATED ? TN / 2 : TN, H = GATED ? 2 : 1;
+    constexpr int NROWS = GATED ? BN / 2 : BN;  // n of a tile; gated: one half of the N side per projection
+    using NSide = Side8<NROWS, NW>;
+    using MSide = Side8<BM, NW>;
+    constexpr int NL = NSide::loads * H, L = NL + MSide::loads + 1 + H;  // loads of a stage
+    constexpr int WROWS = NROWS / WN, MROWS = BM / WM;               // n and m of a wavefront
+    static_assert(128 % WROWS == 0 && MROWS <= 64 && TNG % 2 == 0 && TN >= 4, "shape");
+    constexpr int JOIN = TN - 2;                // the row of fragments at which the next stage is waited for
+    constexpr int RATE = (L + 1) / 2;           // loads that go out with each of the last two rows
+    extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+
+    const Gemm8 &g = a.g;
+    const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
+    const int wn = wave % WN, wm = wave / WN;
+    const int nrow = wn * WROWS, mrow = wm * MROWS;
+
+    // Workgroup b runs on XCD b mod 8, which walks one contiguous range of tiles (its own
+    // L2); its workgroups take the range's tiles in turn.
+    const int xcd = blockIdx.x & 7, local = blockIdx.x >> 3;
+    const int per = a.tiles >> 3, extra = a.tiles & 7;
+    const int first = uni(xcd * per + min(xcd, extra) + local);
+    const int end = uni((xcd + 1) * per + min(xcd + 1, extra));
+    const int stride = uni((a.groups >> 3) + (xcd < (a.groups & 7) ? 1 : 0));
+    if (first >= end) return;
+    const int mine = (end - first + stride - 1) / stride;  // tiles of this workgroup
+
+    const int K = uni((int)g.K), ns = (K + kBlock - 1) / kBlock;  // stages of a tile
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)smem;
+    const int64_t nld = g.w[0].ld, mld = g.x.ld;
+
+    // A tile: bands of 8 M tiles, down each band first, so that neighbours share operands
+    struct Tile {
+        int64_t m0, n0;
+        int chunk;
+        int s0, s1;  // its stages
+    };
+    auto tile_at = [&](int i) {
+        int t = first + i * stride;
+        const int one = a.mtiles * a.ntiles;
+        Tile q;
+        q.chunk = t / one;
+        t -= q.chunk * one;
+        q.s0 = uni((int)((int64_t)ns * q.chunk / a.part.split));
+        q.s1 = uni((int)((int64_t)ns * (q.chunk + 1) / a.part.split));
+        const int band = t / (8 * a.ntiles), in = t - band * 8 * a.ntiles;
+        const int h = min(8, a.mtiles - band * 8);
+        q.m0 = (int64_t)(band * 8 + in % h) * BM;
+        q.n0 = (int64_t)(in / h) * NROWS;
+        return q;
+    };
+
+    NSide nside;
+    MSide mside;
+    nside.setup(nld, wave, lane);
+    mside.setup(mld, wave, lane);
+    const Reads8 read(lane);
+
+    // The loads run over the stages of all tiles without a break, two stages ahead of the
+    // products.  A run of stages below K differs from stage to stage by one addition per
+    // operand; what else there is to work out is done between runs.
+    typename NSide::Cursor nc, nc1;
+    typename MSide::Cursor mc;
+    i32x4 xs, ws[H];  // the scales' buffers
+    const uint32_t xoff = lane < MROWS ? (uint32_t)lane * (uint32_t)g.x.scale_row * 4u : kInvalidOffset;
+    const uint32_t woff = lane == 0 ? 0u : kInvalidOffset;
+    uint32_t lat = lds0 + wave * 1024, slat = lds0 + Cfg::scales_at + wave * Cfg::scales;
+    int run = 0, lstage = 0, lend = 0, ltile = -1, lslot = 0;
+    int cuts = 0;  // slots that hold, or will, a chunk which K cuts
+    auto next_run = [&]() {
+        if (lstage == lend) ++ltile;
+        if (ltile >= mine) {  // past the last stage: the loads write zeros that are not used
+            nc.rs[2] = nc1.rs[2] = mc.rs[2] = xs[2] = ws[0][2] = ws[H - 1][2] = 0;
+            nc.so = nc1.so = mc.so = 0;
+            run = 1;
+            return;
+        }
+        const Tile q = tile_at(ltile);
+        if (lstage == lend) {
+            lstage = q.s0;
+            lend = q.s1;
+        }
+        const int nrows = uni((int)min(g.N - q.n0, (int64_t)NROWS)), mrows = uni((int)min(g.M - q.m0, (int64_t)BM));
+        const int k0 = lstage * kBlock;
+        nc = NSide::open(g.w[0].codes + q.n0 * nld, nld, nrows, K, k0);
+        if constexpr (GATED) nc1 = NSide::open(g.w[1].codes + q.n0 * nld, nld, nrows, K, k0);
+        mc = MSide::open(g.x.codes + q.m0 * mld, mld, mrows, K, k0);
+        nside.limit(K - k0);
+        mside.limit(K - k0);
+        const int64_t m = q.m0 + mrow;
+        const int have = uni((int)min(g.M - m, (int64_t)MROWS));
+        xs = buffer_at(reinterpret_cast<uint64_t>(g.x.scales + m * g.x.scale_row + lstage * g.x.scale_col),
+                       have > 0 ? ((uint32_t)(have - 1) * (uint32_t)g.x.scale_row + 1u) * 4u : 0u);
+        const int64_t n = q.n0 + nrow;
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+            ws[h] = buffer_at(reinterpret_cast<uint64_t>(g.w[h].scales + n / kBlock * g.w[h].scale_row + lstage * g.w[h].scale_col),
+                              n < g.N ? 4u : 0u);
+        if (kBlock > K - k0 && (K & 15) != 0) cuts |= 1 << lslot;
+        run = uni(kBlock <= K - k0 ? min(K / kBlock - lstage, lend - lstage) : 1);
+        lstage += run;
+    };
+    // The stage that is loaded next: begin, its loads 0 .. L - 1, end.
+    auto begin_stage = [&]() {
+        if (run == 0) next_run();
+        --run;
+    };
+    auto load = [&](auto which) {
+        constexpr int i = decltype(which)::value;
+        if constexpr (i < NSide::loads) nside.template load<i>(nc, lat);
+        else if constexpr (i < NL) nside.template load<i - NSide::loads>(nc1, lat + NSide::bytes);
+        else if constexpr (i < NL + MSide::loads) mside.template load<i - NL>(mc, lat + BN * kBlock);
+        else if constexpr (i == NL + MSide::loads) dma4<0>(xs, xoff, 0, slat);
+        else if constexpr (i < L) dma4<256 * (i - NL - MSide::loads)>(ws[i - NL - MSide::loads - 1], woff, 0, slat);
+    };
+    auto move = [](i32x4 &rs, uint64_t by) {
+        const uint64_t base = ((uint64_t)(uint32_t)rs[1] << 32 | (uint32_t)rs[0]) + by;
+        rs[0] = uni((int)(uint32_t)base);
+        rs[1] = uni((int)(uint32_t)(base >> 32));
+    };
+    auto end_stage = [&]() {
+        NSide::advance(nc);
+        if constexpr (GATED) NSide::advance(nc1);
+        MSide::advance(mc);
+        move(xs, (uint64_t)g.x.scale_col * 4);
+#pragma unroll
+        for (int h = 0; h < H; ++h) move(ws[h], (uint64_t)g.w[h].scale_col * 4);
+        lslot ^= 1;
+        lat = lds0 + wave * 1024 + lslot * Cfg::stage;
+        slat = lds0 + Cfg::scales_at + wave * Cfg::scales + lslot * Cfg::stage;
+    };
+    // zeros past K in the stage that has landed in `slot`
+    const int tail = K & (kBlock - 1);
+    auto mend = [&](int slot) {
+        if (uni(cuts >> slot & 1) == 0) return;
+        asm volatile("" ::: "memory");  // a branch of its own: nothing below is done without it
+        cuts &= ~(1 << slot);
+        uint8_t *at = smem + slot * Cfg::stage;
+        nside.mend(at, tail, wave, lane);
+        if constexpr (GATED) nside.mend(at + NSide::bytes, tail, wave, lane);
+        mside.mend(at + BN * kBlock, tail, wave, lane);
+    };
+
+    f32x4 acc[TN][TM];
+    int slot = 0;
+    if (ns > 0) {
+        begin_stage();
+        each<L>(load);
+        end_stage();
+        wait_vm<0>();
+        mend(0);
+        lds_barrier();
+        begin_stage();
+        each<L>(load);
+        end_stage();
+    }
+
+    // A stage is multiplied, a row of fragments at a time; the codes of X are widened once,
+    // those of a row of W two rows ahead.  When the last row's have been read, this stage's
+    // buffer is free and the next stage is waited for.
+    auto multiply = [&]() {
+        const uint8_t *cur = smem + slot * Cfg::stage;
+        slot ^= 1;
+        auto readn = [&](int i) {
+            if constexpr (GATED) return read(cur + (i >= TNG ? NSide::bytes : 0), nrow + i % TNG * 16);
+            else return read(cur, nrow + i * 16);
+        };
+        i32x8 raw[TM];
+#pragma unroll
+        for (int j = 0; j < TM; ++j) raw[j] = read(cur + BN * kBlock, mrow + j * 16);
+        i32x8 fa[2] = {readn(0), readn(1)};
+        float scale[H][TM];
+        {
+            const float *s = reinterpret_cast<const float *>(cur + Cfg::scales_at + wave * Cfg::scales);
+#pragma unroll
+            for (int h = 0; h < H; ++h)
+#pragma unroll
+                for (int j = 0; j < TM; ++j) scale[h][j] = s[j * 16 + (lane & 15)] * s[64 * (h + 1)];
+        }
+        Wide fb[TM];
+#pragma unroll
+        for (int j = 0; j < TM; ++j) fb[j] = Wide(raw[j]);
+#pragma unroll
+        for (int i = 0; i < TN; ++i) {
+            const Wide w(fa[i & 1]);
+            if (i + 2 < TN) fa[i & 1] = readn(i + 2);
+            f32x4 part[TM] = {};
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int j = 0; j < TM; ++j)
+                    part[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.k[q], fb[j].k[q], part[j], 0, 0, 0);
+#pragma unroll
+            for (int j = 0; j < TM; ++j) add_scaled(acc[i][j], part[j], scale[GATED && i >= TNG][j]);
+            if (i == JOIN) {
+                wait_vm<0>();
+                mend(slot);
+                lds_barrier();
+                begin_stage();
+            }
+            if (i >= JOIN)
+                pick<TN>(i, [&](auto ic) {
+                    constexpr int at = (decltype(ic)::value - JOIN) * RATE;
+                    if constexpr (at >= 0) each<RATE>([&](auto e) { load(std::integral_constant<int, at + decltype(e)::value>{}); });
+                });
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        end_stage();
+    };
+
+    const int nl = ((lane >> 4) & 1) * 16 + (lane >> 5) * 8;  // this lane's 8 n of two fragments, see below
+#pragma unroll 1
+    for (int ti = 0; ti < mine; ++ti) {
+        const Tile q = tile_at(ti);
+#pragma unroll
+        for (int i = 0; i < TN; ++i)
+#pragma unroll
+            for (int j = 0; j < TM; ++j) acc[i][j] = f32x4{};
+#pragma unroll 1
+        for (int s = q.s0; s < q.s1; ++s) multiply();
+
+        // Results straight from the registers.  A lane holds 4 consecutive n of every 16;
+        // exchanging the odd rows of 16 lanes of one such group with the even ones of the
+        // next leaves 8 consecutive n in each lane.
+        const bool eight = a.part.keep == 0 && g.q.codes;
+        float top[TM] = {};  // largest values of this lane's rows
+#pragma unroll 1
+        for (int f = 0; f < TNG / 2 * TM; ++f) {
+            f32x4 t[H][2];
+            pick<TNG / 2 * TM>(f, [&](auto fc) {
+                constexpr int i = decltype(fc)::value / TM * 2, j = decltype(fc)::value % TM;
+#pragma unroll
+                for (int h = 0; h < H; ++h) {
+                    t[h][0] = acc[h * TNG + i][j];
+                    t[h][1] = acc[h * TNG + i + 1][j];
+                }
+            });
+            float z[8], u[8];
+#pragma unroll
+            for (int h = 0; h < H; ++h)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const auto w = __builtin_amdgcn_permlane16_swap(__float_as_uint(t[h][0][e]), __float_as_uint(t[h][1][e]), false, false);
+                    (h ? u : z)[e] = __uint_as_float(w[0]);
+                    (h ? u : z)[e + 4] = __uint_as_float(w[1]);
+                }
+            const int64_t m = q.m0 + mrow + f % TM * 16 + (lane & 15), n = q.n0 + nrow + f / TM * 32 + nl;
+            const int cnt = m < g.M ? (int)max((int64_t)0, min((int64_t)8, g.N - n)) : 0;
+            if (cnt > 0) {
+                if (a.part.keep) {
+                    store_vec<float, 8>(partial_at(a.part, g, q.chunk, 0, m, n), z);
+                    if constexpr (GATED) store_vec<float, 8>(partial_at(a.part, g, q.chunk, 1, m, n), u);
+                } else {
+                    Addends<T, 8> with;
+                    with.has_r = false;
+                    with.load_bias(g.e, n, cnt);
+                    finish_values<T, GATED, 8>(g.e, m, n, cnt, z, u, with);
+                    if (g.e.Y) put_values<T, 8>(g.e, g.e.Y, m, n, cnt, z);
+                }
+            }
+            if (!eight) continue;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) z[e] = e < cnt ? z[e] : 0.0f;
+            const float most = largest(z);
+            pick<TNG / 2 * TM>(f, [&](auto fc) {
+                constexpr int i = decltype(fc)::value / TM * 2, j = decltype(fc)::value % TM;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    acc[i][j][e] = z[e];
+                    acc[i + 1][j][e] = z[e + 4];
+                }
+                top[j] = fmaxf(top[j], most);
+            });
+        }
+        if (!eight) continue;
+        // a row's block lies in one wavefront, or in some neighbours
+        float *all = reinterpret_cast<float *>(smem + Cfg::join_at);
+#pragma unroll
+        for (int j = 0; j < TM; ++j) {
+            top[j] = lanes_max<16, 64>(top[j]);
+            if (WROWS < kBlock && lane < 16) all[wn * BM + mrow + j * 16 + lane] = top[j];
+        }
+        if constexpr (WROWS < kBlock) {
+            constexpr int PER = kBlock / WROWS;  // wavefronts a block
+            lds_barrier();
+#pragma unroll
+            for (int j = 0; j < TM; ++j)
+#pragma unroll
+                for (int w = 1; w < PER; ++w)
+                    top[j] = fmaxf(top[j], all[(wn ^ w) * BM + mrow + j * 16 + (lane & 15)]);
+            lds_barrier();  // read before the next tile's are written
+        }
+        const int64_t nb = q.n0 + nrow;
+#pragma unroll
+        for (int j = 0; j < TM; ++j) {
+            const int64_t m = q.m0 + mrow + j * 16 + (lane & 15);
+            const float s = block_scale(top[j]), inv = 1.0f / s;
+            if (m >= g.M) continue;
+            if (nb % kBlock == 0 && lane < 16 && nb < g.N) g.q.scales[m * g.q.scale_row + nb / kBlock * g.q.scale_col] = s;
+#pragma unroll
+            for (int i = 0; i < TNG; i += 2) {
+                const int64_t n = nb + i * 16 + nl;
+                const int cnt = (int)min((int64_t)8, g.N - n);
+                if (cnt <= 0) continue;
+                float z[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) z[e] = acc[i + e / 4][j][e % 4];
+                store_codes(g.q.codes + m * g.q.ld + n, cnt, codes8(z, inv));
+            }
+        }
+    }
+    wait_vm<0>();  // the loads past the last stage still write to LDS
+}
+
 // ---------------------------------------------------------------- host side
+enum Path8 { kRows8, kTile8 };
 struct Plan8 {
+    Path8 path;
     int split;
     int keep;  // the epilogue runs in k_join8
 };
 
-Plan8 plan_of(const Gemm8 &g) { return Plan8{1, g.q.codes != nullptr}; }
+Plan8 plan_of(const Gemm8 &g) {
+    if (g.M <= 64) return Plan8{kRows8, 1, g.q.codes != nullptr};
+    return Plan8{kTile8, 1, 0};
+}
 
 size_t partial_bytes(const Gemm8 &g, const Plan8 &p) {
     return p.keep ? (size_t)p.split * (g.gated ? 2 : 1) * g.M * round_up(g.N, 8) * sizeof(float) : 0;
@@ -218,8 +661,27 @@ int join(const Gemm8 &g, const Partial8 &q, hipStream_t stream) {
     return SA_OK;
 }
 
+template <typename T, bool GATED, int BN, int BM, int WN, int WM>
+int launch_tiles(const Gemm8 &g, const Partial8 &q, hipStream_t stream) {
+    using Cfg = TileCfg8<GATED, BN, BM, WN, WM>;
+    auto kern = k_tile8<T, GATED, BN, BM, WN, WM>;
+    int groups = 0;
+    if (int rc = resident(reinterpret_cast<const void *>(kern), Cfg::NT, Cfg::lds, &groups)) return rc;
+    constexpr int rows = GATED ? BN / 2 : BN;
+    const int64_t mt = (g.M + BM - 1) / BM, nt = (g.N + rows - 1) / rows;
+    if (mt * nt * q.split >= (int64_t(1) << 30)) return fail(SA_E_UNSUPPORTED, "matrix product of 2^30 tiles or more");
+    TileArgs8 a{g, q, (int)mt, (int)nt, (int)(mt * nt) * q.split, 0};
+    a.groups = std::min(a.tiles, groups);
+    hipLaunchKernelGGL(kern, dim3(a.groups), dim3(Cfg::NT), Cfg::lds, stream, a);
+    return check_hip(hipGetLastError(), "k_tile8");
+}
+
 template <typename T, bool GATED>
 int run(const Gemm8 &g, const Plan8 &p, const Partial8 &q, hipStream_t stream) {
+    if (p.path == kTile8) {
+        if (int rc = launch_tiles<T, GATED, 256, 128, 4, 2>(g, q, stream)) return rc;
+        return q.keep ? join<T, GATED>(g, q, stream) : SA_OK;
+    }
     constexpr int NF = 1, MF = 4;
     hipLaunchKernelGGL((k_rows8<T, GATED, NF, MF, 1>), dim3((unsigned)((g.N + NF * 16 - 1) / (NF * 16)), q.split,
                        (unsigned)((g.M + MF * 16 - 1) / (MF * 16))), dim3(512), 0, stream, g, q);

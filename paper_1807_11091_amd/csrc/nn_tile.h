@@ -44,6 +44,13 @@ __device__ inline void dma16(i32x4 r, uint32_t voff, uint32_t soff, uint32_t lds
                  "s"(r), "s"(soff), "n"(AT)
                  : "memory", "scc", "m0");
 }
+// The same with 4 bytes per lane, at lds + AT + 4 * i.
+template <int AT>
+__device__ inline void dma4(i32x4 r, uint32_t voff, uint32_t soff, uint32_t lds) {
+    asm volatile("s_add_u32 m0, %0, %4\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(lds), "v"(voff),
+                 "s"(r), "s"(soff), "n"(AT)
+                 : "memory", "scc", "m0");
+}
 #pragma clang diagnostic pop
 template <int N>
 __device__ inline void wait_vm() {
