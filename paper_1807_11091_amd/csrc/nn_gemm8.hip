@@ -197,7 +197,7 @@ __global__ __launch_bounds__(512) void k_rows8(Gemm8 g, Partial8 q) {
 
 // ------------------------------------------------------------ tiled product
 // k_tile8: BN x BM outputs (N side by M side) per workgroup of WN x WM wavefronts, a block
-// of 128 k a stage.  Stages go through a ring of two LDS buffers, written by buffer_load ..
+// of 128 k a stage.  Stages go through a ring of S LDS buffers, written by buffer_load ..
 // lds: the codes, 128 bytes a row, the 16-byte chunks of a row XOR-swizzled so that the rows
 // of a fragment read hit distinct banks (the swizzle is applied to the source address); for
 // each wavefront the scales of its rows of X, and of its block row of W.  The weights are
@@ -205,14 +205,15 @@ __global__ __launch_bounds__(512) void k_rows8(Gemm8 g, Partial8 q) {
 // share one scale.
 //
 // Workgroups are persistent and their loads run over the stages of all their tiles.
-template <bool GATED, int BN, int BM, int WN, int WM>
+template <bool GATED, int BN, int BM, int WN, int WM, int S>
 struct TileCfg8 {
     static constexpr int NW = WN * WM, NT = NW * 64;
     static constexpr int TN = BN / WN / 16, TM = BM / WM / 16;  // fragments of a wavefront
     static constexpr int scales_at = (BN + BM) * kBlock;
-    static constexpr int scales = GATED ? 768 : 512;            // bytes a wavefront: X's, W's (64 places each, 1 used)
+    static constexpr int xl = (BM / WM + 63) / 64;              // loads of X's scales
+    static constexpr int scales = xl * 256 + 16;                // bytes a wavefront: X's, then W's
     static constexpr int stage = scales_at + NW * scales;
-    static constexpr int join_at = 2 * stage;                   // largest values of the results' rows
+    static constexpr int join_at = S * stage;                   // largest values of the results' rows
     static constexpr int lds = join_at + WN * BM * 4;
     static_assert(lds <= kMaxLds, "LDS");
 };
@@ -296,13 +297,16 @@ struct Reads8 {
 #pragma unroll
         for (int q = 0; q < 2; ++q) fo[q] = r * kBlock + (((q * 4 + (lane >> 4)) ^ (r >> 1)) & 7) * 16;
     }
+    __device__ i32x4 half(const uint8_t *lds, int row0, int q) const {
+        return *reinterpret_cast<const i32x4 *>(lds + fo[q] + row0 * kBlock);
+    }
     __device__ i32x8 operator()(const uint8_t *lds, int row0) const {
         union {
             i32x4 h[2];
             i32x8 v;
         } x;
 #pragma unroll
-        for (int q = 0; q < 2; ++q) x.h[q] = *reinterpret_cast<const i32x4 *>(lds + fo[q] + row0 * kBlock);
+        for (int q = 0; q < 2; ++q) x.h[q] = half(lds, row0, q);
         return x.v;
     }
 };
@@ -317,38 +321,48 @@ struct Wide {
     Wide() = default;
 };
 
-template <typename T, bool GATED, int BN, int BM, int WN, int WM>
-__global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8 a) {
-    using Cfg = TileCfg8<GATED, BN, BM, WN, WM>;
+template <typename T, bool GATED, int BN, int BM, int WN, int WM, int S>
+__global__ __launch_bounds__(WN *WM * 64, WN * WM / 4) void k_tile8(TileArgs8) {
+    using Cfg = TileCfg8<GATED, BN, BM, WN, WM, S>;
     constexpr int NW = Cfg::NW, TN = Cfg::TN, TM = Cfg::TM, TNG = GATED ? TN / 2 : TN, H = GATED ? 2 : 1;
     constexpr int NROWS = GATED ? BN / 2 : BN;  // n of a tile; gated: one half of the N side per projection
     using NSide = Side8<NROWS, NW>;
     using MSide = Side8<BM, NW>;
-    constexpr int NL = NSide::loads * H, L = NL + MSide::loads + 1 + H;  // loads of a stage
+    constexpr int NL = NSide::loads * H, ML = NL + MSide::loads, XL = Cfg::xl, L = ML + XL + H;  // loads of a stage
     constexpr int WROWS = NROWS / WN, MROWS = BM / WM;               // n and m of a wavefront
-    static_assert(128 % WROWS == 0 && MROWS <= 64 && TNG % 2 == 0 && TN >= 4, "shape");
+    static_assert(128 % WROWS == 0 && (MROWS <= 64 || MROWS % 64 == 0) && TNG % 2 == 0 && TN >= 4 && TN % 2 == 0 && L * (S - 1) < 64, "shape");
     constexpr int JOIN = TN - 2;                // the row of fragments at which the next stage is waited for
     constexpr int RATE = (L + 1) / 2;           // loads that go out with each of the last two rows
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
 
-    const Gemm8 &g = a.g;
+    // The arguments are read anew where they are used, so that the loop over the stages has
+    // the registers: kept in scalar registers from the start they spill into vector ones,
+    // and those into memory, whose waits would be for the loads of the stages too.
+    auto args = []() -> const TileArgs8 & {
+        auto p = (const __attribute__((address_space(4))) TileArgs8 *)__builtin_amdgcn_kernarg_segment_ptr();
+        asm volatile("" : "+s"(p));
+        return *(const TileArgs8 *)p;
+    };
     const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
     const int wn = wave % WN, wm = wave / WN;
     const int nrow = wn * WROWS, mrow = wm * MROWS;
 
     // Workgroup b runs on XCD b mod 8, which walks one contiguous range of tiles (its own
     // L2); its workgroups take the range's tiles in turn.
-    const int xcd = blockIdx.x & 7, local = blockIdx.x >> 3;
-    const int per = a.tiles >> 3, extra = a.tiles & 7;
-    const int first = uni(xcd * per + min(xcd, extra) + local);
-    const int end = uni((xcd + 1) * per + min(xcd + 1, extra));
-    const int stride = uni((a.groups >> 3) + (xcd < (a.groups & 7) ? 1 : 0));
-    if (first >= end) return;
-    const int mine = (end - first + stride - 1) / stride;  // tiles of this workgroup
+    int first, mine, stride;
+    {
+        const TileArgs8 &a = args();
+        const int xcd = blockIdx.x & 7, local = blockIdx.x >> 3;
+        const int per = a.tiles >> 3, extra = a.tiles & 7;
+        first = uni(xcd * per + min(xcd, extra) + local);
+        const int end = uni((xcd + 1) * per + min(xcd + 1, extra));
+        stride = uni((a.groups >> 3) + (xcd < (a.groups & 7) ? 1 : 0));
+        if (first >= end) return;
+        mine = (end - first + stride - 1) / stride;  // tiles of this workgroup
+    }
 
-    const int K = uni((int)g.K), ns = (K + kBlock - 1) / kBlock;  // stages of a tile
+    const int K = uni((int)args().g.K), ns = (K + kBlock - 1) / kBlock;  // stages of a tile
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)smem;
-    const int64_t nld = g.w[0].ld, mld = g.x.ld;
 
     // A tile: bands of 8 M tiles, down each band first, so that neighbours share operands
     struct Tile {
@@ -357,6 +371,7 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8 a) {
         int s0, s1;  // its stages
     };
     auto tile_at = [&](int i) {
+        const TileArgs8 &a = args();
         int t = first + i * stride;
         const int one = a.mtiles * a.ntiles;
         Tile q;
@@ -373,18 +388,19 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8 a) {
 
     NSide nside;
     MSide mside;
-    nside.setup(nld, wave, lane);
-    mside.setup(mld, wave, lane);
+    nside.setup(args().g.w[0].ld, wave, lane);
+    mside.setup(args().g.x.ld, wave, lane);
     const Reads8 read(lane);
 
-    // The loads run over the stages of all tiles without a break, two stages ahead of the
-    // products.  A run of stages below K differs from stage to stage by one addition per
+    // The loads run over the stages of all tiles without a break, S stages ahead of
+    // the products.  A run of stages below K differs from stage to stage by one addition per
     // operand; what else there is to work out is done between runs.
     typename NSide::Cursor nc, nc1;
     typename MSide::Cursor mc;
     i32x4 xs, ws[H];  // the scales' buffers
-    const uint32_t xoff = lane < MROWS ? (uint32_t)lane * (uint32_t)g.x.scale_row * 4u : kInvalidOffset;
-    const uint32_t woff = lane == 0 ? 0u : kInvalidOffset;
+    const uint32_t xoff = lane < MROWS ? (uint32_t)lane * (uint32_t)args().g.x.scale_row * 4u : kInvalidOffset;
+    const uint32_t xmore = XL > 1 ? uni((int)args().g.x.scale_row * 256) : 0;  // 64 rows further on
+    const uint64_t xstep = (uint64_t)args().g.x.scale_col * 4, wstep = (uint64_t)args().g.w[0].scale_col * 4;
     uint32_t lat = lds0 + wave * 1024, slat = lds0 + Cfg::scales_at + wave * Cfg::scales;
     int run = 0, lstage = 0, lend = 0, ltile = -1, lslot = 0;
     int cuts = 0;  // slots that hold, or will, a chunk which K cuts
@@ -397,6 +413,8 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8 a) {
             return;
         }
         const Tile q = tile_at(ltile);
+        const Gemm8 &g = args().g;
+        const int64_t nld = g.w[0].ld, mld = g.x.ld;
         if (lstage == lend) {
             lstage = q.s0;
             lend = q.s1;
@@ -415,7 +433,7 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8 a) {
         const int64_t n = q.n0 + nrow;
 #pragma unroll
         for (int h = 0; h < H; ++h)
-            ws[h] = buffer_at(reinterpret_cast<uint64_t>(g.w[h].scales + n / kBlock * g.w[h].scale_row + lstage * g.w[h].scale_col),
+            ws[h] = buffer_at(reinterpret_cast<uint64_t>(g.w[h].scales + n / kBlock * g.w[0].scale_row + lstage * g.w[0].scale_col),
                               n < g.N ? 4u : 0u);
         if (kBlock > K - k0 && (K & 15) != 0) cuts |= 1 << lslot;
         run = uni(kBlock <= K - k0 ? min(K / kBlock - lstage, lend - lstage) : 1);
@@ -430,9 +448,11 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8 a) {
         constexpr int i = decltype(which)::value;
         if constexpr (i < NSide::loads) nside.template load<i>(nc, lat);
         else if constexpr (i < NL) nside.template load<i - NSide::loads>(nc1, lat + NSide::bytes);
-        else if constexpr (i < NL + MSide::loads) mside.template load<i - NL>(mc, lat + BN * kBlock);
-        else if constexpr (i == NL + MSide::loads) dma4<0>(xs, xoff, 0, slat);
-        else if constexpr (i < L) dma4<256 * (i - NL - MSide::loads)>(ws[i - NL - MSide::loads - 1], woff, 0, slat);
+        else if constexpr (i < ML) mside.template load<i - NL>(mc, lat + BN * kBlock);
+        else if constexpr (i < ML + XL) dma4<256 * (i - ML)>(xs, xoff, (i - ML) * xmore, slat);
+        else if constexpr (i < L) {
+            if (lane == 0) dma4<256 * XL + 4 * (i - ML - XL)>(ws[i - ML - XL], 0, 0, slat);
+        }
     };
     auto move = [](i32x4 &rs, uint64_t by) {
         const uint64_t base = ((uint64_t)(uint32_t)rs[1] << 32 | (uint32_t)rs[0]) + by;
@@ -443,10 +463,10 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8 a) {
         NSide::advance(nc);
         if constexpr (GATED) NSide::advance(nc1);
         MSide::advance(mc);
-        move(xs, (uint64_t)g.x.scale_col * 4);
+        move(xs, xstep);
 #pragma unroll
-        for (int h = 0; h < H; ++h) move(ws[h], (uint64_t)g.w[h].scale_col * 4);
-        lslot ^= 1;
+        for (int h = 0; h < H; ++h) move(ws[h], wstep);
+        lslot = lslot + 1 == S ? 0 : lslot + 1;
         lat = lds0 + wave * 1024 + lslot * Cfg::stage;
         slat = lds0 + Cfg::scales_at + wave * Cfg::scales + lslot * Cfg::stage;
     };
@@ -465,10 +485,12 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8 a) {
     f32x4 acc[TN][TM];
     int slot = 0;
     if (ns > 0) {
-        begin_stage();
-        each<L>(load);
-        end_stage();
-        wait_vm<0>();
+        for (int s = 0; s + 1 < S; ++s) {
+            begin_stage();
+            each<L>(load);
+            end_stage();
+        }
+        wait_vm<L *(S - 2)>();
         mend(0);
         lds_barrier();
         begin_stage();
@@ -476,45 +498,48 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8 a) {
         end_stage();
     }
 
-    // A stage is multiplied, a row of fragments at a time; the codes of X are widened once,
-    // those of a row of W two rows ahead.  When the last row's have been read, this stage's
-    // buffer is free and the next stage is waited for.
-    auto multiply = [&]() {
-        const uint8_t *cur = smem + slot * Cfg::stage;
-        slot ^= 1;
-        auto readn = [&](int i) {
-            if constexpr (GATED) return read(cur + (i >= TNG ? NSide::bytes : 0), nrow + i % TNG * 16);
-            else return read(cur, nrow + i * 16);
-        };
+    // codes of W: row i of a stage's fragments
+    auto codes_n = [&](const uint8_t *st, int i) {
+        if constexpr (GATED) return read(st + (i >= TNG ? NSide::bytes : 0), nrow + i % TNG * 16);
+        else return read(st, nrow + i * 16);
+    };
+    i32x8 fa[2];
+    float scale[H][TM];
+    Wide fb[TM];
+    Vec8<__bf16>::type w[2];  // of a row of W, one step of 32 k ahead
+    auto fetch_scales = [&](const uint8_t *st) {
+        const float *s = reinterpret_cast<const float *>(st + Cfg::scales_at + wave * Cfg::scales);
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+#pragma unroll
+            for (int j = 0; j < TM; ++j) scale[h][j] = s[j * 16 + (lane & 15)] * s[64 * XL + h];
+    };
+    auto fetch = [&]() {  // what the first products of the stage in `slot` need
+        const uint8_t *st = smem + slot * Cfg::stage;
         i32x8 raw[TM];
+        fa[0] = codes_n(st, 0);
+        fa[1] = codes_n(st, 1);
 #pragma unroll
-        for (int j = 0; j < TM; ++j) raw[j] = read(cur + BN * kBlock, mrow + j * 16);
-        i32x8 fa[2] = {readn(0), readn(1)};
-        float scale[H][TM];
-        {
-            const float *s = reinterpret_cast<const float *>(cur + Cfg::scales_at + wave * Cfg::scales);
-#pragma unroll
-            for (int h = 0; h < H; ++h)
-#pragma unroll
-                for (int j = 0; j < TM; ++j) scale[h][j] = s[j * 16 + (lane & 15)] * s[64 * (h + 1)];
-        }
-        Wide fb[TM];
+        for (int j = 0; j < TM; ++j) raw[j] = read(st + BN * kBlock, mrow + j * 16);
+        fetch_scales(st);
+        w[0] = widen(fa[0][0], fa[0][1]);
 #pragma unroll
         for (int j = 0; j < TM; ++j) fb[j] = Wide(raw[j]);
+    };
+    // A stage is multiplied, a row of fragments at a time.  Beside a row's products stand the
+    // scaling of the row before and the widening of the next row's codes; beside the last
+    // row's the widening of the next stage's codes of X.  When the codes of the last row have
+    // been read, this stage's buffer is free and the next stage is waited for.
+    auto multiply = [&]() {
+        const uint8_t *cur = smem + slot * Cfg::stage;
+        slot = slot + 1 == S ? 0 : slot + 1;
+        const uint8_t *nxt = smem + slot * Cfg::stage;
+        f32x4 part[TM];
+        i32x4 raw[TM];  // half of X's codes of the next stage
 #pragma unroll
         for (int i = 0; i < TN; ++i) {
-            const Wide w(fa[i & 1]);
-            if (i + 2 < TN) fa[i & 1] = readn(i + 2);
-            f32x4 part[TM] = {};
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-#pragma unroll
-                for (int j = 0; j < TM; ++j)
-                    part[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.k[q], fb[j].k[q], part[j], 0, 0, 0);
-#pragma unroll
-            for (int j = 0; j < TM; ++j) add_scaled(acc[i][j], part[j], scale[GATED && i >= TNG][j]);
             if (i == JOIN) {
-                wait_vm<0>();
+                wait_vm<L *(S - 2)>();
                 mend(slot);
                 lds_barrier();
                 begin_stage();
@@ -524,8 +549,32 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8 a) {
                     constexpr int at = (decltype(ic)::value - JOIN) * RATE;
                     if constexpr (at >= 0) each<RATE>([&](auto e) { load(std::integral_constant<int, at + decltype(e)::value>{}); });
                 });
-            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                if (i == TN - 1 && q % 2 == 0)
+#pragma unroll
+                    for (int j = 0; j < TM; ++j) raw[j] = read.half(nxt + BN * kBlock, mrow + j * 16, q / 2);
+#pragma unroll
+                for (int j = 0; j < TM; ++j) {
+                    if (i > 0 && q == 0) add_scaled(acc[i - 1][j], part[j], scale[GATED && i - 1 >= TNG][j]);
+                    part[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[q & 1], fb[j].k[q], q ? part[j] : f32x4{}, 0, 0, 0);
+                }
+                {
+                    const i32x8 &from = fa[q < 3 ? i & 1 : (i + 1) & 1];
+                    const int at = (q + 1) % 4 * 2;
+                    w[(q + 1) & 1] = widen(from[at], from[at + 1]);
+                }
+                if (i == TN - 1)
+#pragma unroll
+                    for (int j = 0; j < TM; ++j) fb[j].k[q] = widen(raw[j][q % 2 * 2], raw[j][q % 2 * 2 + 1]);
+                // two rows ahead, in the end the next stage's first two
+                if (q == 3) fa[i & 1] = i + 2 < TN ? codes_n(cur, i + 2) : codes_n(nxt, i + 2 - TN);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
+#pragma unroll
+        for (int j = 0; j < TM; ++j) add_scaled(acc[TN - 1][j], part[j], scale[GATED][j]);
+        fetch_scales(nxt);
         end_stage();
     };
 
@@ -537,12 +586,15 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8 a) {
         for (int i = 0; i < TN; ++i)
 #pragma unroll
             for (int j = 0; j < TM; ++j) acc[i][j] = f32x4{};
+        if (q.s0 < q.s1) fetch();
 #pragma unroll 1
         for (int s = q.s0; s < q.s1; ++s) multiply();
 
         // Results straight from the registers.  A lane holds 4 consecutive n of every 16;
         // exchanging the odd rows of 16 lanes of one such group with the even ones of the
         // next leaves 8 consecutive n in each lane.
+        const TileArgs8 &a = args();
+        const Gemm8 &g = a.g;
         const bool eight = a.part.keep == 0 && g.q.codes;
         float top[TM] = {};  // largest values of this lane's rows
 #pragma unroll 1
@@ -555,6 +607,7 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8 a) {
                     t[h][0] = acc[h * TNG + i][j];
                     t[h][1] = acc[h * TNG + i + 1][j];
                 }
+                asm volatile("" ::"n"(i * TM + j));  // keeps the compiler from merging the branches, which would index registers
             });
             float z[8], u[8];
 #pragma unroll
@@ -591,6 +644,7 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8 a) {
                     acc[i + 1][j][e] = z[e + 4];
                 }
                 top[j] = fmaxf(top[j], most);
+                asm volatile("" ::"n"(i * TM + j));
             });
         }
         if (!eight) continue;
@@ -661,10 +715,10 @@ int join(const Gemm8 &g, const Partial8 &q, hipStream_t stream) {
     return SA_OK;
 }
 
-template <typename T, bool GATED, int BN, int BM, int WN, int WM>
+template <typename T, bool GATED, int BN, int BM, int WN, int WM, int S>
 int launch_tiles(const Gemm8 &g, const Partial8 &q, hipStream_t stream) {
-    using Cfg = TileCfg8<GATED, BN, BM, WN, WM>;
-    auto kern = k_tile8<T, GATED, BN, BM, WN, WM>;
+    using Cfg = TileCfg8<GATED, BN, BM, WN, WM, S>;
+    auto kern = k_tile8<T, GATED, BN, BM, WN, WM, S>;
     int groups = 0;
     if (int rc = resident(reinterpret_cast<const void *>(kern), Cfg::NT, Cfg::lds, &groups)) return rc;
     constexpr int rows = GATED ? BN / 2 : BN;
@@ -679,7 +733,7 @@ int launch_tiles(const Gemm8 &g, const Partial8 &q, hipStream_t stream) {
 template <typename T, bool GATED>
 int run(const Gemm8 &g, const Plan8 &p, const Partial8 &q, hipStream_t stream) {
     if (p.path == kTile8) {
-        if (int rc = launch_tiles<T, GATED, 256, 128, 4, 2>(g, q, stream)) return rc;
+        if (int rc = launch_tiles<T, GATED, 256, 128, 4, 2, 3>(g, q, stream)) return rc;
         return q.keep ? join<T, GATED>(g, q, stream) : SA_OK;
     }
     constexpr int NF = 1, MF = 4;
