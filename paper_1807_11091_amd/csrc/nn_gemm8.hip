@@ -29,14 +29,22 @@ __device__ inline Vec8<__bf16>::type widen(int lo, int hi) {
 // spread over lanes and bytes does not matter as long as both operands agree.
 //
 // The codes are widened for the bfloat16 instructions, whose binary32 sums are good to
-// 1e-8 here.  The 8-bit ones (all that take e4m3, of 32 or 128 k) cut the products of a
-// group of k 14 bits below its largest: sums of 128 are off by 1.3e-5 of their size.
+// 1e-8 here.
 __device__ inline f32x4 block_products(i32x8 a, i32x8 b) {
     f32x4 c = {};
 #pragma unroll
     for (int q = 0; q < 4; ++q)
         c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(a[2 * q], a[2 * q + 1]), widen(b[2 * q], b[2 * q + 1]), c, 0, 0, 0);
     return c;
+}
+
+// The same by one 8-bit instruction, which spans the block.  It cuts each product of 8
+// consecutive k at 2^-13 of the largest one's power of two (so do all that take e4m3): the
+// sums are off by 1.3e-5 of their size.  That is lost in the rounding of a 16-bit result
+// (1.7e-3 in bfloat16, 2.1e-4 in binary16), but not in binary32 ones or in the scales of
+// 8-bit ones, which are made of exact products.
+__device__ inline f32x4 block_products8(i32x8 a, i32x8 b) {
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, f32x4{}, 0, 0, 0, 0, 0, 0);
 }
 
 __device__ inline void add_scaled(f32x4 &acc, f32x4 part, float scale) {
@@ -321,7 +329,7 @@ struct Wide {
     Wide() = default;
 };
 
-template <typename T, bool GATED, int BN, int BM, int WN, int WM, int S>
+template <typename T, bool GATED, bool EXACT, int BN, int BM, int WN, int WM, int S>
 __global__ __launch_bounds__(WN *WM * 64, WN * WM / 4) void k_tile8(TileArgs8) {
     using Cfg = TileCfg8<GATED, BN, BM, WN, WM, S>;
     constexpr int NW = Cfg::NW, TN = Cfg::TN, TM = Cfg::TM, TNG = GATED ? TN / 2 : TN, H = GATED ? 2 : 1;
@@ -331,8 +339,9 @@ __global__ __launch_bounds__(WN *WM * 64, WN * WM / 4) void k_tile8(TileArgs8) {
     constexpr int NL = NSide::loads * H, ML = NL + MSide::loads, XL = Cfg::xl, L = ML + XL + H;  // loads of a stage
     constexpr int WROWS = NROWS / WN, MROWS = BM / WM;               // n and m of a wavefront
     static_assert(128 % WROWS == 0 && (MROWS <= 64 || MROWS % 64 == 0) && TNG % 2 == 0 && TN >= 4 && TN % 2 == 0 && L * (S - 1) < 64, "shape");
-    constexpr int JOIN = TN - 2;                // the row of fragments at which the next stage is waited for
-    constexpr int RATE = (L + 1) / 2;           // loads that go out with each of the last two rows
+    constexpr int JOIN = EXACT ? TN - 2 : 0;         // the row of fragments at which the next stage is waited for
+    constexpr int RATE = (L + TN - JOIN - 1) / (TN - JOIN);  // loads that go out with each row from there on
+    constexpr int AHEAD = EXACT ? 2 : TN;            // rows of W's codes in registers
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
 
     // The arguments are read anew where they are used, so that the loop over the stages has
@@ -503,10 +512,10 @@ __global__ __launch_bounds__(WN *WM * 64, WN * WM / 4) void k_tile8(TileArgs8) {
         if constexpr (GATED) return read(st + (i >= TNG ? NSide::bytes : 0), nrow + i % TNG * 16);
         else return read(st, nrow + i * 16);
     };
-    i32x8 fa[2];
+    i32x8 fa[AHEAD];
     float scale[H][TM];
-    Wide fb[TM];
-    Vec8<__bf16>::type w[2];  // of a row of W, one step of 32 k ahead
+    typename std::conditional<EXACT, Wide, i32x8>::type fb[TM];
+    Vec8<__bf16>::type w[2];  // EXACT: of a row of W, one step of 32 k ahead
     auto fetch_scales = [&](const uint8_t *st) {
         const float *s = reinterpret_cast<const float *>(st + Cfg::scales_at + wave * Cfg::scales);
 #pragma unroll
@@ -517,14 +526,17 @@ __global__ __launch_bounds__(WN *WM * 64, WN * WM / 4) void k_tile8(TileArgs8) {
     auto fetch = [&]() {  // what the first products of the stage in `slot` need
         const uint8_t *st = smem + slot * Cfg::stage;
         i32x8 raw[TM];
-        fa[0] = codes_n(st, 0);
-        fa[1] = codes_n(st, 1);
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) fa[i] = codes_n(st, i);
 #pragma unroll
         for (int j = 0; j < TM; ++j) raw[j] = read(st + BN * kBlock, mrow + j * 16);
         fetch_scales(st);
-        w[0] = widen(fa[0][0], fa[0][1]);
+        if constexpr (EXACT) w[0] = widen(fa[0][0], fa[0][1]);
 #pragma unroll
-        for (int j = 0; j < TM; ++j) fb[j] = Wide(raw[j]);
+        for (int j = 0; j < TM; ++j) {
+            if constexpr (EXACT) fb[j] = Wide(raw[j]);
+            else fb[j] = raw[j];
+        }
     };
     // A stage is multiplied, a row of fragments at a time.  Beside a row's products stand the
     // scaling of the row before and the widening of the next row's codes; beside the last
@@ -549,6 +561,7 @@ __global__ __launch_bounds__(WN *WM * 64, WN * WM / 4) void k_tile8(TileArgs8) {
                     constexpr int at = (decltype(ic)::value - JOIN) * RATE;
                     if constexpr (at >= 0) each<RATE>([&](auto e) { load(std::integral_constant<int, at + decltype(e)::value>{}); });
                 });
+            if constexpr (EXACT) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 if (i == TN - 1 && q % 2 == 0)
@@ -569,6 +582,19 @@ __global__ __launch_bounds__(WN *WM * 64, WN * WM / 4) void k_tile8(TileArgs8) {
                     for (int j = 0; j < TM; ++j) fb[j].k[q] = widen(raw[j][q % 2 * 2], raw[j][q % 2 * 2 + 1]);
                 // two rows ahead, in the end the next stage's first two
                 if (q == 3) fa[i & 1] = i + 2 < TN ? codes_n(cur, i + 2) : codes_n(nxt, i + 2 - TN);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            } else {
+#pragma unroll
+                for (int j = 0; j < TM; ++j) {
+                    if (i > 0) {
+                        add_scaled(acc[i - 1][j], part[j], scale[GATED && i - 1 >= TNG][j]);
+                        asm volatile("" : "+v"(acc[i - 1][j]));  // here, and not when all rows' products are there
+                    }
+                    part[j] = block_products8(fa[i], fb[j]);
+                    if (i == TN - 1) fb[j] = read(nxt + BN * kBlock, mrow + j * 16);
+                }
+                fa[i] = codes_n(nxt, i);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
@@ -715,10 +741,10 @@ int join(const Gemm8 &g, const Partial8 &q, hipStream_t stream) {
     return SA_OK;
 }
 
-template <typename T, bool GATED, int BN, int BM, int WN, int WM, int S>
+template <typename T, bool GATED, bool EXACT, int BN, int BM, int WN, int WM, int S>
 int launch_tiles(const Gemm8 &g, const Partial8 &q, hipStream_t stream) {
     using Cfg = TileCfg8<GATED, BN, BM, WN, WM, S>;
-    auto kern = k_tile8<T, GATED, BN, BM, WN, WM, S>;
+    auto kern = k_tile8<T, GATED, EXACT, BN, BM, WN, WM, S>;
     int groups = 0;
     if (int rc = resident(reinterpret_cast<const void *>(kern), Cfg::NT, Cfg::lds, &groups)) return rc;
     constexpr int rows = GATED ? BN / 2 : BN;
@@ -733,7 +759,12 @@ int launch_tiles(const Gemm8 &g, const Partial8 &q, hipStream_t stream) {
 template <typename T, bool GATED>
 int run(const Gemm8 &g, const Plan8 &p, const Partial8 &q, hipStream_t stream) {
     if (p.path == kTile8) {
-        if (int rc = launch_tiles<T, GATED, 256, 128, 4, 2, 3>(g, q, stream)) return rc;
+        // 8-bit instructions where every result has 16 bits (8192 x 4096 x 9830: 362 us, and 585
+        // of exact products)
+        const bool exact = g.q.codes || g.e.out_f32;
+        const int rc = exact ? launch_tiles<T, GATED, true, 256, 128, 4, 2, 3>(g, q, stream)
+                             : launch_tiles<T, GATED, false, 256, 128, 4, 2, 3>(g, q, stream);
+        if (rc) return rc;
         return q.keep ? join<T, GATED>(g, q, stream) : SA_OK;
     }
     constexpr int NF = 1, MF = 4;

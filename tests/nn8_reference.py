@@ -79,20 +79,35 @@ def rms_bwd(dy, s, rstd, gamma, dr):
     return (dx if dr is None else dx + dr), (dy * xn).sum(0)
 
 
-def product(x, w):
+def _highest(m, block):
+    """2^e of the largest exponent e of each 8 codes of a row, scaled, [rows, groups]."""
+    q, s = m
+    r, c = q.shape
+    v = torch.nn.functional.pad(q.double().abs(), (0, -c % 8))
+    e = torch.floor(torch.log2(torch.clamp(v.view(r, -1, 8).amax(2), min=2.0 ** -6)))
+    return torch.exp2(e) * wide(s, r, c, block)[:, ::8]
+
+
+def product(x, w, exact=True):
     """z = x w^T of two 8-bit matrices and how far a binary32 sum may be from it: within
     a block 128 exact products in any order, each addition off by at most 2 E of the
     sums of magnitudes (the matrix cores' adders may cut instead of rounding); then the
     scales' product, a multiplication and an addition for each block, and the joining of
-    at most 32 parts and 8 wavefronts."""
+    at most 32 parts and 8 wavefronts.
+
+    exact=False: the 8-bit matrix instructions, which cut each product of 8 consecutive k
+    at 2^-13 of 2^(largest sum of two exponents among them)."""
     a, b = values(x, 1), values(w, B)
     mag = a.abs() @ b.abs().t()
-    return a @ b.t(), (2 * B + 2 * blocks(a.shape[1]) + 48) * E * mag
+    tol = (2 * B + 2 * blocks(a.shape[1]) + 48) * E * mag
+    if not exact:
+        tol = tol + 8 * 2.0 ** -13 * (_highest(x, 1) @ _highest(w, B).t())
+    return a @ b.t(), tol
 
 
-def linear8(x, w, bias, r, act):
+def linear8(x, w, bias, r, act, exact=True):
     """(y, its tolerance before rounding, z, z's)."""
-    z, tol = product(x, w)
+    z, tol = product(x, w, exact)
     if bias is not None:
         z = z + bias.double()
         tol = tol + E * (z.abs() + bias.double().abs())
@@ -105,9 +120,9 @@ def linear8(x, w, bias, r, act):
     return y, ty, z, tol
 
 
-def glu8(x, wg, wu, bg, bu, act):
+def glu8(x, wg, wu, bg, bu, act, exact=True):
     """(h, its tolerance, g, g's, u, u's)."""
-    a, ta, g, tg = linear8(x, wg, bg, None, act)
-    u, tu = linear8(x, wu, bu, None, "none")[:2]
+    a, ta, g, tg = linear8(x, wg, bg, None, act, exact)
+    u, tu = linear8(x, wu, bu, None, "none", exact)[:2]
     h = a * u
     return h, ta * (u.abs() + tu) + tu * a.abs() + 2 * E * h.abs(), g, tg, u, tu

@@ -227,7 +227,7 @@ def test_linear8(M, N, K, out):
     Q, qbufs = out8(M, N) if out in ("q", "both") else (None, None)
     got = sa.linear8_fwd(X, W, bias, R=R, act=sa.ACTS[act], Y=Y, Z=Z, Q=Q, out="")
     assert got[0] is Y and got[1] is Q
-    y, ty, z, tz = ref8.linear8(X, W, bias, R, act)
+    y, ty, z, tz = ref8.linear8(X, W, bias, R, act, exact=out != "same")
     if Y is not None:
         check_out(Y, y, ty, to, ybuf, "Y")
     if Z is not None:
@@ -235,8 +235,8 @@ def test_linear8(M, N, K, out):
     if Q is not None:
         ref8.check_codes(Q, y, ty, "Q")
         assert untouched8(Q, qbufs)
-    if R is not None and Y is not None:  # Y in R's place
-        sa.linear8_fwd(X, W, bias, R=R, act=sa.ACTS[act], Y=R, out="")
+    if R is not None and Y is not None:  # Y in R's place; with the same outputs, which choose the instructions
+        sa.linear8_fwd(X, W, bias, R=R, act=sa.ACTS[act], Y=R, Z=Z, Q=Q, out="")
         assert T.equal(R, Y)
 
 
@@ -254,7 +254,7 @@ def test_glu8(M, N, K, out):
     U, ubuf = out_matrix(M, N, dt, pitch) if out == "all" else (None, None)
     Q, qbufs = out8(M, N, 1, layout) if out != "h" else (None, None)
     sa.glu8_fwd(X, Wg, Wu, bg, bu, act=sa.ACTS[act], H=H, Q=Q, G=G, U=U, out="")
-    h, th, gg, tg, u, tu = ref8.glu8(X, Wg, Wu, bg, bu, act)
+    h, th, gg, tg, u, tu = ref8.glu8(X, Wg, Wu, bg, bu, act, exact=out != "h")
     if H is not None:
         check_out(H, h, th, dt, hbuf, "H")
     if G is not None:
