@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdint>
 
 #include "nn_epilogue.h"
@@ -25,16 +26,25 @@ __device__ inline Vec8<__bf16>::type widen(int lo, int hi) {
     return Vec8<__bf16>::type{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
+// A lane's 32 codes of 16 rows' block, as the bfloat16 instructions take them.
+struct Wide {
+    Vec8<__bf16>::type k[4];
+    __device__ explicit Wide(i32x8 v) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) k[q] = widen(v[2 * q], v[2 * q + 1]);
+    }
+    Wide() = default;
+};
+
 // A block's products of 16 rows with 16, a lane's 32 codes of each in a and b.  How k is
 // spread over lanes and bytes does not matter as long as both operands agree.
 //
 // The codes are widened for the bfloat16 instructions, whose binary32 sums are good to
 // 1e-8 here.
-__device__ inline f32x4 block_products(i32x8 a, i32x8 b) {
+__device__ inline f32x4 block_products(const Wide &a, const Wide &b) {
     f32x4 c = {};
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(a[2 * q], a[2 * q + 1]), widen(b[2 * q], b[2 * q + 1]), c, 0, 0, 0);
+    for (int q = 0; q < 4; ++q) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.k[q], b.k[q], c, 0, 0, 0);
     return c;
 }
 
@@ -102,17 +112,18 @@ __global__ __launch_bounds__(256) void k_join8(Gemm8 g, Partial8 q, int64_t firs
 // ------------------------------------------------------------- few rows of M
 // k_rows8: products with few rows of M, bound by reading the weights once and by latency.
 // A workgroup of 8 wavefronts takes NF * 16 of their rows and MF * 16 of M; its wavefronts
-// take the blocks of k in turn, U at a time, and feed the matrix cores straight from
-// memory.  Their sums are joined through LDS in a fixed order.  Rows past M or N read the
-// last row and are not stored.
-template <typename T, bool GATED, int NF, int MF, int U>
+// take the blocks of k in turn, U at a time with the next U on their way, and feed the
+// matrix cores straight from memory.  Their sums are joined through LDS in a fixed order.
+// Rows past M or N read the last row and are not stored.
+template <typename T, bool GATED, bool EXACT, int NF, int MF, int U>
 __global__ __launch_bounds__(512) void k_rows8(Gemm8 g, Partial8 q) {
     constexpr int NW = 8, H = GATED ? 2 : 1;
+    static_assert(128 % (NF * 16) == 0, "one block row");
     __shared__ float sums[NW][NF * H * MF][256];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6);
     const int r = lane & 15, kg = (lane >> 4) * 16;
     const int64_t n0 = (int64_t)blockIdx.x * NF * 16, m0 = (int64_t)blockIdx.z * MF * 16;
-    const int K = (int)g.K;
+    const int K = (int)g.K, last = (K - 1) & ~15;  // the last chunk of a row that holds codes
     // blocks of k of this workgroup
     const int blocks = (K + kBlock - 1) / kBlock;
     const int b0 = (int)((int64_t)blocks * blockIdx.y / q.split), b1 = (int)((int64_t)blocks * (blockIdx.y + 1) / q.split);
@@ -122,59 +133,95 @@ __global__ __launch_bounds__(512) void k_rows8(Gemm8 g, Partial8 q) {
 #pragma unroll
     for (int h = 0; h < H; ++h) {
 #pragma unroll
-        for (int f = 0; f < NF; ++f) wp[h * NF + f] = g.w[h].codes + min(n0 + f * 16 + r, g.N - 1) * g.w[h].ld + kg;
-        sw[h] = g.w[h].scales + n0 / kBlock * g.w[h].scale_row;  // NF * 16 divides 128: one block row
+        for (int f = 0; f < NF; ++f) wp[h * NF + f] = g.w[h].codes + min(n0 + f * 16 + r, g.N - 1) * g.w[h].ld;
+        sw[h] = g.w[h].scales + n0 / kBlock * g.w[h].scale_row;
     }
 #pragma unroll
     for (int j = 0; j < MF; ++j) {
         const int64_t m = min(m0 + j * 16 + r, g.M - 1);
-        xp[j] = g.x.codes + m * g.x.ld + kg;
+        xp[j] = g.x.codes + m * g.x.ld;
         sx[j] = g.x.scales + m * g.x.scale_row;
     }
 
-    f32x4 acc[H * NF][MF] = {};
-    for (int b = b0 + wave * U; b < b1; b += NW * U) {
-        i32x8 w[U][H * NF], x[U][MF];
+    struct Set {  // this lane's part of U blocks: chunks of 16 codes at kg and kg + 64, and scales
+        i32x4 w[U][H * NF][2], x[U][MF][2];
         float cx[U][MF], cw[U][H];
-        // this lane's bytes of a block: chunks of 16 at kg and kg + 64, zeros past K
-        auto load = [&](const uint8_t *p, int k) {
-            union {
-                i32x4 h[2];
-                i32x8 v;
-            } o;
+    };
+    auto fetch = [&](Set &s, int b) {  // blocks past the last one: the last one again
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int at = min(b + u * NW, b1 - 1);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const int n = K - k - i * 64 - kg;
-                o.h[i] = i32x4{};
-                if (n > 0) o.h[i] = *reinterpret_cast<const i32x4 *>(p + k + i * 64);
-                if (n < 16)
+                const int k = min(at * kBlock + i * 64 + kg, last);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int have = n - e * 4;
-                        if (have < 4) o.h[i][e] = have <= 0 ? 0 : o.h[i][e] & ((1 << have * 8) - 1);
-                    }
-            }
-            return o.v;
-        };
+                for (int f = 0; f < H * NF; ++f) s.w[u][f][i] = *reinterpret_cast<const i32x4 *>(wp[f] + k);
 #pragma unroll
-        for (int s = 0; s < U; ++s) {
-            const int at = min(b + s, b1 - 1), k = b + s < b1 ? at * kBlock : K;
-#pragma unroll
-            for (int f = 0; f < H * NF; ++f) w[s][f] = load(wp[f], k);
-#pragma unroll
-            for (int j = 0; j < MF; ++j) {
-                x[s][j] = load(xp[j], k);
-                cx[s][j] = b + s < b1 ? sx[j][at * g.x.scale_col] : 0.0f;
+                for (int j = 0; j < MF; ++j) s.x[u][j][i] = *reinterpret_cast<const i32x4 *>(xp[j] + k);
             }
 #pragma unroll
-            for (int h = 0; h < H; ++h) cw[s][h] = b + s < b1 ? sw[h][at * g.w[h].scale_col] : 0.0f;
+            for (int j = 0; j < MF; ++j) s.cx[u][j] = sx[j][at * g.x.scale_col];
+#pragma unroll
+            for (int h = 0; h < H; ++h) s.cw[u][h] = sw[h][at * g.w[0].scale_col];
         }
+    };
+    f32x4 acc[H * NF][MF] = {};
+    auto whole = [&](i32x4 (&c)[2], int k) {  // a lane's codes, zeros past K
+        union {
+            i32x4 h[2];
+            i32x8 v;
+        } o;
 #pragma unroll
-        for (int s = 0; s < U; ++s)
+        for (int i = 0; i < 2; ++i) {
+            o.h[i] = c[i];
+            if (k + kBlock > K)
 #pragma unroll
-            for (int f = 0; f < H * NF; ++f)
+                for (int e = 0; e < 4; ++e) {
+                    const int have = K - k - i * 64 - kg - e * 4;
+                    if (have < 4) o.h[i][e] = have <= 0 ? 0 : o.h[i][e] & ((1 << have * 8) - 1);
+                }
+        }
+        return o.v;
+    };
+    auto work = [&](Set &s, int b) {
 #pragma unroll
-                for (int j = 0; j < MF; ++j) add_scaled(acc[f][j], block_products(w[s][f], x[s][j]), cx[s][j] * cw[s][f / NF]);
+        for (int u = 0; u < U; ++u) {
+            if (b + u * NW >= b1) break;
+            const int k = (b + u * NW) * kBlock;
+            i32x8 x[MF];
+#pragma unroll
+            for (int j = 0; j < MF; ++j) x[j] = whole(s.x[u][j], k);
+            if constexpr (EXACT) {
+                Wide wx[MF];
+#pragma unroll
+                for (int j = 0; j < MF; ++j) wx[j] = Wide(x[j]);
+#pragma unroll
+                for (int f = 0; f < H * NF; ++f) {
+                    const Wide w(whole(s.w[u][f], k));
+#pragma unroll
+                    for (int j = 0; j < MF; ++j) add_scaled(acc[f][j], block_products(w, wx[j]), s.cx[u][j] * s.cw[u][f / NF]);
+                }
+            } else {
+#pragma unroll
+                for (int f = 0; f < H * NF; ++f) {
+                    const i32x8 w = whole(s.w[u][f], k);
+#pragma unroll
+                    for (int j = 0; j < MF; ++j) add_scaled(acc[f][j], block_products8(w, x[j]), s.cx[u][j] * s.cw[u][f / NF]);
+                }
+            }
+        }
+    };
+    if (b0 + wave < b1) {
+        Set one, two;
+        fetch(one, b0 + wave);
+        for (int b = b0 + wave; b < b1; b += 2 * NW * U) {
+            fetch(two, b + NW * U);
+            __builtin_amdgcn_sched_barrier(0);  // the next loads go out before the products
+            work(one, b);
+            fetch(one, b + 2 * NW * U);
+            __builtin_amdgcn_sched_barrier(0);
+            work(two, b + NW * U);
+        }
     }
 #pragma unroll
     for (int f = 0; f < H * NF; ++f)
@@ -319,18 +366,8 @@ struct Reads8 {
     }
 };
 
-// A fragment's codes as the matrix instructions take them.
-struct Wide {
-    Vec8<__bf16>::type k[4];
-    __device__ explicit Wide(i32x8 v) {
-#pragma unroll
-        for (int q = 0; q < 4; ++q) k[q] = widen(v[2 * q], v[2 * q + 1]);
-    }
-    Wide() = default;
-};
-
 template <typename T, bool GATED, bool EXACT, int BN, int BM, int WN, int WM, int S>
-__global__ __launch_bounds__(WN *WM * 64, WN * WM / 4) void k_tile8(TileArgs8) {
+__global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8) {
     using Cfg = TileCfg8<GATED, BN, BM, WN, WM, S>;
     constexpr int NW = Cfg::NW, TN = Cfg::TN, TM = Cfg::TM, TNG = GATED ? TN / 2 : TN, H = GATED ? 2 : 1;
     constexpr int NROWS = GATED ? BN / 2 : BN;  // n of a tile; gated: one half of the N side per projection
@@ -621,7 +658,7 @@ __global__ __launch_bounds__(WN *WM * 64, WN * WM / 4) void k_tile8(TileArgs8) {
         // next leaves 8 consecutive n in each lane.
         const TileArgs8 &a = args();
         const Gemm8 &g = a.g;
-        const bool eight = a.part.keep == 0 && g.q.codes;
+        const bool eight = NROWS % kBlock == 0 && a.part.keep == 0 && g.q.codes;  // smaller tiles: k_join8
         float top[TM] = {};  // largest values of this lane's rows
 #pragma unroll 1
         for (int f = 0; f < TNG / 2 * TM; ++f) {
@@ -673,6 +710,7 @@ __global__ __launch_bounds__(WN *WM * 64, WN * WM / 4) void k_tile8(TileArgs8) {
                 asm volatile("" ::"n"(i * TM + j));
             });
         }
+        if constexpr (NROWS % kBlock != 0) continue;
         if (!eight) continue;
         // a row's block lies in one wavefront, or in some neighbours
         float *all = reinterpret_cast<float *>(smem + Cfg::join_at);
@@ -688,7 +726,7 @@ __global__ __launch_bounds__(WN *WM * 64, WN * WM / 4) void k_tile8(TileArgs8) {
             for (int j = 0; j < TM; ++j)
 #pragma unroll
                 for (int w = 1; w < PER; ++w)
-                    top[j] = fmaxf(top[j], all[(wn ^ w) * BM + mrow + j * 16 + (lane & 15)]);
+                    top[j] = fmaxf(top[j], all[((wn ^ w) % WN) * BM + mrow + j * 16 + (lane & 15)]);
             lds_barrier();  // read before the next tile's are written
         }
         const int64_t nb = q.n0 + nrow;
@@ -714,16 +752,119 @@ __global__ __launch_bounds__(WN *WM * 64, WN * WM / 4) void k_tile8(TileArgs8) {
 }
 
 // ---------------------------------------------------------------- host side
-enum Path8 { kRows8, kTile8 };
+enum Path8 { kRows16, kRows32, kRows64, kTile64, kTile128, kTile256 };
 struct Plan8 {
     Path8 path;
     int split;
     int keep;  // the epilogue runs in k_join8
 };
 
+// 8-bit instructions where every result has 16 bits (8192 x 4096 x 9830: 362 us, and 585 of
+// exact products).
+bool is_exact(const Gemm8 &g) { return g.q.codes || g.e.out_f32; }
+
+// n of a tile
+int tile_rows(Path8 path, bool gated) { return (path == kTile256 ? 256 : 128) / (gated ? 2 : 1); }
+
+// Time models, microseconds, fitted to the GPU times of 19000 launches (392 sizes: 1 to 4096
+// rows, 64 to 16384 by 64 to 16384, every path in 1 to 32 parts of k; median error 3 to 12% a
+// kernel).  Over 120 other sizes the choice takes 1.02 of the best one's time on average,
+// 1.4 at most.  Sets: plain and gated, of each 8-bit instructions and exact products.
+struct RowsModel8 {
+    float launch, block;              // a launch; a block of a wavefront's k
+    float more;                       // the same for every 256 workgroups past the first
+    float in_mb;                      // a MB of operands
+    float join, join_part, join_mb;   // k_join8: a launch, a part of k, a MB of sums
+};
+constexpr int kRowsM8[3] = {16, 32, 64};
+constexpr RowsModel8 kRowsModel8[3][4] = {
+    {{3.01f, 0.646f, 1.13f, 0.13f, 1.97f, 0.27f, 6.76f},
+     {5.12f, 0.648f, 1.11f, 0.124f, 0.00119f, 0.292f, 6.91f},
+     {2.7f, 1.06f, 0.865f, 0.115f, 2.05f, 0.327f, 1.95f},
+     {4.88f, 1.06f, 0.857f, 0.109f, 0.0349f, 0.339f, 2.15f}},
+    {{2.68f, 0.764f, 0.782f, 0.117f, 1.7f, 0.278f, 2.02f},
+     {4.14f, 0.755f, 0.772f, 0.116f, 0.659f, 0.282f, 1.89f},
+     {2.88f, 1.24f, 1.06f, 0.123f, 2.12f, 0.329f, 1.43f},
+     {5.3f, 1.23f, 1.59f, 0.11f, 0.00225f, 0.343f, 1.38f}},
+    {{3.44f, 1.13f, 1.6f, 0.111f, 1.72f, 0.296f, 1.9f},
+     {0.000752f, 1.21f, 1.68f, 0.0751f, 5.53f, 0.308f, 2.4f},
+     {3.85f, 1.66f, 2.27f, 0.0926f, 2.11f, 0.347f, 1.13f},
+     {0.00258f, 1.77f, 2.27f, 0.073f, 6.14f, 0.368f, 1.36f}},
+};
+struct TileModel8 {
+    float launch, round;              // a launch; a round of tiles
+    float one, two;                   // a stage: one tile per CU, every slot taken
+    float out_mb, in_mb;              // a million results; a MB of operands
+    float join, join_part, join_mb;
+};
+struct TileShape8 {
+    int bn, bm, slots;                // tile; workgroups that the 256 CUs hold
+};
+constexpr TileShape8 kTileShape8[3] = {{128, 64, 512}, {128, 128, 512}, {256, 128, 256}};
+constexpr TileModel8 kTileModel8[3][4] = {
+    {{5.62f, 1.01f, 0.385f, 0.629f, 1.02f, 0.0406f, 1.55f, 0.288f, 0.315f},
+     {6.95f, 0.809f, 0.74f, 1.11f, 1.11f, 0.0403f, 0.777f, 0.289f, 0.297f},
+     {4.97f, 1.33f, 0.42f, 0.686f, 0.744f, 0.0411f, 1.9f, 0.325f, 0.326f},
+     {5.44f, 0.408f, 0.68f, 1.11f, 0.694f, 0.0395f, 2.61f, 0.347f, 0.358f}},
+    {{7.08f, 1.05f, 0.591f, 0.881f, 1.01f, 0.0557f, 1.29f, 0.285f, 0.291f},
+     {9.77f, 0.869f, 1.01f, 1.69f, 1.14f, 0.0334f, 0.0f, 0.267f, 0.251f},
+     {6.26f, 0.956f, 0.609f, 0.94f, 0.742f, 0.0523f, 1.66f, 0.32f, 0.313f},
+     {1.16f, 0.0521f, 1.02f, 1.71f, 0.816f, 0.0385f, 8.2f, 0.351f, 0.3f}},
+    {{6.74f, 2.3f, 9.11f, 0.741f, 1.12f, 0.0413f, 1.53f, 0.281f, 0.315f},
+     {8.84f, 2.63f, 3.43f, 1.51f, 1.26f, 0.0415f, 0.0f, 0.268f, 0.276f},
+     {6.25f, 2.09f, 10.9f, 0.81f, 0.819f, 0.046f, 2.1f, 0.311f, 0.331f},
+     {7.58f, 2.13f, 13.0f, 1.63f, 0.938f, 0.045f, 1.3f, 0.319f, 0.302f}},
+};
+
+// Do the results of a path go through k_join8?
+bool is_joined(const Gemm8 &g, Path8 path, int split) {
+    return split > 1 || (g.q.codes && (path < kTile64 || tile_rows(path, g.gated) < kBlock));
+}
+
+float rows_time(const Gemm8 &g, int i, int split) {
+    const RowsModel8 &m = kRowsModel8[i][(g.gated ? 2 : 0) + is_exact(g)];
+    const float nt = (float)((g.N + 15) / 16), mt = (float)((g.M + kRowsM8[i] - 1) / kRowsM8[i]);
+    const int64_t blocks = (g.K + kBlock - 1) / kBlock, mine = ((blocks + split - 1) / split + 7) / 8;
+    const float nn = (float)g.N * (g.gated ? 2 : 1);
+    float more = nt * mt * split / 256;
+    if (i == 2) more = ceilf(more);
+    float t = m.launch + mine * (m.block + m.more * std::max(0.0f, more - 1)) + (nt * g.M + mt * nn) * g.K * 1e-6f * m.in_mb;
+    if (is_joined(g, (Path8)i, split)) t += m.join + m.join_part * split + m.join_mb * split * g.M * nn * 4e-6f;
+    return t;
+}
+
+float tile_time(const Gemm8 &g, int i, int split) {
+    const TileModel8 &m = kTileModel8[i][(g.gated ? 2 : 0) + is_exact(g)];
+    const TileShape8 &s = kTileShape8[i];
+    const int64_t nn = g.N * (g.gated ? 2 : 1);
+    const int64_t tiles = ((g.M + s.bm - 1) / s.bm) * ((nn + s.bn - 1) / s.bn) * split, rest = tiles % s.slots;
+    const bool sparse = s.slots > 256 && rest > 0 && rest <= 256;
+    const float full = (float)(tiles / s.slots + (rest > 0 && !sparse)), last = sparse ? 1.0f : 0.0f;
+    const float stages = (float)((g.K + kBlock - 1) / kBlock) / split;
+    float t = m.launch + m.round * (full + last) + stages * (m.one * last + m.two * full) + (float)g.M * nn * 1e-6f * m.out_mb +
+              ((float)g.M + nn) * g.K * 1e-6f * m.in_mb;
+    if (is_joined(g, (Path8)(kTile64 + i), split)) t += m.join + m.join_part * split + m.join_mb * split * g.M * nn * 4e-6f;
+    return t;
+}
+
 Plan8 plan_of(const Gemm8 &g) {
-    if (g.M <= 64) return Plan8{kRows8, 1, g.q.codes != nullptr};
-    return Plan8{kTile8, 1, 0};
+    Plan8 best{kTile256, 1, 0};
+    float least = 3e38f;
+    const int64_t blocks = (g.K + kBlock - 1) / kBlock, nn = g.N * (g.gated ? 2 : 1);
+    const auto consider = [&](Path8 path, int64_t groups, auto &&time) {  // groups: workgroups with k in one part
+        for (int split = 1; split == 1 || (split <= 32 && split * 2 <= blocks && groups < 512 && groups * split <= 2048); split *= 2) {
+            const float t = time(split);
+            if (t < least) least = t, best = {path, split, is_joined(g, path, split)};
+        }
+    };
+    for (int i = 0; i < 3; ++i)  // up to 256 rows, where the models were fitted, and as many as a workgroup takes
+        if (g.M <= (i == 2 ? 256 : kRowsM8[i]))
+            consider((Path8)i, ((g.N + 15) / 16) * ((g.M + kRowsM8[i] - 1) / kRowsM8[i]), [&](int split) { return rows_time(g, i, split); });
+    for (int i = 0; i < 3; ++i) {
+        const TileShape8 &s = kTileShape8[i];
+        consider((Path8)(kTile64 + i), ((g.M + s.bm - 1) / s.bm) * ((nn + s.bn - 1) / s.bn), [&](int split) { return tile_time(g, i, split); });
+    }
+    return best;
 }
 
 size_t partial_bytes(const Gemm8 &g, const Plan8 &p) {
@@ -756,21 +897,28 @@ int launch_tiles(const Gemm8 &g, const Partial8 &q, hipStream_t stream) {
     return check_hip(hipGetLastError(), "k_tile8");
 }
 
+template <typename T, bool GATED, bool EXACT, int NF, int MF, int U>
+int launch_rows(const Gemm8 &g, const Partial8 &q, hipStream_t stream) {
+    hipLaunchKernelGGL((k_rows8<T, GATED, EXACT, NF, MF, U>), dim3((unsigned)((g.N + NF * 16 - 1) / (NF * 16)), q.split,
+                       (unsigned)((g.M + MF * 16 - 1) / (MF * 16))), dim3(512), 0, stream, g, q);
+    return check_hip(hipGetLastError(), "k_rows8");
+}
+
+template <typename T, bool GATED, bool EXACT>
+int by_path(const Gemm8 &g, const Plan8 &p, const Partial8 &q, hipStream_t stream) {
+    switch (p.path) {
+    case kRows16: return launch_rows<T, GATED, EXACT, 1, 1, GATED ? 1 : 2>(g, q, stream);
+    case kRows32: return launch_rows<T, GATED, EXACT, 1, 2, 1>(g, q, stream);
+    case kRows64: return launch_rows<T, GATED, EXACT, 1, 4, 1>(g, q, stream);
+    case kTile64: return launch_tiles<T, GATED, EXACT, 128, 64, 2, 2, 3>(g, q, stream);
+    case kTile128: return launch_tiles<T, GATED, EXACT, 128, 128, 2, 2, 2>(g, q, stream);
+    default: return launch_tiles<T, GATED, EXACT, 256, 128, 4, 2, 3>(g, q, stream);
+    }
+}
+
 template <typename T, bool GATED>
 int run(const Gemm8 &g, const Plan8 &p, const Partial8 &q, hipStream_t stream) {
-    if (p.path == kTile8) {
-        // 8-bit instructions where every result has 16 bits (8192 x 4096 x 9830: 362 us, and 585
-        // of exact products)
-        const bool exact = g.q.codes || g.e.out_f32;
-        const int rc = exact ? launch_tiles<T, GATED, true, 256, 128, 4, 2, 3>(g, q, stream)
-                             : launch_tiles<T, GATED, false, 256, 128, 4, 2, 3>(g, q, stream);
-        if (rc) return rc;
-        return q.keep ? join<T, GATED>(g, q, stream) : SA_OK;
-    }
-    constexpr int NF = 1, MF = 4;
-    hipLaunchKernelGGL((k_rows8<T, GATED, NF, MF, 1>), dim3((unsigned)((g.N + NF * 16 - 1) / (NF * 16)), q.split,
-                       (unsigned)((g.M + MF * 16 - 1) / (MF * 16))), dim3(512), 0, stream, g, q);
-    if (int rc = check_hip(hipGetLastError(), "k_rows8")) return rc;
+    if (int rc = is_exact(g) ? by_path<T, GATED, true>(g, p, q, stream) : by_path<T, GATED, false>(g, p, q, stream)) return rc;
     return q.keep ? join<T, GATED>(g, q, stream) : SA_OK;
 }
 
@@ -784,12 +932,16 @@ Gemm8 product(const sa_glu8_desc &d) {
                  Epilogue{d.act, 0, d.bg, d.bu, nullptr, 0, d.H, d.ldh, d.G, d.U, d.ldgu}, d.Q};
 }
 
-// A query that comes before the outputs is for all of them.
+// The outputs choose the plan, so a query covers each call that it holds for: with these
+// outputs or fewer, and before the outputs with any of them.
 template <typename D>
 size_t workspace(const D &d, const void *y) {
-    Gemm8 g = product(d);
-    if (!y && !g.q.codes) g.q.codes = reinterpret_cast<uint8_t *>(16);
-    return gemm8_workspace(g);
+    Gemm8 with = product(d), without = with;
+    if (!y && !with.q.codes) with.q.codes = reinterpret_cast<uint8_t *>(16);
+    without.q.codes = nullptr;
+    if (d.Q.codes && !y) return gemm8_workspace(with);
+    if (y && !d.Q.codes) return gemm8_workspace(without);
+    return std::max(gemm8_workspace(with), gemm8_workspace(without));
 }
 
 }  // namespace

@@ -154,6 +154,7 @@ def test_query_before_the_outputs(M, N, K):
         bare = ask(name, desc(None, False))
         for y, q in ((FAKE, False), (None, True), (FAKE, True)):
             assert ask(name, desc(y, q)) <= bare
+            assert y is None or ask(name, desc(y, False)) <= ask(name, desc(FAKE, True))  # fewer outputs
         before = desc(None, False)  # nor do the operands have to be there
         before.X.codes = before.X.scales = None
         assert ask(name, before) == bare
