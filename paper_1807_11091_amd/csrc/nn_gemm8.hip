@@ -263,7 +263,6 @@ __global__ __launch_bounds__(512) void k_rows8(Gemm8 g, Partial8 q) {
 template <bool GATED, int BN, int BM, int WN, int WM, int S>
 struct TileCfg8 {
     static constexpr int NW = WN * WM, NT = NW * 64;
-    static constexpr int TN = BN / WN / 16, TM = BM / WM / 16;  // fragments of a wavefront
     static constexpr int scales_at = (BN + BM) * kBlock;
     static constexpr int xl = (BM / WM + 63) / 64;              // loads of X's scales
     static constexpr int scales = xl * 256 + 16;                // bytes a wavefront: X's, then W's
@@ -344,24 +343,24 @@ struct Side8 {
     }
 };
 
-// A lane's 32 codes of a fragment of 16 rows from row0 on: chunks lane / 16 and 4 + lane / 16.
+// A lane's codes of a fragment of 16 rows from row0 on: chunks lane / 16 and 4 + lane / 16.
 struct Reads8 {
     uint32_t fo[2];
     __device__ explicit Reads8(int lane) {
         const int r = lane & 15;
 #pragma unroll
-        for (int q = 0; q < 2; ++q) fo[q] = r * kBlock + (((q * 4 + (lane >> 4)) ^ (r >> 1)) & 7) * 16;
+        for (int c = 0; c < 2; ++c) fo[c] = r * kBlock + (((c * 4 + (lane >> 4)) ^ (r >> 1)) & 7) * 16;
     }
-    __device__ i32x4 half(const uint8_t *lds, int row0, int q) const {
-        return *reinterpret_cast<const i32x4 *>(lds + fo[q] + row0 * kBlock);
+    __device__ i32x4 chunk(const uint8_t *lds, int row0, int c) const {
+        return *reinterpret_cast<const i32x4 *>(lds + fo[c] + row0 * kBlock);
     }
     __device__ i32x8 operator()(const uint8_t *lds, int row0) const {
         union {
             i32x4 h[2];
             i32x8 v;
         } x;
-#pragma unroll
-        for (int q = 0; q < 2; ++q) x.h[q] = half(lds, row0, q);
+        x.h[0] = chunk(lds, row0, 0);
+        x.h[1] = chunk(lds, row0, 1);
         return x.v;
     }
 };
@@ -369,16 +368,14 @@ struct Reads8 {
 template <typename T, bool GATED, bool EXACT, int BN, int BM, int WN, int WM, int S>
 __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8) {
     using Cfg = TileCfg8<GATED, BN, BM, WN, WM, S>;
-    constexpr int NW = Cfg::NW, TN = Cfg::TN, TM = Cfg::TM, TNG = GATED ? TN / 2 : TN, H = GATED ? 2 : 1;
+    constexpr int MI = 16;  // rows of a fragment
+    constexpr int NW = Cfg::NW, TN = BN / WN / MI, TM = BM / WM / MI, TNG = GATED ? TN / 2 : TN, H = GATED ? 2 : 1;
     constexpr int NROWS = GATED ? BN / 2 : BN;  // n of a tile; gated: one half of the N side per projection
     using NSide = Side8<NROWS, NW>;
     using MSide = Side8<BM, NW>;
     constexpr int NL = NSide::loads * H, ML = NL + MSide::loads, XL = Cfg::xl, L = ML + XL + H;  // loads of a stage
     constexpr int WROWS = NROWS / WN, MROWS = BM / WM;               // n and m of a wavefront
-    static_assert(128 % WROWS == 0 && (MROWS <= 64 || MROWS % 64 == 0) && TNG % 2 == 0 && TN >= 4 && TN % 2 == 0 && L * (S - 1) < 64, "shape");
-    constexpr int JOIN = EXACT ? TN - 2 : 0;         // the row of fragments at which the next stage is waited for
-    constexpr int RATE = (L + TN - JOIN - 1) / (TN - JOIN);  // loads that go out with each row from there on
-    constexpr int AHEAD = EXACT ? 2 : TN;            // rows of W's codes in registers
+    static_assert(128 % WROWS == 0 && (MROWS <= 64 || MROWS % 64 == 0) && TNG % 2 == 0 && TN % 2 == 0 && L * (S - 1) < 64, "shape");
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
 
     // The arguments are read anew where they are used, so that the loop over the stages has
@@ -544,104 +541,123 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8) {
         end_stage();
     }
 
-    // codes of W: row i of a stage's fragments
-    auto codes_n = [&](const uint8_t *st, int i) {
-        if constexpr (GATED) return read(st + (i >= TNG ? NSide::bytes : 0), nrow + i % TNG * 16);
-        else return read(st, nrow + i * 16);
-    };
-    i32x8 fa[AHEAD];
+    auto rows_n = [&](const uint8_t *st, int i) { return st + (GATED && i >= TNG ? NSide::bytes : 0); };
+    auto row_n = [&](int i) { return nrow + i % TNG * MI; };  // row i of a stage's fragments of W
+    auto rows_m = [&](const uint8_t *st) { return st + BN * kBlock; };
     float scale[H][TM];
-    typename std::conditional<EXACT, Wide, i32x8>::type fb[TM];
-    Vec8<__bf16>::type w[2];  // EXACT: of a row of W, one step of 32 k ahead
     auto fetch_scales = [&](const uint8_t *st) {
         const float *s = reinterpret_cast<const float *>(st + Cfg::scales_at + wave * Cfg::scales);
 #pragma unroll
         for (int h = 0; h < H; ++h)
 #pragma unroll
-            for (int j = 0; j < TM; ++j) scale[h][j] = s[j * 16 + (lane & 15)] * s[64 * XL + h];
+            for (int j = 0; j < TM; ++j) scale[h][j] = s[j * MI + (lane & (MI - 1))] * s[64 * XL + h];
     };
-    auto fetch = [&]() {  // what the first products of the stage in `slot` need
+    f32x4 part[TM];
+    auto add = [&](int i, int j) {  // beside the next row's products, not after all of them
+        add_scaled(acc[i][j], part[j], scale[GATED && i >= TNG][j]);
+        asm volatile("" : "+v"(acc[i][j]));
+    };
+    auto join = [&]() {  // the next stage has landed, `slot` before it has been read by all
+        wait_vm<L *(S - 2)>();
+        mend(slot);
+        lds_barrier();
+        begin_stage();
+    };
+
+    // 8-bit instructions.  Up to four rows of W's codes are in registers, each replaced by the
+    // one as many further on behind its last product; X's by the next stage's behind the last
+    // row's.  Where all rows are, the stage's buffer is free from its begin on.
+    constexpr int RING = TN > 4 ? 2 : TN;
+    i32x8 fa[RING], fb[TM];
+    auto fetch8 = [&]() {
         const uint8_t *st = smem + slot * Cfg::stage;
-        i32x8 raw[TM];
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) fa[i] = codes_n(st, i);
+        for (int i = 0; i < RING; ++i) fa[i] = read(rows_n(st, i), row_n(i));
 #pragma unroll
-        for (int j = 0; j < TM; ++j) raw[j] = read(st + BN * kBlock, mrow + j * 16);
+        for (int j = 0; j < TM; ++j) fb[j] = read(rows_m(st), mrow + j * MI);
         fetch_scales(st);
-        if constexpr (EXACT) w[0] = widen(fa[0][0], fa[0][1]);
-#pragma unroll
-        for (int j = 0; j < TM; ++j) {
-            if constexpr (EXACT) fb[j] = Wide(raw[j]);
-            else fb[j] = raw[j];
-        }
     };
-    // A stage is multiplied, a row of fragments at a time.  Beside a row's products stand the
-    // scaling of the row before and the widening of the next row's codes; beside the last
-    // row's the widening of the next stage's codes of X.  When the codes of the last row have
-    // been read, this stage's buffer is free and the next stage is waited for.
-    auto multiply = [&]() {
+    auto multiply8 = [&]() {
+        constexpr int JOIN = TN - RING, RATE = (L + RING - 1) / RING;  // loads that go out with a row from JOIN on
         const uint8_t *cur = smem + slot * Cfg::stage;
         slot = slot + 1 == S ? 0 : slot + 1;
         const uint8_t *nxt = smem + slot * Cfg::stage;
-        f32x4 part[TM];
-        i32x4 raw[TM];  // half of X's codes of the next stage
+        each<TN>([&](auto ic) {
+            constexpr int i = decltype(ic)::value;
+            if (i == JOIN) join();
+            if constexpr (i >= JOIN) each<RATE>([&](auto e) { load(std::integral_constant<int, (i - JOIN) * RATE + decltype(e)::value>{}); });
 #pragma unroll
-        for (int i = 0; i < TN; ++i) {
-            if (i == JOIN) {
-                wait_vm<L *(S - 2)>();
-                mend(slot);
-                lds_barrier();
-                begin_stage();
+            for (int j = 0; j < TM; ++j) {
+                if (i > 0) add(i - 1, j);
+                part[j] = block_products8(fa[i % RING], fb[j]);
+                if (i == TN - 1) fb[j] = read(rows_m(nxt), mrow + j * MI);
             }
-            if (i >= JOIN)
-                pick<TN>(i, [&](auto ic) {
-                    constexpr int at = (decltype(ic)::value - JOIN) * RATE;
-                    if constexpr (at >= 0) each<RATE>([&](auto e) { load(std::integral_constant<int, at + decltype(e)::value>{}); });
-                });
-            if constexpr (EXACT) {
+            constexpr int next = (i + RING) % TN;
+            fa[i % RING] = read(rows_n(i < JOIN ? cur : nxt, next), row_n(next));
+            __builtin_amdgcn_sched_barrier(0);
+        });
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                if (i == TN - 1 && q % 2 == 0)
-#pragma unroll
-                    for (int j = 0; j < TM; ++j) raw[j] = read.half(nxt + BN * kBlock, mrow + j * 16, q / 2);
-#pragma unroll
-                for (int j = 0; j < TM; ++j) {
-                    if (i > 0 && q == 0) add_scaled(acc[i - 1][j], part[j], scale[GATED && i - 1 >= TNG][j]);
-                    part[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[q & 1], fb[j].k[q], q ? part[j] : f32x4{}, 0, 0, 0);
-                }
-                {
-                    const i32x8 &from = fa[q < 3 ? i & 1 : (i + 1) & 1];
-                    const int at = (q + 1) % 4 * 2;
-                    w[(q + 1) & 1] = widen(from[at], from[at + 1]);
-                }
-                if (i == TN - 1)
-#pragma unroll
-                    for (int j = 0; j < TM; ++j) fb[j].k[q] = widen(raw[j][q % 2 * 2], raw[j][q % 2 * 2 + 1]);
-                // two rows ahead, in the end the next stage's first two
-                if (q == 3) fa[i & 1] = i + 2 < TN ? codes_n(cur, i + 2) : codes_n(nxt, i + 2 - TN);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            } else {
-#pragma unroll
-                for (int j = 0; j < TM; ++j) {
-                    if (i > 0) {
-                        add_scaled(acc[i - 1][j], part[j], scale[GATED && i - 1 >= TNG][j]);
-                        asm volatile("" : "+v"(acc[i - 1][j]));  // here, and not when all rows' products are there
-                    }
-                    part[j] = block_products8(fa[i], fb[j]);
-                    if (i == TN - 1) fb[j] = read(nxt + BN * kBlock, mrow + j * 16);
-                }
-                fa[i] = codes_n(nxt, i);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < TM; ++j) add_scaled(acc[TN - 1][j], part[j], scale[GATED][j]);
+        for (int j = 0; j < TM; ++j) add(TN - 1, j);
         fetch_scales(nxt);
         end_stage();
     };
 
-    const int nl = ((lane >> 4) & 1) * 16 + (lane >> 5) * 8;  // this lane's 8 n of two fragments, see below
+    // Exact products, in four steps of 32 k a row.  X's codes are widened once a stage, the
+    // next stage's in place beside the last row's products, W's a step ahead; W's codes are
+    // read two rows ahead.
+    typedef Vec8<__bf16>::type Vec;
+    i32x8 ra[2];
+    Vec wa[2];
+    Wide wb[TM];
+    auto fetch_exact = [&]() {
+        const uint8_t *st = smem + slot * Cfg::stage;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) ra[i] = read(rows_n(st, i), row_n(i));
+#pragma unroll
+        for (int j = 0; j < TM; ++j) wb[j] = Wide(read(rows_m(st), mrow + j * MI));
+        wa[0] = widen(ra[0][0], ra[0][1]);
+        fetch_scales(st);
+    };
+    auto multiply_exact = [&]() {
+        constexpr int JOIN = TN - 2, RATE = (L + 1) / 2;  // loads that go out with each of the last two rows
+        const uint8_t *cur = smem + slot * Cfg::stage;
+        slot = slot + 1 == S ? 0 : slot + 1;
+        const uint8_t *nxt = smem + slot * Cfg::stage;
+        i32x4 raw[TM];  // half of X's codes of the next stage
+        each<TN>([&](auto ic) {
+            constexpr int i = decltype(ic)::value;
+            if (i == JOIN) join();
+            if constexpr (i >= JOIN) each<RATE>([&](auto e) { load(std::integral_constant<int, (i - JOIN) * RATE + decltype(e)::value>{}); });
+            each<4>([&](auto qc) {
+                constexpr int q = decltype(qc)::value;
+                if (i == TN - 1 && q % 2 == 0)
+#pragma unroll
+                    for (int j = 0; j < TM; ++j) raw[j] = read.chunk(rows_m(nxt), mrow + j * MI, q / 2);
+#pragma unroll
+                for (int j = 0; j < TM; ++j) {
+                    if (i > 0 && q == 0) add(i - 1, j);
+                    part[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wa[q & 1], wb[j].k[q], q ? part[j] : f32x4{}, 0, 0, 0);
+                }
+                const i32x8 &from = ra[q < 3 ? i & 1 : (i + 1) & 1];
+                constexpr int at = (q + 1) % 4 * 2;
+                wa[(q + 1) & 1] = widen(from[at], from[at + 1]);
+                if (i == TN - 1)
+#pragma unroll
+                    for (int j = 0; j < TM; ++j) wb[j].k[q] = widen(raw[j][q % 2 * 2], raw[j][q % 2 * 2 + 1]);
+                constexpr int next = (i + 2) % TN;
+                if (q == 3) ra[i & 1] = read(rows_n(i < JOIN ? cur : nxt, next), row_n(next));
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        });
+#pragma unroll
+        for (int j = 0; j < TM; ++j) add(TN - 1, j);
+        fetch_scales(nxt);
+        end_stage();
+    };
+
+    // this lane's first n of two fragments, see below, and its m
+    const int nl = ((lane >> 4) & 1) * 16 + (lane >> 5) * 8, ml = lane & 15;
+    constexpr int PN = TNG / 2;  // pairs of fragments
 #pragma unroll 1
     for (int ti = 0; ti < mine; ++ti) {
         const Tile q = tile_at(ti);
@@ -649,39 +665,45 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8) {
         for (int i = 0; i < TN; ++i)
 #pragma unroll
             for (int j = 0; j < TM; ++j) acc[i][j] = f32x4{};
-        if (q.s0 < q.s1) fetch();
+        if constexpr (EXACT) {
+            if (q.s0 < q.s1) fetch_exact();
 #pragma unroll 1
-        for (int s = q.s0; s < q.s1; ++s) multiply();
+            for (int s = q.s0; s < q.s1; ++s) multiply_exact();
+        } else {
+            if (q.s0 < q.s1) fetch8();
+#pragma unroll 1
+            for (int s = q.s0; s < q.s1; ++s) multiply8();
+        }
 
         // Results straight from the registers.  A lane holds 4 consecutive n of every 16;
-        // exchanging the odd rows of 16 lanes of one such group with the even ones of the
-        // next leaves 8 consecutive n in each lane.
+        // exchanging the odd rows of 16 lanes of one such group with the even ones of the next
+        // leaves 8 consecutive n in each lane.
         const TileArgs8 &a = args();
         const Gemm8 &g = a.g;
-        const bool eight = NROWS % kBlock == 0 && a.part.keep == 0 && g.q.codes;  // smaller tiles: k_join8
+        constexpr bool EIGHT = EXACT && NROWS % kBlock == 0;  // smaller tiles: k_join8
+        const bool eight = EIGHT && a.part.keep == 0 && g.q.codes;
         float top[TM] = {};  // largest values of this lane's rows
 #pragma unroll 1
-        for (int f = 0; f < TNG / 2 * TM; ++f) {
-            f32x4 t[H][2];
-            pick<TNG / 2 * TM>(f, [&](auto fc) {
-                constexpr int i = decltype(fc)::value / TM * 2, j = decltype(fc)::value % TM;
-#pragma unroll
-                for (int h = 0; h < H; ++h) {
-                    t[h][0] = acc[h * TNG + i][j];
-                    t[h][1] = acc[h * TNG + i + 1][j];
-                }
-                asm volatile("" ::"n"(i * TM + j));  // keeps the compiler from merging the branches, which would index registers
-            });
+        for (int f = 0; f < PN * TM; ++f) {
             float z[8], u[8];
+            pick<PN * TM>(f, [&](auto fc) {
+                constexpr int p = decltype(fc)::value / TM, j = decltype(fc)::value % TM;
+#pragma unroll
+                for (int h = 0; h < H; ++h)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) (h ? u : z)[e] = acc[h * TNG + 2 * p + e / 4][j][e % 4];
+                asm volatile("" ::"n"(p * TM + j));  // keeps the compiler from merging the branches, which would index registers
+            });
 #pragma unroll
             for (int h = 0; h < H; ++h)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const auto w = __builtin_amdgcn_permlane16_swap(__float_as_uint(t[h][0][e]), __float_as_uint(t[h][1][e]), false, false);
-                    (h ? u : z)[e] = __uint_as_float(w[0]);
-                    (h ? u : z)[e + 4] = __uint_as_float(w[1]);
+                    float *v = h ? u : z;
+                    const auto w = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[e]), __float_as_uint(v[e + 4]), false, false);
+                    v[e] = __uint_as_float(w[0]);
+                    v[e + 4] = __uint_as_float(w[1]);
                 }
-            const int64_t m = q.m0 + mrow + f % TM * 16 + (lane & 15), n = q.n0 + nrow + f / TM * 32 + nl;
+            const int64_t m = q.m0 + mrow + f % TM * MI + ml, n = q.n0 + nrow + f / TM * 32 + nl;
             const int cnt = m < g.M ? (int)max((int64_t)0, min((int64_t)8, g.N - n)) : 0;
             if (cnt > 0) {
                 if (a.part.keep) {
@@ -695,29 +717,27 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8) {
                     if (g.e.Y) put_values<T, 8>(g.e, g.e.Y, m, n, cnt, z);
                 }
             }
+            if constexpr (!EIGHT) continue;
             if (!eight) continue;
 #pragma unroll
             for (int e = 0; e < 8; ++e) z[e] = e < cnt ? z[e] : 0.0f;
             const float most = largest(z);
-            pick<TNG / 2 * TM>(f, [&](auto fc) {
-                constexpr int i = decltype(fc)::value / TM * 2, j = decltype(fc)::value % TM;
+            pick<PN * TM>(f, [&](auto fc) {
+                constexpr int p = decltype(fc)::value / TM, j = decltype(fc)::value % TM;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    acc[i][j][e] = z[e];
-                    acc[i + 1][j][e] = z[e + 4];
-                }
+                for (int e = 0; e < 8; ++e) acc[2 * p + e / 4][j][e % 4] = z[e];
                 top[j] = fmaxf(top[j], most);
-                asm volatile("" ::"n"(i * TM + j));
+                asm volatile("" ::"n"(p * TM + j));
             });
         }
-        if constexpr (NROWS % kBlock != 0) continue;
+        if constexpr (!EIGHT) continue;
         if (!eight) continue;
         // a row's block lies in one wavefront, or in some neighbours
         float *all = reinterpret_cast<float *>(smem + Cfg::join_at);
 #pragma unroll
         for (int j = 0; j < TM; ++j) {
-            top[j] = lanes_max<16, 64>(top[j]);
-            if (WROWS < kBlock && lane < 16) all[wn * BM + mrow + j * 16 + lane] = top[j];
+            top[j] = lanes_max<MI, 64>(top[j]);
+            if (WROWS < kBlock && lane < MI) all[wn * BM + mrow + j * MI + lane] = top[j];
         }
         if constexpr (WROWS < kBlock) {
             constexpr int PER = kBlock / WROWS;  // wavefronts a block
@@ -726,26 +746,25 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8) {
             for (int j = 0; j < TM; ++j)
 #pragma unroll
                 for (int w = 1; w < PER; ++w)
-                    top[j] = fmaxf(top[j], all[((wn ^ w) % WN) * BM + mrow + j * 16 + (lane & 15)]);
+                    top[j] = fmaxf(top[j], all[((wn ^ w) % WN) * BM + mrow + j * MI + ml]);
             lds_barrier();  // read before the next tile's are written
         }
         const int64_t nb = q.n0 + nrow;
 #pragma unroll
         for (int j = 0; j < TM; ++j) {
-            const int64_t m = q.m0 + mrow + j * 16 + (lane & 15);
+            const int64_t m = q.m0 + mrow + j * MI + ml;
             const float s = block_scale(top[j]), inv = 1.0f / s;
             if (m >= g.M) continue;
-            if (nb % kBlock == 0 && lane < 16 && nb < g.N) g.q.scales[m * g.q.scale_row + nb / kBlock * g.q.scale_col] = s;
-#pragma unroll
-            for (int i = 0; i < TNG; i += 2) {
-                const int64_t n = nb + i * 16 + nl;
+            if (nb % kBlock == 0 && lane < MI && nb < g.N) g.q.scales[m * g.q.scale_row + nb / kBlock * g.q.scale_col] = s;
+            each<PN>([&](auto pc) {
+                const int64_t n = nb + decltype(pc)::value * 32 + nl;
                 const int cnt = (int)min((int64_t)8, g.N - n);
-                if (cnt <= 0) continue;
+                if (cnt <= 0) return;
                 float z[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) z[e] = acc[i + e / 4][j][e % 4];
+                for (int e = 0; e < 8; ++e) z[e] = acc[2 * decltype(pc)::value + e / 4][j][e % 4];
                 store_codes(g.q.codes + m * g.q.ld + n, cnt, codes8(z, inv));
-            }
+            });
         }
     }
     wait_vm<0>();  // the loads past the last stage still write to LDS
@@ -912,7 +931,9 @@ int by_path(const Gemm8 &g, const Plan8 &p, const Partial8 &q, hipStream_t strea
     case kRows64: return launch_rows<T, GATED, EXACT, 1, 4, 1>(g, q, stream);
     case kTile64: return launch_tiles<T, GATED, EXACT, 128, 64, 2, 2, 3>(g, q, stream);
     case kTile128: return launch_tiles<T, GATED, EXACT, 128, 128, 2, 2, 2>(g, q, stream);
-    default: return launch_tiles<T, GATED, EXACT, 256, 128, 4, 2, 3>(g, q, stream);
+    default:
+        if constexpr (GATED || EXACT) return launch_tiles<T, GATED, EXACT, 256, 128, 4, 2, 3>(g, q, stream);
+        else return launch_tiles<T, GATED, EXACT, 256, 256, 2, 4, 2>(g, q, stream);
     }
 }
 
