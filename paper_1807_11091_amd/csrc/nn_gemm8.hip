@@ -655,8 +655,6 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8) {
         end_stage();
     };
 
-    // this lane's first n of two fragments, see below, and its m
-    const int nl = ((lane >> 4) & 1) * 16 + (lane >> 5) * 8, ml = lane & 15;
     constexpr int PN = TNG / 2;  // pairs of fragments
 #pragma unroll 1
     for (int ti = 0; ti < mine; ++ti) {
@@ -680,6 +678,10 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8) {
         // leaves 8 consecutive n in each lane.
         const TileArgs8 &a = args();
         const Gemm8 &g = a.g;
+        int el = lane;
+        asm volatile("" : "+v"(el));  // what follows from it takes no registers before
+        // this lane's first n of two fragments and its m
+        const int nl = ((el >> 4) & 1) * 16 + (el >> 5) * 8, ml = el & 15;
         constexpr bool EIGHT = EXACT && NROWS % kBlock == 0;  // smaller tiles: k_join8
         const bool eight = EIGHT && a.part.keep == 0 && g.q.codes;
         float top[TM] = {};  // largest values of this lane's rows
@@ -737,7 +739,7 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8) {
 #pragma unroll
         for (int j = 0; j < TM; ++j) {
             top[j] = lanes_max<MI, 64>(top[j]);
-            if (WROWS < kBlock && lane < MI) all[wn * BM + mrow + j * MI + lane] = top[j];
+            if (WROWS < kBlock && el < MI) all[wn * BM + mrow + j * MI + el] = top[j];
         }
         if constexpr (WROWS < kBlock) {
             constexpr int PER = kBlock / WROWS;  // wavefronts a block
@@ -755,7 +757,7 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8) {
             const int64_t m = q.m0 + mrow + j * MI + ml;
             const float s = block_scale(top[j]), inv = 1.0f / s;
             if (m >= g.M) continue;
-            if (nb % kBlock == 0 && lane < MI && nb < g.N) g.q.scales[m * g.q.scale_row + nb / kBlock * g.q.scale_col] = s;
+            if (nb % kBlock == 0 && el < MI && nb < g.N) g.q.scales[m * g.q.scale_row + nb / kBlock * g.q.scale_col] = s;
             each<PN>([&](auto pc) {
                 const int64_t n = nb + decltype(pc)::value * 32 + nl;
                 const int cnt = (int)min((int64_t)8, g.N - n);
@@ -771,7 +773,7 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8) {
 }
 
 // ---------------------------------------------------------------- host side
-enum Path8 { kRows16, kRows32, kRows64, kTile64, kTile128, kTile256 };
+enum Path8 { kRows16, kRows32, kRows64, kTile64, kTile128, kTile256, kTile256x256 };
 struct Plan8 {
     Path8 path;
     int split;
@@ -783,7 +785,7 @@ struct Plan8 {
 bool is_exact(const Gemm8 &g) { return g.q.codes || g.e.out_f32; }
 
 // n of a tile
-int tile_rows(Path8 path, bool gated) { return (path == kTile256 ? 256 : 128) / (gated ? 2 : 1); }
+int tile_rows(Path8 path, bool gated) { return (path >= kTile256 ? 256 : 128) / (gated ? 2 : 1); }
 
 // Time models, microseconds, fitted to the GPU times of 19000 launches (392 sizes: 1 to 4096
 // rows, 64 to 16384 by 64 to 16384, every path in 1 to 32 parts of k; median error 3 to 12% a
@@ -797,18 +799,18 @@ struct RowsModel8 {
 };
 constexpr int kRowsM8[3] = {16, 32, 64};
 constexpr RowsModel8 kRowsModel8[3][4] = {
-    {{3.01f, 0.646f, 1.13f, 0.13f, 1.97f, 0.27f, 6.76f},
-     {5.12f, 0.648f, 1.11f, 0.124f, 0.00119f, 0.292f, 6.91f},
-     {2.7f, 1.06f, 0.865f, 0.115f, 2.05f, 0.327f, 1.95f},
-     {4.88f, 1.06f, 0.857f, 0.109f, 0.0349f, 0.339f, 2.15f}},
-    {{2.68f, 0.764f, 0.782f, 0.117f, 1.7f, 0.278f, 2.02f},
-     {4.14f, 0.755f, 0.772f, 0.116f, 0.659f, 0.282f, 1.89f},
-     {2.88f, 1.24f, 1.06f, 0.123f, 2.12f, 0.329f, 1.43f},
-     {5.3f, 1.23f, 1.59f, 0.11f, 0.00225f, 0.343f, 1.38f}},
-    {{3.44f, 1.13f, 1.6f, 0.111f, 1.72f, 0.296f, 1.9f},
-     {0.000752f, 1.21f, 1.68f, 0.0751f, 5.53f, 0.308f, 2.4f},
-     {3.85f, 1.66f, 2.27f, 0.0926f, 2.11f, 0.347f, 1.13f},
-     {0.00258f, 1.77f, 2.27f, 0.073f, 6.14f, 0.368f, 1.36f}},
+    {{3.05f, 0.667f, 1.08f, 0.133f, 1.89f, 0.27f, 6.97f},
+     {0.000699f, 0.665f, 1.02f, 0.124f, 5.13f, 0.29f, 7.31f},
+     {2.7f, 1.08f, 0.846f, 0.112f, 2.02f, 0.32f, 2.2f},
+     {4.85f, 1.08f, 0.811f, 0.108f, 0.0411f, 0.334f, 2.35f}},
+    {{2.69f, 0.759f, 0.71f, 0.128f, 1.65f, 0.279f, 2.13f},
+     {0.0083f, 0.757f, 0.717f, 0.123f, 4.77f, 0.281f, 2.1f},
+     {2.9f, 1.24f, 0.991f, 0.126f, 2.05f, 0.327f, 1.55f},
+     {0.231f, 1.24f, 1.53f, 0.11f, 5.08f, 0.335f, 1.59f}},
+    {{3.48f, 1.12f, 1.59f, 0.113f, 1.69f, 0.294f, 1.84f},
+     {0.000386f, 1.2f, 1.67f, 0.0775f, 5.55f, 0.305f, 2.34f},
+     {3.91f, 1.64f, 2.24f, 0.0949f, 2.04f, 0.344f, 1.13f},
+     {0.000244f, 1.75f, 2.24f, 0.076f, 6.16f, 0.362f, 1.37f}},
 };
 struct TileModel8 {
     float launch, round;              // a launch; a round of tiles
@@ -819,20 +821,24 @@ struct TileModel8 {
 struct TileShape8 {
     int bn, bm, slots;                // tile; workgroups that the 256 CUs hold
 };
-constexpr TileShape8 kTileShape8[3] = {{128, 64, 512}, {128, 128, 512}, {256, 128, 256}};
-constexpr TileModel8 kTileModel8[3][4] = {
-    {{5.62f, 1.01f, 0.385f, 0.629f, 1.02f, 0.0406f, 1.55f, 0.288f, 0.315f},
-     {6.95f, 0.809f, 0.74f, 1.11f, 1.11f, 0.0403f, 0.777f, 0.289f, 0.297f},
-     {4.97f, 1.33f, 0.42f, 0.686f, 0.744f, 0.0411f, 1.9f, 0.325f, 0.326f},
-     {5.44f, 0.408f, 0.68f, 1.11f, 0.694f, 0.0395f, 2.61f, 0.347f, 0.358f}},
-    {{7.08f, 1.05f, 0.591f, 0.881f, 1.01f, 0.0557f, 1.29f, 0.285f, 0.291f},
-     {9.77f, 0.869f, 1.01f, 1.69f, 1.14f, 0.0334f, 0.0f, 0.267f, 0.251f},
-     {6.26f, 0.956f, 0.609f, 0.94f, 0.742f, 0.0523f, 1.66f, 0.32f, 0.313f},
-     {1.16f, 0.0521f, 1.02f, 1.71f, 0.816f, 0.0385f, 8.2f, 0.351f, 0.3f}},
-    {{6.74f, 2.3f, 9.11f, 0.741f, 1.12f, 0.0413f, 1.53f, 0.281f, 0.315f},
-     {8.84f, 2.63f, 3.43f, 1.51f, 1.26f, 0.0415f, 0.0f, 0.268f, 0.276f},
-     {6.25f, 2.09f, 10.9f, 0.81f, 0.819f, 0.046f, 2.1f, 0.311f, 0.331f},
-     {7.58f, 2.13f, 13.0f, 1.63f, 0.938f, 0.045f, 1.3f, 0.319f, 0.302f}},
+constexpr TileShape8 kTileShape8[4] = {{128, 64, 512}, {128, 128, 512}, {256, 128, 256}, {256, 256, 256}};
+constexpr TileModel8 kTileModel8[4][4] = {
+    {{5.5f, 1.06f, 0.384f, 0.633f, 1.01f, 0.0397f, 1.5f, 0.288f, 0.319f},
+     {6.95f, 1.06f, 0.703f, 1.1f, 1.21f, 0.0378f, 0.674f, 0.291f, 0.294f},
+     {5.1f, 1.3f, 0.405f, 0.675f, 0.745f, 0.0442f, 1.84f, 0.325f, 0.34f},
+     {3.8f, 0.209f, 0.716f, 1.13f, 0.489f, 0.0393f, 4.46f, 0.344f, 0.386f}},
+    {{7.34f, 0.581f, 0.577f, 0.912f, 0.977f, 0.0585f, 1.2f, 0.282f, 0.31f},
+     {10.0f, 0.917f, 1.02f, 1.7f, 1.18f, 0.0287f, 0.0f, 0.255f, 0.25f},
+     {6.56f, 0.843f, 0.618f, 0.955f, 0.738f, 0.0544f, 1.55f, 0.321f, 0.318f},
+     {8.6f, 0.0f, 1.05f, 1.74f, 0.607f, 0.0372f, 0.834f, 0.349f, 0.321f}},
+    {{6.94f, 2.05f, 2.92f, 0.737f, 1.02f, 0.0395f, 1.4f, 0.279f, 0.332f},
+     {8.96f, 2.69f, 2.25f, 1.53f, 1.17f, 0.0361f, 0.0f, 0.262f, 0.28f},
+     {6.55f, 1.63f, 3.06f, 0.816f, 0.796f, 0.0484f, 1.89f, 0.317f, 0.338f},
+     {8.13f, 1.81f, 3.55f, 1.64f, 0.97f, 0.0487f, 1.02f, 0.325f, 0.304f}},
+    {{8.41f, 4.36f, 5.62f, 1.39f, 1.02f, 0.0583f, 0.571f, 0.276f, 0.282f},
+     {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f},
+     {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f},
+     {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f}},
 };
 
 // Do the results of a path go through k_join8?
@@ -879,7 +885,7 @@ Plan8 plan_of(const Gemm8 &g) {
     for (int i = 0; i < 3; ++i)  // up to 256 rows, where the models were fitted, and as many as a workgroup takes
         if (g.M <= (i == 2 ? 256 : kRowsM8[i]))
             consider((Path8)i, ((g.N + 15) / 16) * ((g.M + kRowsM8[i] - 1) / kRowsM8[i]), [&](int split) { return rows_time(g, i, split); });
-    for (int i = 0; i < 3; ++i) {
+    for (int i = 0; i < (g.gated || is_exact(g) ? 3 : 4); ++i) {
         const TileShape8 &s = kTileShape8[i];
         consider((Path8)(kTile64 + i), ((g.M + s.bm - 1) / s.bm) * ((nn + s.bn - 1) / s.bn), [&](int split) { return tile_time(g, i, split); });
     }
@@ -931,9 +937,9 @@ int by_path(const Gemm8 &g, const Plan8 &p, const Partial8 &q, hipStream_t strea
     case kRows64: return launch_rows<T, GATED, EXACT, 1, 4, 1>(g, q, stream);
     case kTile64: return launch_tiles<T, GATED, EXACT, 128, 64, 2, 2, 3>(g, q, stream);
     case kTile128: return launch_tiles<T, GATED, EXACT, 128, 128, 2, 2, 2>(g, q, stream);
-    default:
-        if constexpr (GATED || EXACT) return launch_tiles<T, GATED, EXACT, 256, 128, 4, 2, 3>(g, q, stream);
-        else return launch_tiles<T, GATED, EXACT, 256, 256, 2, 4, 2>(g, q, stream);
+    case kTile256x256:
+        if constexpr (!GATED && !EXACT) return launch_tiles<T, GATED, EXACT, 256, 256, 2, 4, 2>(g, q, stream);
+    default: return launch_tiles<T, GATED, EXACT, 256, 128, 4, 2, 3>(g, q, stream);
     }
 }
 
