@@ -912,10 +912,11 @@ def _matrix8(m, rows: int, cols: int, block_rows: int, dev, what: str) -> Matrix
 
 def _codes_of(m, what: str):
     """The [rows, cols] of an 8-bit operand in GPU memory."""
-    if not isinstance(m, (tuple, list)) or len(m) != 2 or m[0].dim() != 2 or not m[0].is_cuda:
+    if type(m) is not Matrix8 or m.codes.dim() != 2 or not m.codes.is_cuda:
         raise StructAdmmError(f"{what} must be a Matrix8 in GPU memory")
-    _type_code(m[1], what)
-    return m[0].shape
+    if not _type_codes:
+        _type_code(m.scales, what)
+    return m.codes.shape
 
 
 def rms_norm_fwd(X, gamma=None, R=None, eps: float = 1e-5, S=None, Y=None, Q=None, rstd=None, out: str = "ysr",
@@ -988,12 +989,6 @@ def quantize8(X, block_rows: int = 1, Q=None, QT=None, out: str = "q", stream=No
     return Q, QT
 
 
-def _type16(t, what: str) -> Optional[int]:
-    """bfloat16's or float16's code of an output that may be None or float32 (None)."""
-    code = None if t is None else _type_code(t, what)
-    return None if code == F32 else code
-
-
 def linear8_fwd(X, W, bias=None, R=None, act: int = ACT_NONE, Y=None, Z=None, Q=None, out_dtype=None, out: str = "y",
                 ws=None, stream=None):
     """structadmm_linear8_fwd: act(X W^T + bias) + R for 8-bit X [M, K] (row blocks) and W
@@ -1011,8 +1006,10 @@ def linear8_fwd(X, W, bias=None, R=None, act: int = ACT_NONE, Y=None, Z=None, Q=
         Y = _new(stream, X[0], M, N, out_dtype or like)
     if Q is None and "q" in out:
         Q = matrix8(M, N, 1, dev, stream)
-    code = next((c for c in (_type16(Z, w + "Z"), _type16(Y, w + "Y"), _type16(R, w + "R")) if c is not None), BF16)
-    to = code if Y is None and R is None else _type_code(R if Y is None else Y, w + "Y")
+    to = BF16 if Y is None and R is None else _type_code(R if Y is None else Y, w + "Y")
+    code = _type_code(Z, w + "Z") if Z is not None else BF16 if to == F32 else to
+    if Y is None and R is None:
+        to = code
     r, ldr = _optional(R, M, N, to, dev, w + "R")
     y, ldy = _optional(Y, M, N, to, dev, w + "Y")
     z, ldz = _optional(Z, M, N, code, dev, w + "Z")

@@ -755,7 +755,7 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8) {
 #pragma unroll
         for (int j = 0; j < TM; ++j) {
             const int64_t m = q.m0 + mrow + j * MI + ml;
-            const float s = block_scale(top[j]), inv = 1.0f / s;
+            const float s = block_scale(top[j]), inv = block_inverse(s);
             if (m >= g.M) continue;
             if (nb % kBlock == 0 && el < MI && nb < g.N) g.q.scales[m * g.q.scale_row + nb / kBlock * g.q.scale_col] = s;
             each<PN>([&](auto pc) {
