@@ -729,7 +729,7 @@ typedef struct sa_matrix8 {
  * S = X + R, rounded to its type (S = X where R is NULL),
  * Y[r][c] = S[r][c] * rstd[r] * gamma[c], rstd[r] = 1 / sqrt(sum_c S[r][c]^2 / cols + eps).
  * gamma NULL stands for ones.  S, Y, Q and rstd may each be left out (NULL; at least
- * one of S, Y and Q is given): Y receives the result in the inputs' type, Q in 8 bits
+ * one is given): Y receives the result in the inputs' type, Q in 8 bits
  * with row blocks, both from the same binary32 values.  S may be X or R itself, and Y
  * one of them that S is not, with the same pitch.
  */

@@ -904,10 +904,10 @@ def _matrix8(m, rows: int, cols: int, block_rows: int, dev, what: str) -> Matrix
     ld, step = codes.stride()
     if step != 1 and cols > 1 and rows > 0:
         raise StructAdmmError(f"{what} must have unit column stride")
-    if rows <= 1 and (ld < cols or ld % 16 or ld > MAX_LD):
+    if cols == 0 or rows <= 1 and (ld < cols or ld % 16 or ld > MAX_LD):
         ld = (cols + 15) // 16 * 16  # a single row has no pitch
     row, col = scales.stride()
-    return Matrix8Arg(codes.data_ptr(), ld, scales.data_ptr(), row if nr > 1 else 1, col if nc > 1 else 1)
+    return Matrix8Arg(codes.data_ptr(), ld, scales.data_ptr(), row if nr > 1 and nc else 1, col if nc > 1 and nr else 1)
 
 
 def _codes_of(m, what: str):

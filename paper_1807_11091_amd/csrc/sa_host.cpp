@@ -486,7 +486,8 @@ int validate_rms_norm(const sa_rms_norm_desc &d) {
     SA_TRY(check_matrix8(w, "Q", d.Q, false, d.rows, d.cols, 1, true, true));
     SA_TRY(check_vector(w, "gamma", d.gamma));
     SA_TRY(check_vector(w, "rstd", d.rstd));
-    if (!d.S && !d.Y && !d.Q.codes && d.rows > 0) return fail(SA_E_ARG, "%s: nothing to do (S, Y and Q are NULL)", w);
+    if (!d.S && !d.Y && !d.Q.codes && !d.rstd && d.rows > 0)
+        return fail(SA_E_ARG, "%s: nothing to do (S, Y, Q and rstd are NULL)", w);
     SA_TRY(check_alias(w, "S and X with another pitch", d.S, d.X, d.lds == d.ldx));
     SA_TRY(check_alias(w, "S and R with another pitch", d.S, d.R, d.lds == d.ldr));
     SA_TRY(check_alias(w, "Y and X with another pitch", d.Y, d.X, d.ldy == d.ldx));

@@ -68,7 +68,7 @@ REFUSED = [
     ("rms_norm_fwd", dict(rows=-1), -1), ("rms_norm_fwd", dict(cols=0), -1), ("rms_norm_fwd", dict(type=3), -1),
     ("rms_norm_fwd", dict(X=None), -1), ("rms_norm_fwd", dict(eps=-1.0), -1), ("rms_norm_fwd", dict(eps=float("nan")), -1),
     ("rms_norm_fwd", dict(ldr=7), -1), ("rms_norm_fwd", dict(X=FAKE + 1), -2), ("rms_norm_fwd", dict(gamma=FAKE + 2), -2),
-    ("rms_norm_fwd", dict(S=None, Y=None, Q=NONE), -1), ("rms_norm_fwd", dict(S=20 * FAKE, lds=9), -1),
+    ("rms_norm_fwd", dict(S=None, Y=None, Q=NONE, rstd=None), -1), ("rms_norm_fwd", dict(S=20 * FAKE, lds=9), -1),
     ("rms_norm_fwd", dict(S=21 * FAKE, lds=9), -1), ("rms_norm_fwd", dict(Y=23 * FAKE), -1),
     ("rms_norm_fwd", dict(Q=eight(1, 24)), -2), ("rms_norm_fwd", dict(Q=eight(1, 0)), -1),
     ("rms_norm_fwd", dict(Q=sa.Matrix8Arg(FAKE + 8, 16, 2 * FAKE, 1, 4)), -2),
