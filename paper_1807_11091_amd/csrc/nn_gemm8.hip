@@ -112,11 +112,14 @@ __global__ __launch_bounds__(256) void k_join8(Gemm8 g, Partial8 q, int64_t firs
 // ------------------------------------------------------------- few rows of M
 // k_rows8: products with few rows of M, bound by reading the weights once and by latency.
 // A workgroup of 8 wavefronts takes NF * 16 of their rows and MF * 16 of M; its wavefronts
-// take the blocks of k in turn, U at a time with the next U on their way, and feed the
-// matrix cores straight from memory.  Their sums are joined through LDS in a fixed order.
-// Rows past M or N read the last row and are not stored.
-template <typename T, bool GATED, bool EXACT, int NF, int MF, int U>
-__global__ __launch_bounds__(512) void k_rows8(Gemm8 g, Partial8 q) {
+// take the blocks of k in turn, U at a time, and feed the matrix cores straight from memory.
+// Their sums are joined through LDS in a fixed order.  Rows past M or N read the last row and
+// are not stored.  What hides the memory's latency is the other wavefronts of the CU: PER of
+// them a SIMD.  With the next blocks on their way in a second set of registers and two
+// workgroups a CU instead of three, 1 x 4096 x 9830 took 11.0 us instead of 9.5 (4.3 TB/s of
+// weights), 16 x 9830 x 4096 18.5 instead of 13.9, gated 23.0 instead of 19.9.
+template <typename T, bool GATED, bool EXACT, int NF, int MF, int U, int PER>
+__global__ __launch_bounds__(512, PER) void k_rows8(Gemm8 g, Partial8 q) {
     constexpr int NW = 8, H = GATED ? 2 : 1;
     static_assert(128 % (NF * 16) == 0, "one block row");
     __shared__ float sums[NW][NF * H * MF][256];
@@ -212,15 +215,11 @@ __global__ __launch_bounds__(512) void k_rows8(Gemm8 g, Partial8 q) {
         }
     };
     if (b0 + wave < b1) {
-        Set one, two;
-        fetch(one, b0 + wave);
-        for (int b = b0 + wave; b < b1; b += 2 * NW * U) {
-            fetch(two, b + NW * U);
-            __builtin_amdgcn_sched_barrier(0);  // the next loads go out before the products
-            work(one, b);
-            fetch(one, b + 2 * NW * U);
-            __builtin_amdgcn_sched_barrier(0);
-            work(two, b + NW * U);
+        Set set;
+        for (int b = b0 + wave; b < b1; b += NW * U) {
+            fetch(set, b);
+            __builtin_amdgcn_sched_barrier(0);  // every load goes out before the first product
+            work(set, b);
         }
     }
 #pragma unroll
@@ -787,10 +786,10 @@ bool is_exact(const Gemm8 &g) { return g.q.codes || g.e.out_f32; }
 // n of a tile
 int tile_rows(Path8 path, bool gated) { return (path >= kTile256 ? 256 : 128) / (gated ? 2 : 1); }
 
-// Time models, microseconds, fitted to the GPU times of 19000 launches (392 sizes: 1 to 4096
+// Time models, microseconds, fitted to the GPU times of 23000 launches (440 sizes: 1 to 4096
 // rows, 64 to 16384 by 64 to 16384, every path in 1 to 32 parts of k; median error 3 to 12% a
-// kernel).  Over 120 other sizes the choice takes 1.02 of the best one's time on average,
-// 1.4 at most.  Sets: plain and gated, of each 8-bit instructions and exact products.
+// kernel).  Over 140 other sizes the choice takes 1.02 of the best one's time on average,
+// 1.3 at most.  Sets: plain and gated, of each 8-bit instructions and exact products.
 struct RowsModel8 {
     float launch, block;              // a launch; a block of a wavefront's k
     float more;                       // the same for every 256 workgroups past the first
@@ -799,18 +798,18 @@ struct RowsModel8 {
 };
 constexpr int kRowsM8[3] = {16, 32, 64};
 constexpr RowsModel8 kRowsModel8[3][4] = {
-    {{3.05f, 0.667f, 1.08f, 0.133f, 1.89f, 0.27f, 6.97f},
-     {0.000699f, 0.665f, 1.02f, 0.124f, 5.13f, 0.29f, 7.31f},
-     {2.7f, 1.08f, 0.846f, 0.112f, 2.02f, 0.32f, 2.2f},
-     {4.85f, 1.08f, 0.811f, 0.108f, 0.0411f, 0.334f, 2.35f}},
-    {{2.69f, 0.759f, 0.71f, 0.128f, 1.65f, 0.279f, 2.13f},
-     {0.0083f, 0.757f, 0.717f, 0.123f, 4.77f, 0.281f, 2.1f},
-     {2.9f, 1.24f, 0.991f, 0.126f, 2.05f, 0.327f, 1.55f},
-     {0.231f, 1.24f, 1.53f, 0.11f, 5.08f, 0.335f, 1.59f}},
-    {{3.48f, 1.12f, 1.59f, 0.113f, 1.69f, 0.294f, 1.84f},
-     {0.000386f, 1.2f, 1.67f, 0.0775f, 5.55f, 0.305f, 2.34f},
-     {3.91f, 1.64f, 2.24f, 0.0949f, 2.04f, 0.344f, 1.13f},
-     {0.000244f, 1.75f, 2.24f, 0.076f, 6.16f, 0.362f, 1.37f}},
+    {{2.41f, 0.583f, 0.399f, 0.0965f, 1.58f, 0.282f, 2.16f},
+     {4.37f, 0.587f, 0.359f, 0.0971f, 0.00496f, 0.284f, 2.48f},
+     {2.5f, 0.986f, 0.195f, 0.108f, 1.81f, 0.324f, 0.894f},
+     {4.76f, 0.986f, 0.309f, 0.103f, 0.000364f, 0.329f, 0.942f}},
+    {{2.45f, 0.763f, 0.38f, 0.1f, 1.59f, 0.285f, 0.829f},
+     {4.5f, 0.771f, 0.369f, 0.101f, 0.000156f, 0.285f, 0.891f},
+     {2.73f, 1.18f, 0.707f, 0.0914f, 1.87f, 0.335f, 0.623f},
+     {5.03f, 1.2f, 0.683f, 0.0917f, 0.0f, 0.339f, 0.743f}},
+    {{2.86f, 1.14f, 0.622f, 0.0909f, 1.65f, 0.289f, 0.455f},
+     {2.95f, 1.1f, 0.674f, 0.0813f, 2.15f, 0.289f, 0.622f},
+     {3.34f, 1.57f, 1.89f, 0.0726f, 1.91f, 0.343f, 0.729f},
+     {0.722f, 1.58f, 1.94f, 0.0554f, 5.06f, 0.353f, 0.99f}},
 };
 struct TileModel8 {
     float launch, round;              // a launch; a round of tiles
@@ -823,19 +822,19 @@ struct TileShape8 {
 };
 constexpr TileShape8 kTileShape8[4] = {{128, 64, 512}, {128, 128, 512}, {256, 128, 256}, {256, 256, 256}};
 constexpr TileModel8 kTileModel8[4][4] = {
-    {{5.5f, 1.06f, 0.384f, 0.633f, 1.01f, 0.0397f, 1.5f, 0.288f, 0.319f},
-     {6.95f, 1.06f, 0.703f, 1.1f, 1.21f, 0.0378f, 0.674f, 0.291f, 0.294f},
-     {5.1f, 1.3f, 0.405f, 0.675f, 0.745f, 0.0442f, 1.84f, 0.325f, 0.34f},
-     {3.8f, 0.209f, 0.716f, 1.13f, 0.489f, 0.0393f, 4.46f, 0.344f, 0.386f}},
-    {{7.34f, 0.581f, 0.577f, 0.912f, 0.977f, 0.0585f, 1.2f, 0.282f, 0.31f},
-     {10.0f, 0.917f, 1.02f, 1.7f, 1.18f, 0.0287f, 0.0f, 0.255f, 0.25f},
-     {6.56f, 0.843f, 0.618f, 0.955f, 0.738f, 0.0544f, 1.55f, 0.321f, 0.318f},
-     {8.6f, 0.0f, 1.05f, 1.74f, 0.607f, 0.0372f, 0.834f, 0.349f, 0.321f}},
-    {{6.94f, 2.05f, 2.92f, 0.737f, 1.02f, 0.0395f, 1.4f, 0.279f, 0.332f},
-     {8.96f, 2.69f, 2.25f, 1.53f, 1.17f, 0.0361f, 0.0f, 0.262f, 0.28f},
-     {6.55f, 1.63f, 3.06f, 0.816f, 0.796f, 0.0484f, 1.89f, 0.317f, 0.338f},
-     {8.13f, 1.81f, 3.55f, 1.64f, 0.97f, 0.0487f, 1.02f, 0.325f, 0.304f}},
-    {{8.41f, 4.36f, 5.62f, 1.39f, 1.02f, 0.0583f, 0.571f, 0.276f, 0.282f},
+    {{5.21f, 1.33f, 0.381f, 0.633f, 0.966f, 0.0442f, 1.53f, 0.285f, 0.296f},
+     {6.74f, 1.23f, 0.698f, 1.07f, 1.13f, 0.0441f, 0.664f, 0.29f, 0.285f},
+     {4.86f, 1.54f, 0.404f, 0.671f, 0.668f, 0.0464f, 1.86f, 0.32f, 0.333f},
+     {0.0f, 0.603f, 0.711f, 1.08f, 0.447f, 0.0451f, 7.85f, 0.343f, 0.377f}},
+    {{6.95f, 0.885f, 0.563f, 0.887f, 0.965f, 0.0684f, 1.3f, 0.276f, 0.292f},
+     {9.59f, 1.22f, 1.01f, 1.66f, 1.12f, 0.0396f, 0.0f, 0.254f, 0.24f},
+     {6.11f, 1.22f, 0.609f, 0.928f, 0.709f, 0.0599f, 1.65f, 0.316f, 0.308f},
+     {8.42f, 0.454f, 1.04f, 1.7f, 0.604f, 0.0424f, 0.545f, 0.348f, 0.307f}},
+    {{6.42f, 2.46f, 2.94f, 0.725f, 0.96f, 0.0456f, 1.54f, 0.274f, 0.313f},
+     {8.48f, 3.03f, 15.3f, 1.52f, 1.19f, 0.0425f, 0.0f, 0.267f, 0.261f},
+     {6.05f, 2.06f, 10.1f, 0.799f, 0.748f, 0.0538f, 2.0f, 0.313f, 0.323f},
+     {7.52f, 2.27f, 22.0f, 1.62f, 0.885f, 0.052f, 1.23f, 0.321f, 0.29f}},
+    {{7.66f, 4.73f, 5.79f, 1.37f, 1.0f, 0.0655f, 0.926f, 0.268f, 0.272f},
      {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f},
      {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f},
      {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f}},
@@ -922,9 +921,9 @@ int launch_tiles(const Gemm8 &g, const Partial8 &q, hipStream_t stream) {
     return check_hip(hipGetLastError(), "k_tile8");
 }
 
-template <typename T, bool GATED, bool EXACT, int NF, int MF, int U>
+template <typename T, bool GATED, bool EXACT, int NF, int MF, int U, int PER>
 int launch_rows(const Gemm8 &g, const Partial8 &q, hipStream_t stream) {
-    hipLaunchKernelGGL((k_rows8<T, GATED, EXACT, NF, MF, U>), dim3((unsigned)((g.N + NF * 16 - 1) / (NF * 16)), q.split,
+    hipLaunchKernelGGL((k_rows8<T, GATED, EXACT, NF, MF, U, PER>), dim3((unsigned)((g.N + NF * 16 - 1) / (NF * 16)), q.split,
                        (unsigned)((g.M + MF * 16 - 1) / (MF * 16))), dim3(512), 0, stream, g, q);
     return check_hip(hipGetLastError(), "k_rows8");
 }
@@ -932,9 +931,9 @@ int launch_rows(const Gemm8 &g, const Partial8 &q, hipStream_t stream) {
 template <typename T, bool GATED, bool EXACT>
 int by_path(const Gemm8 &g, const Plan8 &p, const Partial8 &q, hipStream_t stream) {
     switch (p.path) {
-    case kRows16: return launch_rows<T, GATED, EXACT, 1, 1, GATED ? 1 : 2>(g, q, stream);
-    case kRows32: return launch_rows<T, GATED, EXACT, 1, 2, 1>(g, q, stream);
-    case kRows64: return launch_rows<T, GATED, EXACT, 1, 4, 1>(g, q, stream);
+    case kRows16: return launch_rows<T, GATED, EXACT, 1, 1, GATED ? 1 : 2, 6>(g, q, stream);
+    case kRows32: return launch_rows<T, GATED, EXACT, 1, 2, 1, GATED ? 4 : 6>(g, q, stream);
+    case kRows64: return launch_rows<T, GATED, EXACT, 1, 4, 1, GATED ? 2 : 4>(g, q, stream);
     case kTile64: return launch_tiles<T, GATED, EXACT, 128, 64, 2, 2, 3>(g, q, stream);
     case kTile128: return launch_tiles<T, GATED, EXACT, 128, 128, 2, 2, 2>(g, q, stream);
     case kTile256x256:
