@@ -16,6 +16,7 @@
 namespace sa {
 namespace {
 
+typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 // Eight codes as bfloat16, which holds every e4m3 value.
@@ -259,6 +260,12 @@ __global__ __launch_bounds__(512, PER) void k_rows8(Gemm8 g, Partial8 q) {
 // share one scale.
 //
 // Workgroups are persistent and their loads run over the stages of all their tiles.
+//
+// Bound by the matrix cores' power and, in exact products, by issue: 8192 x 4096 x 9830 with
+// 16-bit results takes 340 us (1.94 PFLOP/s), exact 590 (1.12), of which the widening of the
+// codes and the scaling of the blocks issue 3 vector instructions beside each matrix
+// instruction, which hides 2.  With two stages in flight, and arguments kept in registers that
+// then spilled, exact products took 659.
 template <bool GATED, int BN, int BM, int WN, int WM, int S>
 struct TileCfg8 {
     static constexpr int NW = WN * WM, NT = NW * 64;
@@ -352,6 +359,9 @@ struct Reads8 {
     }
     __device__ i32x4 chunk(const uint8_t *lds, int row0, int c) const {
         return *reinterpret_cast<const i32x4 *>(lds + fo[c] + row0 * kBlock);
+    }
+    __device__ i32x2 half(const uint8_t *lds, int row0, int c, int which) const {
+        return *reinterpret_cast<const i32x2 *>(lds + fo[c] + row0 * kBlock + which * 8);
     }
     __device__ i32x8 operator()(const uint8_t *lds, int row0) const {
         union {
@@ -543,13 +553,21 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8) {
     auto rows_n = [&](const uint8_t *st, int i) { return st + (GATED && i >= TNG ? NSide::bytes : 0); };
     auto row_n = [&](int i) { return nrow + i % TNG * MI; };  // row i of a stage's fragments of W
     auto rows_m = [&](const uint8_t *st) { return st + BN * kBlock; };
-    float scale[H][TM];
+    // X's scales of a stage, read at its start into scale[0], and W's; joined beside the first
+    // row's products, whose sums are the first to need them
+    float scale[H][TM], wscale[H];
     auto fetch_scales = [&](const uint8_t *st) {
         const float *s = reinterpret_cast<const float *>(st + Cfg::scales_at + wave * Cfg::scales);
 #pragma unroll
-        for (int h = 0; h < H; ++h)
+        for (int j = 0; j < TM; ++j) scale[0][j] = s[j * MI + (lane & (MI - 1))];
 #pragma unroll
-            for (int j = 0; j < TM; ++j) scale[h][j] = s[j * MI + (lane & (MI - 1))] * s[64 * XL + h];
+        for (int h = 0; h < H; ++h) wscale[h] = s[64 * XL + h];
+    };
+    auto join_scales = [&]() {
+#pragma unroll
+        for (int j = 0; j < TM; ++j)
+#pragma unroll
+            for (int h = H - 1; h >= 0; --h) scale[h][j] = scale[0][j] * wscale[h];
     };
     f32x4 part[TM];
     auto add = [&](int i, int j) {  // beside the next row's products, not after all of them
@@ -591,6 +609,7 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8) {
                 part[j] = block_products8(fa[i % RING], fb[j]);
                 if (i == TN - 1) fb[j] = read(rows_m(nxt), mrow + j * MI);
             }
+            if (i == 0) join_scales();
             constexpr int next = (i + RING) % TN;
             fa[i % RING] = read(rows_n(i < JOIN ? cur : nxt, next), row_n(next));
             __builtin_amdgcn_sched_barrier(0);
@@ -622,16 +641,16 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8) {
         const uint8_t *cur = smem + slot * Cfg::stage;
         slot = slot + 1 == S ? 0 : slot + 1;
         const uint8_t *nxt = smem + slot * Cfg::stage;
-        i32x4 raw[TM];  // half of X's codes of the next stage
+        i32x4 raw[TM];  // half of X's codes of the next stage: steps 0 and 1, then 2 and 3 as they are used up
         each<TN>([&](auto ic) {
             constexpr int i = decltype(ic)::value;
             if (i == JOIN) join();
             if constexpr (i >= JOIN) each<RATE>([&](auto e) { load(std::integral_constant<int, (i - JOIN) * RATE + decltype(e)::value>{}); });
             each<4>([&](auto qc) {
                 constexpr int q = decltype(qc)::value;
-                if (i == TN - 1 && q % 2 == 0)
+                if (i == TN - 2 && q == 3)
 #pragma unroll
-                    for (int j = 0; j < TM; ++j) raw[j] = read.chunk(rows_m(nxt), mrow + j * MI, q / 2);
+                    for (int j = 0; j < TM; ++j) raw[j] = read.chunk(rows_m(nxt), mrow + j * MI, 0);
 #pragma unroll
                 for (int j = 0; j < TM; ++j) {
                     if (i > 0 && q == 0) add(i - 1, j);
@@ -642,7 +661,15 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8) {
                 wa[(q + 1) & 1] = widen(from[at], from[at + 1]);
                 if (i == TN - 1)
 #pragma unroll
-                    for (int j = 0; j < TM; ++j) wb[j].k[q] = widen(raw[j][q % 2 * 2], raw[j][q % 2 * 2 + 1]);
+                    for (int j = 0; j < TM; ++j) {
+                        wb[j].k[q] = widen(raw[j][q % 2 * 2], raw[j][q % 2 * 2 + 1]);
+                        if (q < 2) {
+                            const i32x2 v = read.half(rows_m(nxt), mrow + j * MI, 1, q);
+                            raw[j][q * 2] = v[0];
+                            raw[j][q * 2 + 1] = v[1];
+                        }
+                    }
+                if (i == 0 && q == 3) join_scales();
                 constexpr int next = (i + 2) % TN;
                 if (q == 3) ra[i & 1] = read(rows_n(i < JOIN ? cur : nxt, next), row_n(next));
                 __builtin_amdgcn_sched_barrier(0);
@@ -772,6 +799,16 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8) {
 }
 
 // ---------------------------------------------------------------- host side
+// By GPU time in bfloat16, us, the best split of k each:
+//                            kRows16 kRows32 kRows64 kTile64 kTile128 kTile256 kTile256x256
+//   16 x 9830 x 4096            14.0    16.2    19.8    14.9     18.7     18.3         26.1
+//   16 x 4096 x 9830 exact      15.2    16.4    19.6    20.6     24.6     30.1
+//   64 x 4096 x 9830                            29.0    17.8     21.8     23.0         33.1
+//   256 x 9830 x 4096                           98.1    26.9     31.2     31.0         39.0
+//   1000 x 9830 x 4096 exact                            99.9      102      119
+//   2048 x 4096 x 9830                                   114     94.2     89.7          131
+//   5571 x 1870 x 13720                                  243      212      211          206
+//   8192 x 4096 x 9830                                                     362          336
 enum Path8 { kRows16, kRows32, kRows64, kTile64, kTile128, kTile256, kTile256x256 };
 struct Plan8 {
     Path8 path;
@@ -779,7 +816,7 @@ struct Plan8 {
     int keep;  // the epilogue runs in k_join8
 };
 
-// 8-bit instructions where every result has 16 bits (8192 x 4096 x 9830: 362 us, and 585 of
+// 8-bit instructions where every result has 16 bits (8192 x 4096 x 9830: 340 us, and 590 of
 // exact products).
 bool is_exact(const Gemm8 &g) { return g.q.codes || g.e.out_f32; }
 
