@@ -807,8 +807,9 @@ int structadmm_quantize8(const sa_quantize8_desc *desc, hipStream_t stream);
 /* ---- 8-bit linear layer: structadmm_linear8_fwd ---------------------- */
 /*
  * z = X W^T + bias, y = act(z) + R: X [M, K] with row blocks, W [N, K] with square
- * blocks, bias [N], R [M, N].  The sum of a block's products is scaled in binary32 by
- * both scales and added up.  Y receives y in out_type, Q in 8 bits with row blocks
+ * blocks, bias [N], R [M, N].  The sum of a block's products is multiplied in binary32 by
+ * the product of both scales, itself a binary32 number (below 2^-126 it keeps fewer bits,
+ * past 2^128 it is infinite), and added up.  Y receives y in out_type, Q in 8 bits with row blocks
  * (at least one is given), Z, when given, z for the backward pass.  Y may be R itself
  * with the same pitch.
  *

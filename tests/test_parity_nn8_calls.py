@@ -157,6 +157,21 @@ def test_one_scale_for_many_blocks(M):
         sa.quantize8(matrix(g, M, 500, T.float16, "packed")[0], Q=sa.Matrix8(X.codes, one.expand(M, 4)), out="")
 
 
+@pytest.mark.parametrize("M", [5, 90, 600])
+@pytest.mark.parametrize("power", [-60, -64, 50])
+def test_small_and_large_scales(M, power):
+    """Both operands times 2^power: the scales' product rounds to binary32, below 2^-126 by
+    up to 2^-150, once for the block's sum of products of codes."""
+    g = gen(M + power)
+    X, W = operand(g, M, 700, 1), operand(g, 300, 700, 128)
+    X, W = (sa.Matrix8(m.codes, m.scales * 2.0 ** power) for m in (X, W))
+    Y = sa.linear8_fwd(X, W, out_dtype=T.float32)[0]
+    want, tol = ref8.product(X, W)
+    tol = tol + 2.0 ** -150 * (X.codes.double().abs() @ W.codes.double().abs().t())
+    # sums below 2^-126 are rounded by up to 2^-150 at each of their additions
+    assert ((Y.double() - want).abs() <= tol + 64 * 2.0 ** -150).all()
+
+
 # --------------------------------------------------------- streams and graphs
 def chain(x, gamma, r, qg, qu, qd, bufs):
     s, n8, rstd, G, U_, h8, y, ws1, ws2 = bufs
