@@ -33,28 +33,39 @@ struct Addends {
     }
 };
 
+// V (the first cnt < V at a row's end) results to p; past: 16-bit ones past the caches.
+template <bool PAST, typename E, int V>
+__device__ inline void put_results(E *p, int cnt, const float (&v)[V], int past) {
+    if (cnt < V) {
+        store_part<E, V>(p, cnt, v);
+    } else if (PAST && sizeof(E) == 2 && past) {
+        // an empty statement on either side keeps the compiler from merging the branches, which
+        // drops the hint
+        asm volatile("" ::"n"(0));
+        typedef E vec __attribute__((ext_vector_type(V)));
+        typedef vec loose __attribute__((aligned(alignof(E))));
+        vec x;
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] = (E)v[i];  // round to nearest even
+        __builtin_nontemporal_store(x, reinterpret_cast<loose *>(p));
+        asm volatile("" ::"n"(1));
+    } else {
+        store_vec<E, V>(p, v);
+    }
+}
+
 // V (cnt < V at a row's end) results z to Y.
-template <typename T, int V>
+template <typename T, int V, bool PAST = false>
 __device__ inline void put_values(const Epilogue &e, void *Y, int64_t m, int64_t n, int cnt, const float (&z)[V]) {
-    auto put = [&](auto *p, const float (&v)[V]) {
-        using E = typename std::remove_reference<decltype(*p)>::type;
-        if (cnt == V) store_vec<E, V>(p, v);
-        else store_part<E, V>(p, cnt, v);
-    };
-    if (e.out_f32) put(reinterpret_cast<float *>(Y) + m * e.ldy + n, z);
-    else put(reinterpret_cast<T *>(Y) + m * e.ldy + n, z);
+    if (e.out_f32) put_results<PAST>(reinterpret_cast<float *>(Y) + m * e.ldy + n, cnt, z, e.past);
+    else put_results<PAST>(reinterpret_cast<T *>(Y) + m * e.ldy + n, cnt, z, e.past);
 }
 
 // V (cnt < V at a row's end) consecutive results, in z, from their sums z (and u); the
 // pre-activations are stored.
-template <typename T, bool GATED, int V>
+template <typename T, bool GATED, int V, bool PAST = false>
 __device__ inline void finish_values(const Epilogue &e, int64_t m, int64_t n, int cnt, float (&z)[V], float (&u)[V],
                                      const Addends<T, V> &with) {
-    auto put = [&](auto *p, const float (&v)[V]) {
-        using E = typename std::remove_reference<decltype(*p)>::type;
-        if (cnt == V) store_vec<E, V>(p, v);
-        else store_part<E, V>(p, cnt, v);
-    };
     auto add = [&](const auto *p) {
         using E = typename std::remove_cv<typename std::remove_reference<decltype(*p)>::type>::type;
         float t[V];
@@ -66,13 +77,13 @@ __device__ inline void finish_values(const Epilogue &e, int64_t m, int64_t n, in
     if (e.bias)
 #pragma unroll
         for (int i = 0; i < V; ++i) z[i] += with.bias[i];
-    if (e.Z) put(reinterpret_cast<T *>(e.Z) + m * e.ldz + n, z);
+    if (e.Z) put_results<PAST>(reinterpret_cast<T *>(e.Z) + m * e.ldz + n, cnt, z, e.past);
     if (e.act != SA_ACT_NONE) activate<false, V>(e.act, z, z, z);
     if constexpr (GATED) {
         if (e.bias2)
 #pragma unroll
             for (int i = 0; i < V; ++i) u[i] += with.bias2[i];
-        if (e.Z2) put(reinterpret_cast<T *>(e.Z2) + m * e.ldz + n, u);
+        if (e.Z2) put_results<PAST>(reinterpret_cast<T *>(e.Z2) + m * e.ldz + n, cnt, u, e.past);
 #pragma unroll
         for (int i = 0; i < V; ++i) z[i] *= u[i];
     }

@@ -31,6 +31,7 @@ struct Epilogue {
     int64_t ldy;
     void *Z, *Z2;         // pre-activations or NULL (Z2: gated)
     int64_t ldz;
+    int past = 0;         // 16-bit results go past the caches, in kernels that can
 };
 
 struct Gemm {

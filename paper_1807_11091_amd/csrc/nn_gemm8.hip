@@ -262,10 +262,10 @@ __global__ __launch_bounds__(512, PER) void k_rows8(Gemm8 g, Partial8 q) {
 // Workgroups are persistent and their loads run over the stages of all their tiles.
 //
 // Bound by the matrix cores' power and, in exact products, by issue: 8192 x 4096 x 9830 with
-// 16-bit results takes 340 us (1.94 PFLOP/s), exact 590 (1.12), of which the widening of the
-// codes and the scaling of the blocks issue 3 vector instructions beside each matrix
-// instruction, which hides 2.  With two stages in flight, and arguments kept in registers that
-// then spilled, exact products took 659.
+// 16-bit results takes 284 us (2.3 PFLOP/s; 324 with bias and residual), exact 584 (1.13), of
+// which the widening of the codes and the scaling of the blocks issue 3 vector instructions
+// beside each matrix instruction, which hides 2.  With two stages in flight, and arguments kept
+// in registers that then spilled, exact products took 659.
 template <bool GATED, int BN, int BM, int WN, int WM, int S>
 struct TileCfg8 {
     static constexpr int NW = WN * WM, NT = NW * 64;
@@ -274,7 +274,9 @@ struct TileCfg8 {
     static constexpr int scales = xl * 256 + 16;                // bytes a wavefront: X's, then W's
     static constexpr int stage = scales_at + NW * scales;
     static constexpr int join_at = S * stage;                   // largest values of the results' rows
-    static constexpr int lds = join_at + WN * BM * 4;
+    static constexpr bool touches = BM == 256;                  // see touch()
+    static constexpr int touch_at = join_at + WN * BM * 4;
+    static constexpr int lds = touch_at + (touches ? 256 : 0);
     static_assert(lds <= kMaxLds, "LDS");
 };
 
@@ -681,6 +683,23 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8) {
         end_stage();
     };
 
+    // The lines of a tile's residual, which the epilogue reads piece by piece, into the L2, a
+    // stage before: 8192 x 4096 x 9830 took 337 us without.  The words read go to LDS and are
+    // not used.  Not in smaller tiles, where it cost more than it gave (a binary32 result with a
+    // residual 620 us, 633 with it).
+    auto touch = [&](const Tile &q) {
+        const Gemm8 &g = args().g;
+        if (!g.e.R || args().part.keep) return;
+        const int size = g.e.out_f32 ? 4 : 2, per = NROWS * size / 128;  // lines a row
+        const int rows = (int)min(g.M - q.m0, (int64_t)BM), bytes = (int)min(g.N - q.n0, (int64_t)NROWS) * size;
+        const uint64_t at = reinterpret_cast<uint64_t>(g.e.R) + (q.m0 * g.e.ldr + q.n0) * size;
+        const uint32_t pitch = (uint32_t)g.e.ldr * (uint32_t)size;
+        const i32x4 rs = buffer_at(at & ~(uint64_t)3, uni((int)((uint32_t)(rows - 1) * pitch + (uint32_t)bytes) & ~3));
+        for (int c = 0; c < BM * per; c += Cfg::NT) {
+            const int i = c + tid, row = i / per, in = (i - row * per) * 128;
+            dma4<Cfg::touch_at>(rs, row < rows && in < bytes ? (uint32_t)row * pitch + (uint32_t)in & ~3u : kInvalidOffset, 0, lds0);
+        }
+    };
     constexpr int PN = TNG / 2;  // pairs of fragments
 #pragma unroll 1
     for (int ti = 0; ti < mine; ++ti) {
@@ -696,12 +715,17 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8) {
         } else {
             if (q.s0 < q.s1) fetch8();
 #pragma unroll 1
-            for (int s = q.s0; s < q.s1; ++s) multiply8();
+            for (int s = q.s0; s < q.s1; ++s) {
+                if constexpr (Cfg::touches)
+                    if (s + 1 == q.s1) touch(q);
+                multiply8();
+            }
         }
 
         // Results straight from the registers.  A lane holds 4 consecutive n of every 16;
         // exchanging the odd rows of 16 lanes of one such group with the even ones of the next
-        // leaves 8 consecutive n in each lane.
+        // leaves 8 consecutive n in each lane.  A row's pieces of 64 bytes follow each other
+        // (binary32 results with a residual 640 us in columns of pieces, 620 so).
         const TileArgs8 &a = args();
         const Gemm8 &g = a.g;
         int el = lane;
@@ -715,12 +739,12 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8) {
         for (int f = 0; f < PN * TM; ++f) {
             float z[8], u[8];
             pick<PN * TM>(f, [&](auto fc) {
-                constexpr int p = decltype(fc)::value / TM, j = decltype(fc)::value % TM;
+                constexpr int p = decltype(fc)::value % PN, j = decltype(fc)::value / PN;
 #pragma unroll
                 for (int h = 0; h < H; ++h)
 #pragma unroll
                     for (int e = 0; e < 8; ++e) (h ? u : z)[e] = acc[h * TNG + 2 * p + e / 4][j][e % 4];
-                asm volatile("" ::"n"(p * TM + j));  // keeps the compiler from merging the branches, which would index registers
+                asm volatile("" ::"n"(j * PN + p));  // keeps the compiler from merging the branches, which would index registers
             });
 #pragma unroll
             for (int h = 0; h < H; ++h)
@@ -731,7 +755,7 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8) {
                     v[e] = __uint_as_float(w[0]);
                     v[e + 4] = __uint_as_float(w[1]);
                 }
-            const int64_t m = q.m0 + mrow + f % TM * MI + ml, n = q.n0 + nrow + f / TM * 32 + nl;
+            const int64_t m = q.m0 + mrow + f / PN * MI + ml, n = q.n0 + nrow + f % PN * 32 + nl;
             const int cnt = m < g.M ? (int)max((int64_t)0, min((int64_t)8, g.N - n)) : 0;
             if (cnt > 0) {
                 if (a.part.keep) {
@@ -741,8 +765,8 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8) {
                     Addends<T, 8> with;
                     with.has_r = false;
                     with.load_bias(g.e, n, cnt);
-                    finish_values<T, GATED, 8>(g.e, m, n, cnt, z, u, with);
-                    if (g.e.Y) put_values<T, 8>(g.e, g.e.Y, m, n, cnt, z);
+                    finish_values<T, GATED, 8, true>(g.e, m, n, cnt, z, u, with);
+                    if (g.e.Y) put_values<T, 8, true>(g.e, g.e.Y, m, n, cnt, z);
                 }
             }
             if constexpr (!EIGHT) continue;
@@ -751,11 +775,11 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8) {
             for (int e = 0; e < 8; ++e) z[e] = e < cnt ? z[e] : 0.0f;
             const float most = largest(z);
             pick<PN * TM>(f, [&](auto fc) {
-                constexpr int p = decltype(fc)::value / TM, j = decltype(fc)::value % TM;
+                constexpr int p = decltype(fc)::value % PN, j = decltype(fc)::value / PN;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) acc[2 * p + e / 4][j][e % 4] = z[e];
                 top[j] = fmaxf(top[j], most);
-                asm volatile("" ::"n"(p * TM + j));
+                asm volatile("" ::"n"(j * PN + p));
             });
         }
         if constexpr (!EIGHT) continue;
@@ -808,7 +832,7 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8) {
 //   1000 x 9830 x 4096 exact                            99.9      102      119
 //   2048 x 4096 x 9830                                   114     94.2     89.7          131
 //   5571 x 1870 x 13720                                  243      212      211          206
-//   8192 x 4096 x 9830                                                     362          336
+//   8192 x 4096 x 9830                                                     314          284
 enum Path8 { kRows16, kRows32, kRows64, kTile64, kTile128, kTile256, kTile256x256 };
 struct Plan8 {
     Path8 path;
@@ -816,7 +840,7 @@ struct Plan8 {
     int keep;  // the epilogue runs in k_join8
 };
 
-// 8-bit instructions where every result has 16 bits (8192 x 4096 x 9830: 340 us, and 590 of
+// 8-bit instructions where every result has 16 bits (8192 x 4096 x 9830: 284 us, and 584 of
 // exact products).
 bool is_exact(const Gemm8 &g) { return g.q.codes || g.e.out_f32; }
 
@@ -985,14 +1009,29 @@ int run(const Gemm8 &g, const Plan8 &p, const Partial8 &q, hipStream_t stream) {
     return q.keep ? join<T, GATED>(g, q, stream) : SA_OK;
 }
 
+// Tiles store large 16-bit results past the caches, which the operands need: 8192 x 4096 x 9830
+// takes 284 us instead of 307, 5120 x 6080 x 84 with residual and Z 61 instead of 98, gated
+// 8192 x 9830 x 4096 674 instead of 757.  From 48 MB on where the rows' pieces of 64 bytes are
+// whole lines' halves: smaller ones lose by it if the caches hold where they go (4096 x 4100 x
+// 300 39 us instead of 31).  Cut pieces are better joined there (8192 x 6060 x 1000, 99 MB, 128 us
+// instead of 94) until the results are half of the Infinity Cache's 256 MB (the gated ones above
+// have 161).  Binary32 results, two stores a lane, always lose (608 us, 584).
+int past_caches(int64_t M, int64_t N, const void *Y, int64_t ldy, const void *Z, const void *Z2, int64_t ldz) {
+    const int64_t at = (int64_t)reinterpret_cast<uintptr_t>(Y) | (Y ? ldy * 2 : 0) | (int64_t)reinterpret_cast<uintptr_t>(Z) |
+                       (int64_t)reinterpret_cast<uintptr_t>(Z2) | (Z ? ldz * 2 : 0);
+    return M * N >= int64_t(at % 64 == 0 ? 24 : 64) << 20;
+}
+
 Gemm8 product(const sa_linear8_desc &d) {
     return Gemm8{d.M, d.N, d.K, d.type, 0, d.X, {d.W, sa_matrix8{}},
-                 Epilogue{d.act, d.out_type == SA_F32, d.bias, nullptr, d.R, d.ldr, d.Y, d.ldy, d.Z, nullptr, d.ldz}, d.Q};
+                 Epilogue{d.act, d.out_type == SA_F32, d.bias, nullptr, d.R, d.ldr, d.Y, d.ldy, d.Z, nullptr, d.ldz,
+                          past_caches(d.M, d.N, d.Y, d.ldy, d.Z, nullptr, d.ldz)}, d.Q};
 }
 
 Gemm8 product(const sa_glu8_desc &d) {
     return Gemm8{d.M, d.N, d.K, d.type, 1, d.X, {d.Wg, d.Wu},
-                 Epilogue{d.act, 0, d.bg, d.bu, nullptr, 0, d.H, d.ldh, d.G, d.U, d.ldgu}, d.Q};
+                 Epilogue{d.act, 0, d.bg, d.bu, nullptr, 0, d.H, d.ldh, d.G, d.U, d.ldgu,
+                          past_caches(d.M, d.N, d.H, d.ldh, d.G, d.U, d.ldgu)}, d.Q};
 }
 
 // The outputs choose the plan, so a query covers each call that it holds for: with these

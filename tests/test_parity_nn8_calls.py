@@ -99,6 +99,22 @@ def test_more_sizes(M, N, K, gated, eight):
         check_out(Y, want, tol, T.bfloat16, buf, "Y")
 
 
+@pytest.mark.parametrize("M,N,K,layout", [(8192, 4096, 200, "packed"), (5120, 6080, 84, "packed"), (8300, 4100, 130, "odd"),
+                                          (8200, 8190, 128, "odd")])
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_large_results_with_residual_and_preactivations(M, N, K, layout, dtype):
+    """Results of 48 MB and more, which tiles store past the caches, on aligned and odd rows."""
+    g = gen(M + N)
+    t = {"bf16": T.bfloat16, "f16": T.float16, "f32": T.float32}[dtype]
+    X, W = operand(g, M, K, 1), operand(g, N, K, 128, 1 / math.sqrt(K))
+    bias, R = vec(g, N), matrix(g, M, N, t, layout)[0]
+    (Y, buf), (Z, zbuf) = out_matrix(M, N, t, layout), out_matrix(M, N, T.bfloat16 if dtype == "f32" else t, layout)
+    sa.linear8_fwd(X, W, bias, R, sa.ACT_RELU, Y=Y, Z=Z, out="")
+    want, tol, z, tz = ref8.linear8(X, W, bias, R, "relu", exact=dtype == "f32")
+    check_out(Y, want, tol, t, buf, "Y")
+    check_out(Z, z, tz, Z.dtype, zbuf, "Z")
+
+
 def test_empty_sums_and_sizes():
     g = gen(2)
     X, W = sa.matrix8(5, 0), sa.matrix8(200, 0, 128)
