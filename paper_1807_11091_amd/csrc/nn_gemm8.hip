@@ -1009,17 +1009,17 @@ int run(const Gemm8 &g, const Plan8 &p, const Partial8 &q, hipStream_t stream) {
     return q.keep ? join<T, GATED>(g, q, stream) : SA_OK;
 }
 
-// Tiles store large 16-bit results past the caches, which the operands need: 8192 x 4096 x 9830
-// takes 284 us instead of 307, 5120 x 6080 x 84 with residual and Z 61 instead of 98, gated
-// 8192 x 9830 x 4096 674 instead of 757.  From 48 MB on where the rows' pieces of 64 bytes are
-// whole lines' halves: smaller ones lose by it if the caches hold where they go (4096 x 4100 x
-// 300 39 us instead of 31).  Cut pieces are better joined there (8192 x 6060 x 1000, 99 MB, 128 us
-// instead of 94) until the results are half of the Infinity Cache's 256 MB (the gated ones above
-// have 161).  Binary32 results, two stores a lane, always lose (608 us, 584).
+// Tiles store 16-bit results of 48 MB and more past the caches, which the operands need, where
+// the rows' pieces of 64 bytes are halves of lines: 8192 x 4096 x 9830 takes 284 us instead of
+// 307, 5120 x 6080 x 84 with residual and Z 61 instead of 98.  Smaller ones lose by it if the
+// caches hold where they go (4096 x 4100 x 300 39 us instead of 31).  Cut pieces are better joined
+// there (8192 x 6060 x 1000 128 us instead of 94; gated 8192 x 9830 x 4096 with pre-activations,
+// 1365 instead of 1312, though 1262 where two sets of buffers take turns).  Binary32 results,
+// two stores a lane, lose too (608 us, 584).
 int past_caches(int64_t M, int64_t N, const void *Y, int64_t ldy, const void *Z, const void *Z2, int64_t ldz) {
     const int64_t at = (int64_t)reinterpret_cast<uintptr_t>(Y) | (Y ? ldy * 2 : 0) | (int64_t)reinterpret_cast<uintptr_t>(Z) |
                        (int64_t)reinterpret_cast<uintptr_t>(Z2) | (Z ? ldz * 2 : 0);
-    return M * N >= int64_t(at % 64 == 0 ? 24 : 64) << 20;
+    return at % 64 == 0 && M * N >= int64_t(24) << 20;
 }
 
 Gemm8 product(const sa_linear8_desc &d) {
