@@ -728,6 +728,8 @@ typedef struct sa_matrix8 {
 /*
  * S = X + R, rounded to its type (S = X where R is NULL),
  * Y[r][c] = S[r][c] * rstd[r] * gamma[c], rstd[r] = 1 / sqrt(sum_c S[r][c]^2 / cols + eps).
+ * Rows whose squares leave binary32 on either side keep the formula (rstd is infinite only
+ * where 1 / sqrt(..) is past binary32, and Y is right there too).
  * gamma NULL stands for ones.  S, Y, Q and rstd may each be left out (NULL; at least
  * one is given): Y receives the result in the inputs' type, Q in 8 bits
  * with row blocks, both from the same binary32 values.  S may be X or R itself, and Y

@@ -302,6 +302,28 @@ __device__ inline float rms_sum(float x, float r) {
     return (float)(T)(x + r);
 }
 
+// A row whose sum of squares s leaves binary32's range, or whose bits are lost below it, is
+// summed again times the square of a power of two, chosen by s, that brings it back: no
+// finite row gives 0, and none above 0 an infinite rstd that has one.  1 for every other row.
+constexpr float kMostSquares = 0x1p126f, kLeastSquares = 0x1p-80f, kSmaller = 0x1p-96f, kLarger = 0x1p96f;
+__device__ inline float squares_scale(float s, float eps) {
+    if (!(s < kMostSquares && eps < kMostSquares)) return kSmaller;
+    return s < kLeastSquares && eps < kLeastSquares ? kLarger : 1.0f;
+}
+
+// What such a row's values are multiplied with, one after the other: rstd times the inverse
+// of the scale, and the scale, in the order that keeps a small value's bits.
+struct RmsFactors {
+    float first, second;
+    // s: the sum of (v * scale)^2
+    __device__ RmsFactors(float s, float cols, float eps, float scale) {
+        const float r = 1.0f / sqrtf(s / cols + eps * scale * scale);
+        first = scale > 1.0f ? scale : r;
+        second = scale > 1.0f ? r : scale;
+    }
+    __device__ float rstd() const { return first * second; }
+};
+
 // Bound by HBM: 16384 x 4096 bfloat16 with a residual, S and 8 bits takes 86 us, 5.5 TB/s; one
 // row 3.8 (its launch and two latencies).  The 8-bit result takes sixteen neighbouring lanes'
 // largest value, so nothing leaves the registers between the sum and the codes.
@@ -336,8 +358,37 @@ __global__ __launch_bounds__(Rows<TPR>::threads) void k_rms_fwd(RmsArgs a) {
         if (a.S && in && c < a.cols) store_chunk<T>(reinterpret_cast<T *>(a.S) + row * a.lds, c, a.cols, v[k]);
     }
     row_sums<TPR, NT>(s, none, tmp, 0);
+    // Does any row of the workgroup need a second sum?  All threads keep its barrier, so all
+    // work out every row's first.
+    bool again = false;
+#pragma unroll
+    for (int q = 0; q < (TPR > 64 ? RPB : 1); ++q) {
+        float sum = TPR > 64 ? 0.0f : s;
+        if constexpr (TPR > 64)
+#pragma unroll
+            for (int w = 0; w < TPR / 64; ++w) sum += tmp[0][q * (TPR / 64) + w].x;
+        again = again || squares_scale(sum, a.eps) != 1.0f;
+    }
+    float rstd = 1.0f / sqrtf(s / (float)a.cols + a.eps), by = rstd;
+    if (__builtin_amdgcn_readfirstlane(again)) {
+        const float scale = squares_scale(s, a.eps);
+        s = 0.0f;
+#pragma unroll
+        for (int k = 0; k < CH; ++k)
+#pragma unroll
+            for (int i = 0; i < kV; ++i) s = fmaf(v[k][i] * scale, v[k][i] * scale, s);
+        row_sums<TPR, NT>(s, none, tmp, 1);
+        if (scale != 1.0f) {
+            const RmsFactors f(s, (float)a.cols, a.eps, scale);
+            rstd = f.rstd();
+            by = 1.0f;
+#pragma unroll
+            for (int k = 0; k < CH; ++k)
+#pragma unroll
+                for (int i = 0; i < kV; ++i) v[k][i] = v[k][i] * f.first * f.second;
+        }
+    }
     if (!in) return;
-    const float rstd = 1.0f / sqrtf(s / (float)a.cols + a.eps);
     if (t == 0 && a.rstd) a.rstd[row] = rstd;
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
@@ -345,7 +396,7 @@ __global__ __launch_bounds__(Rows<TPR>::threads) void k_rms_fwd(RmsArgs a) {
         float g[kV];
         load_param(a.gamma, c, a.cols, 1.0f, g);
 #pragma unroll
-        for (int i = 0; i < kV; ++i) g[i] *= v[k][i] * rstd;
+        for (int i = 0; i < kV; ++i) g[i] *= v[k][i] * by;
         rms_results<T>(a, row, c, g);
     }
 }
@@ -368,6 +419,10 @@ __global__ __launch_bounds__(1024) void k_rms_fwd_long(RmsArgs a) {
 #pragma unroll
         for (int i = 0; i < kV; ++i) v[i] = rms_sum<T>(v[i], o[i]);
     };
+    auto load_again = [&](int c, float (&v)[kV]) {
+        if (a.S) load_chunk<T>(sum, c, a.cols, v);  // what this thread wrote
+        else load_sum(c, v);
+    };
     float s = 0.0f, none = 0.0f, v[kV];
     for (int c = threadIdx.x * kV; c < a.cols; c += NT * kV) {
         load_sum(c, v);
@@ -376,17 +431,27 @@ __global__ __launch_bounds__(1024) void k_rms_fwd_long(RmsArgs a) {
         if (a.S) store_chunk<T>(sum, c, a.cols, v);
     }
     row_sums<NT, NT>(s, none, tmp, 0);
-    const float rstd = 1.0f / sqrtf(s / (float)a.cols + a.eps);
-    if (threadIdx.x == 0 && a.rstd) a.rstd[row] = rstd;
+    RmsFactors f(s, (float)a.cols, a.eps, 1.0f);
+    const float scale = squares_scale(s, a.eps);
+    if (__builtin_amdgcn_readfirstlane(scale != 1.0f)) {  // the same for the whole workgroup
+        s = 0.0f;
+        for (int c = threadIdx.x * kV; c < a.cols; c += NT * kV) {
+            load_again(c, v);
+#pragma unroll
+            for (int i = 0; i < kV; ++i) s = fmaf(v[i] * scale, v[i] * scale, s);
+        }
+        row_sums<NT, NT>(s, none, tmp, 1);
+        f = RmsFactors(s, (float)a.cols, a.eps, scale);
+    }
+    if (threadIdx.x == 0 && a.rstd) a.rstd[row] = f.rstd();
     for (int base = 0; base < a.cols; base += NT * kV) {
         const int c = base + threadIdx.x * kV;
         float g[kV] = {};
         if (c < a.cols) {
-            if (a.S) load_chunk<T>(sum, c, a.cols, v);  // what this thread wrote
-            else load_sum(c, v);
+            load_again(c, v);
             load_param(a.gamma, c, a.cols, 1.0f, g);
 #pragma unroll
-            for (int i = 0; i < kV; ++i) g[i] = c + i < a.cols ? g[i] * (v[i] * rstd) : 0.0f;
+            for (int i = 0; i < kV; ++i) g[i] = c + i < a.cols ? g[i] * (v[i] * f.first * f.second) : 0.0f;
         }
         rms_results<T>(a, row, c, g);
     }
