@@ -205,13 +205,15 @@ class Quantize8Desc(ctypes.Structure):
 class Linear8Desc(ctypes.Structure):
     _fields_ = [("M", _i64), ("N", _i64), ("K", _i64), ("type", _i32), ("out_type", _i32), ("act", _i32),
                 ("X", Matrix8Arg), ("W", Matrix8Arg), ("bias", _vp), ("R", _vp), ("ldr", _i64), ("Y", _vp),
-                ("ldy", _i64), ("Z", _vp), ("ldz", _i64), ("Q", Matrix8Arg), ("ws", _vp), ("ws_bytes", _sz)]
+                ("ldy", _i64), ("Z", _vp), ("ldz", _i64), ("Q", Matrix8Arg), ("ws", _vp), ("ws_bytes", _sz),
+                ("exact", _i32)]
 
 
 class Glu8Desc(ctypes.Structure):
     _fields_ = [("M", _i64), ("N", _i64), ("K", _i64), ("type", _i32), ("act", _i32), ("X", Matrix8Arg),
                 ("Wg", Matrix8Arg), ("Wu", Matrix8Arg), ("bg", _vp), ("bu", _vp), ("H", _vp), ("ldh", _i64),
-                ("G", _vp), ("U", _vp), ("ldgu", _i64), ("Q", Matrix8Arg), ("ws", _vp), ("ws_bytes", _sz)]
+                ("G", _vp), ("U", _vp), ("ldgu", _i64), ("Q", Matrix8Arg), ("ws", _vp), ("ws_bytes", _sz),
+                ("exact", _i32)]
 
 
 class StructAdmmError(RuntimeError):
@@ -990,13 +992,14 @@ def quantize8(X, block_rows: int = 1, Q=None, QT=None, out: str = "q", stream=No
 
 
 def linear8_fwd(X, W, bias=None, R=None, act: int = ACT_NONE, Y=None, Z=None, Q=None, out_dtype=None, out: str = "y",
-                ws=None, stream=None):
+                ws=None, stream=None, exact: bool = False):
     """structadmm_linear8_fwd: act(X W^T + bias) + R for 8-bit X [M, K] (row blocks) and W
     [N, K] (square blocks); returns (Y, Q).  out names the results to make besides the
     buffers given: "y" (Y in out_dtype: R's type or else bfloat16 by default, float16 or
     float32) and "q" (Q in 8 bits with row blocks); the others are None.  R has Y's type.
     Z (bfloat16 or float16, Y's type unless that is float32): receives the
-    pre-activations."""
+    pre-activations.  exact: whole products also where every result has 16 bits, whose
+    sums may otherwise lose up to 2^-10 of their products' magnitudes (structadmm.h)."""
     import torch
     M, K = _codes_of(X, "linear8_fwd: X")
     N, _ = _codes_of(W, "linear8_fwd: W")
@@ -1014,18 +1017,19 @@ def linear8_fwd(X, W, bias=None, R=None, act: int = ACT_NONE, Y=None, Z=None, Q=
     y, ldy = _optional(Y, M, N, to, dev, w + "Y")
     z, ldz = _optional(Z, M, N, code, dev, w + "Z")
     d = Linear8Desc(M, N, K, code, to, act, _matrix8(X, M, K, 1, dev, w + "X"), _matrix8(W, N, K, BLOCK, dev, w + "W"),
-                    _vector(bias, N, dev, w + "bias"), r, ldr, y, ldy, z, ldz, _matrix8(Q, M, N, 1, dev, w + "Q"), None, 0)
+                    _vector(bias, N, dev, w + "bias"), r, ldr, y, ldy, z, ldz, _matrix8(Q, M, N, 1, dev, w + "Q"), None, 0, exact)
     _run(d, "structadmm_linear8_fwd", lib().structadmm_linear8_workspace, ws, X[0], stream)
     return Y, Q
 
 
 def glu8_fwd(X, Wg, Wu, bg=None, bu=None, act: int = ACT_SILU, H=None, Q=None, G=None, U=None, dtype=None,
-             out: str = "q", ws=None, stream=None):
+             out: str = "q", ws=None, stream=None, exact: bool = False):
     """structadmm_glu8_fwd: act(X Wg^T + bg) * (X Wu^T + bu) for 8-bit X [M, K] (row blocks),
     Wg and Wu [N, K] (square blocks; one pitch and one layout of scales); returns (H, Q).
     out names the results to make besides the buffers given: "h" (H in dtype: G's type or
     else bfloat16 by default, or float16) and "q" (Q in 8 bits with row blocks); the others
-    are None.  G and U (both or neither) receive the two projections, which glu_bwd reads."""
+    are None.  G and U (both or neither) receive the two projections, which glu_bwd reads.
+    exact: as for linear8_fwd."""
     import torch
     M, K = _codes_of(X, "glu8_fwd: X")
     N, _ = _codes_of(Wg, "glu8_fwd: Wg")
@@ -1041,7 +1045,7 @@ def glu8_fwd(X, Wg, Wu, bg=None, bu=None, act: int = ACT_SILU, H=None, Q=None, G
     ldgu = N if G is None else _pair(G, U, M, N, code, dev, (w + "G", w + "U"))
     d = Glu8Desc(M, N, K, code, act, _matrix8(X, M, K, 1, dev, w + "X"), _matrix8(Wg, N, K, BLOCK, dev, w + "Wg"),
                  _matrix8(Wu, N, K, BLOCK, dev, w + "Wu"), _vector(bg, N, dev, w + "bg"), _vector(bu, N, dev, w + "bu"),
-                 h, ldh, _ptr(G), _ptr(U), ldgu, _matrix8(Q, M, N, 1, dev, w + "Q"), None, 0)
+                 h, ldh, _ptr(G), _ptr(U), ldgu, _matrix8(Q, M, N, 1, dev, w + "Q"), None, 0, exact)
     _run(d, "structadmm_glu8_fwd", lib().structadmm_glu8_workspace, ws, X[0], stream)
     return H, Q
 

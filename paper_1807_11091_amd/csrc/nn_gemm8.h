@@ -20,6 +20,7 @@ struct Gemm8 {
     sa_matrix8 w[2];   // [N, K], square blocks, one pitch and one pair of scale strides
     Epilogue e;        // Y may be NULL
     sa_matrix8 q;      // the result in 8 bits, row blocks; codes NULL: none
+    int exact;         // whole products whatever the results
 };
 
 size_t gemm8_workspace(const Gemm8 &g);

@@ -387,6 +387,7 @@ int check_rms_bwd(const sa_rms_norm_bwd_desc &d, bool ptrs) {
 int check_linear8(const sa_linear8_desc &d, bool ptrs) {
     const char *w = "linear8_fwd";
     SA_TRY(check_product(w, d.M, d.N, d.K, d.type, d.out_type, d.act));
+    if (d.exact != 0 && d.exact != 1) return fail(SA_E_ARG, "%s: exact=%d must be 0 or 1", w, d.exact);
     SA_TRY(check_matrix8(w, "X", d.X, true, d.M, d.K, 1, false, ptrs));
     SA_TRY(check_matrix8(w, "W", d.W, true, d.N, d.K, SA_BLOCK, false, ptrs));
     SA_TRY(check_matrix(w, "R", d.R, false, d.M, d.N, d.ldr, d.out_type, ptrs));
@@ -413,6 +414,7 @@ int check_linear8(const sa_linear8_desc &d, bool ptrs) {
 int check_glu8(const sa_glu8_desc &d, bool ptrs) {
     const char *w = "glu8_fwd";
     SA_TRY(check_product(w, d.M, d.N, d.K, d.type, d.type, d.act));
+    if (d.exact != 0 && d.exact != 1) return fail(SA_E_ARG, "%s: exact=%d must be 0 or 1", w, d.exact);
     SA_TRY(check_matrix8(w, "X", d.X, true, d.M, d.K, 1, false, ptrs));
     SA_TRY(check_matrix8(w, "Wg", d.Wg, true, d.N, d.K, SA_BLOCK, false, ptrs));
     SA_TRY(check_matrix8(w, "Wu", d.Wu, true, d.N, d.K, SA_BLOCK, false, ptrs));
