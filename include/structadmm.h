@@ -885,6 +885,20 @@ typedef struct sa_glu8_desc {
 size_t structadmm_glu8_workspace(const sa_glu8_desc *desc);
 int structadmm_glu8_fwd(const sa_glu8_desc *desc, hipStream_t stream);
 
+/* Which kernel an 8-bit product takes, for programs that log or test it.  Host only: the
+ * device pointers are not read, the workspace is not looked at; otherwise the same
+ * validation and error codes as the call.  All 0 for a call without results. */
+typedef struct sa_product8_plan_info {
+    int32_t rows;    /* k_rows8: rows of M a workgroup takes (16, 32 or 64); 0: k_tile8 */
+    int32_t tile_n;  /* k_tile8: a tile's rows of W (gated: half of them of Wg, half of Wu) ... */
+    int32_t tile_m;  /* ... by its rows of M */
+    int32_t exact;   /* 1: whole products, 0: the 8-bit matrix instructions */
+    int32_t split;   /* parts of k */
+    int32_t joined;  /* 1: k_join8 adds the parts and makes the results */
+} sa_product8_plan_info;
+int structadmm_linear8_plan(const sa_linear8_desc *desc, sa_product8_plan_info *info);
+int structadmm_glu8_plan(const sa_glu8_desc *desc, sa_product8_plan_info *info);
+
 /* Message describing the last error on the calling thread ("" if none). */
 const char *structadmm_last_error(void);
 

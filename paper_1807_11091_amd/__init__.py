@@ -29,6 +29,7 @@ Entry points (same names as the C ABI):
   linear8_fwd(X, W, bias=None, R=None, act=ACT_NONE, ...) -> (Y, Q)
   glu8_fwd(X, Wg, Wu, bg=None, bu=None, act=ACT_SILU, ...) -> (H, Q)
   matrix8(rows, cols, block_rows=1, ...) -> an uninitialised Matrix8
+  product8_plan(M, N, K, gated=False, ...) -> dict: the kernel of linear8_fwd / glu8_fwd
   compacted_matrix(Wc, sizes, group=0) -> the [M, K] matrix of a compacted layer
 """
 from __future__ import annotations
@@ -216,6 +217,10 @@ class Glu8Desc(ctypes.Structure):
                 ("exact", _i32)]
 
 
+class Product8PlanInfo(ctypes.Structure):
+    _fields_ = [(n, _i32) for n in ("rows", "tile_n", "tile_m", "exact", "split", "joined")]
+
+
 class StructAdmmError(RuntimeError):
     pass
 
@@ -268,6 +273,10 @@ def lib():
                           ("quantize8", Quantize8Desc), ("linear8_fwd", Linear8Desc), ("glu8_fwd", Glu8Desc)):
             f = getattr(L, f"structadmm_{name}")
             f.argtypes = [ctypes.POINTER(cls), _vp]
+            f.restype = ctypes.c_int
+        for name, cls in (("linear8", Linear8Desc), ("glu8", Glu8Desc)):
+            f = getattr(L, f"structadmm_{name}_plan")
+            f.argtypes = [ctypes.POINTER(cls), ctypes.POINTER(Product8PlanInfo)]
             f.restype = ctypes.c_int
         for name, cls in (("layer_norm_bwd", LayerNormBwdDesc), ("linear", LinearDesc), ("linear_bwd", LinearBwdDesc),
                           ("glu", GluDesc), ("glu_bwd", GluBwdDesc), ("rms_norm_bwd", RmsNormBwdDesc),
@@ -1048,6 +1057,28 @@ def glu8_fwd(X, Wg, Wu, bg=None, bu=None, act: int = ACT_SILU, H=None, Q=None, G
                  h, ldh, _ptr(G), _ptr(U), ldgu, _matrix8(Q, M, N, 1, dev, w + "Q"), None, 0, exact)
     _run(d, "structadmm_glu8_fwd", lib().structadmm_glu8_workspace, ws, X[0], stream)
     return H, Q
+
+
+def product8_plan(M: int, N: int, K: int, gated: bool = False, out: str = "y", f32: bool = False,
+                  exact: bool = False) -> dict:
+    """structadmm_linear8_plan (gated: structadmm_glu8_plan): the kernel that a product of
+    these sizes takes for the outputs named in out ("y" or "h", "q"), host only.  f32: Y in
+    float32.  "rows" (0: a tile of "tile_n" x "tile_m"), "exact", "split", "joined"."""
+    info, at = Product8PlanInfo(), iter(range(1 << 12, 1 << 16, 1 << 8))  # addresses that nothing reads
+
+    def m8(rows, cols, there=True):
+        return Matrix8Arg(next(at) if there else None, (cols + 15) // 16 * 16, next(at) if there else None, 1, max(rows, 1))
+    q, y = m8(M, N, "q" in out), next(at) if "y" in out or "h" in out else None
+    x, w = m8(M, K), m8(_blocks(N), K)
+    if gated:
+        if f32:
+            raise StructAdmmError("product8_plan: a gated product has no float32 result")
+        d = Glu8Desc(M, N, K, BF16, ACT_NONE, x, w, w, None, None, y, N, None, None, N, q, None, 0, exact)
+        _check(lib().structadmm_glu8_plan(ctypes.byref(d), ctypes.byref(info)), "structadmm_glu8_plan")
+    else:
+        d = Linear8Desc(M, N, K, BF16, F32 if f32 else BF16, ACT_NONE, x, w, None, None, N, y, N, None, N, q, None, 0, exact)
+        _check(lib().structadmm_linear8_plan(ctypes.byref(d), ctypes.byref(info)), "structadmm_linear8_plan")
+    return {n: getattr(info, n) for n, _ in Product8PlanInfo._fields_}
 
 
 def version() -> str:

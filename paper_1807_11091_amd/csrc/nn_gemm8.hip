@@ -1049,6 +1049,22 @@ size_t workspace(const D &d, const void *y) {
     return std::max(gemm8_workspace(with), gemm8_workspace(without));
 }
 
+sa_product8_plan_info plan_info(const Gemm8 &g) {
+    sa_product8_plan_info info{};
+    if (g.M == 0 || g.N == 0) return info;
+    const Plan8 p = plan_of(g);
+    if (p.path < kTile64) {
+        info.rows = kRowsM8[p.path];
+    } else {
+        info.tile_n = kTileShape8[p.path - kTile64].bn;
+        info.tile_m = kTileShape8[p.path - kTile64].bm;
+    }
+    info.exact = is_exact(g);
+    info.split = p.split;
+    info.joined = p.keep;
+    return info;
+}
+
 }  // namespace
 
 size_t gemm8_workspace(const Gemm8 &g) {
@@ -1080,6 +1096,22 @@ extern "C" int structadmm_linear8_fwd(const sa_linear8_desc *desc, hipStream_t s
     const Gemm8 g = product(*desc);
     if (int rc = check_workspace("linear8_fwd", desc->ws, desc->ws_bytes, gemm8_workspace(g))) return rc;
     return gemm8(g, desc->ws, stream);
+}
+
+extern "C" int structadmm_linear8_plan(const sa_linear8_desc *desc, sa_product8_plan_info *info) {
+    clear_error();
+    if (!desc || !info) return fail(SA_E_ARG, "linear8_plan: desc and info are required");
+    if (int rc = validate_linear8(*desc)) return rc;
+    *info = plan_info(product(*desc));
+    return SA_OK;
+}
+
+extern "C" int structadmm_glu8_plan(const sa_glu8_desc *desc, sa_product8_plan_info *info) {
+    clear_error();
+    if (!desc || !info) return fail(SA_E_ARG, "glu8_plan: desc and info are required");
+    if (int rc = validate_glu8(*desc)) return rc;
+    *info = plan_info(product(*desc));
+    return SA_OK;
 }
 
 extern "C" size_t structadmm_glu8_workspace(const sa_glu8_desc *desc) {
