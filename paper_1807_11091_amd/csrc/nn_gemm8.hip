@@ -273,8 +273,7 @@ template <bool GATED, int BN, int BM, int WN, int WM, int S>
 struct TileCfg8 {
     static constexpr int NW = WN * WM, NT = NW * 64;
     static constexpr int scales_at = (BN + BM) * kBlock;
-    static constexpr int xl = (BM / WM + 63) / 64;              // loads of X's scales
-    static constexpr int scales = xl * 256 + 16;                // bytes a wavefront: X's, then W's
+    static constexpr int scales = 256 + 16;                     // bytes a wavefront: X's, one a lane, then W's
     static constexpr int stage = scales_at + NW * scales;
     static constexpr int join_at = S * stage;                   // largest values of the results' rows
     static constexpr bool touches = BM == 256;                  // see touch()
@@ -387,9 +386,9 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8) {
     constexpr int NROWS = GATED ? BN / 2 : BN;  // n of a tile; gated: one half of the N side per projection
     using NSide = Side8<NROWS, NW>;
     using MSide = Side8<BM, NW>;
-    constexpr int NL = NSide::loads * H, ML = NL + MSide::loads, XL = Cfg::xl, L = ML + XL + H;  // loads of a stage
+    constexpr int NL = NSide::loads * H, ML = NL + MSide::loads, L = ML + 1 + H;  // loads of a stage
     constexpr int WROWS = NROWS / WN, MROWS = BM / WM;               // n and m of a wavefront
-    static_assert(128 % WROWS == 0 && (MROWS <= 64 || MROWS % 64 == 0) && TNG % 2 == 0 && TN % 2 == 0 && L * (S - 1) < 64, "shape");
+    static_assert(128 % WROWS == 0 && MROWS <= 64 && TNG % 2 == 0 && TN % 2 == 0 && L * (S - 1) < 64, "shape");
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
 
     // The arguments are read anew where they are used, so that the loop over the stages has
@@ -456,7 +455,6 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8) {
     typename MSide::Cursor mc;
     i32x4 xs, ws[H];  // the scales' buffers
     const uint32_t xoff = lane < MROWS ? (uint32_t)lane * (uint32_t)args().g.x.scale_row * 4u : kInvalidOffset;
-    const uint32_t xmore = XL > 1 ? uni((int)args().g.x.scale_row * 256) : 0;  // 64 rows further on
     const uint64_t xstep = (uint64_t)args().g.x.scale_col * 4, wstep = (uint64_t)args().g.w[0].scale_col * 4;
     uint32_t lat = lds0 + wave * 1024, slat = lds0 + Cfg::scales_at + wave * Cfg::scales;
     int run = 0, lstage = 0, lend = 0, ltile = -1, lslot = 0;
@@ -506,9 +504,9 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8) {
         if constexpr (i < NSide::loads) nside.template load<i>(nc, lat);
         else if constexpr (i < NL) nside.template load<i - NSide::loads>(nc1, lat + NSide::bytes);
         else if constexpr (i < ML) mside.template load<i - NL>(mc, lat + BN * kBlock);
-        else if constexpr (i < ML + XL) dma4<256 * (i - ML)>(xs, xoff, (i - ML) * xmore, slat);
+        else if constexpr (i == ML) dma4<0>(xs, xoff, 0, slat);
         else if constexpr (i < L) {
-            if (lane == 0) dma4<256 * XL + 4 * (i - ML - XL)>(ws[i - ML - XL], 0, 0, slat);
+            if (lane == 0) dma4<256 + 4 * (i - ML - 1)>(ws[i - ML - 1], 0, 0, slat);
         }
     };
     auto move = [](i32x4 &rs, uint64_t by) {
@@ -566,7 +564,7 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8) {
 #pragma unroll
         for (int j = 0; j < TM; ++j) scale[0][j] = s[j * MI + (lane & (MI - 1))];
 #pragma unroll
-        for (int h = 0; h < H; ++h) wscale[h] = s[64 * XL + h];
+        for (int h = 0; h < H; ++h) wscale[h] = s[64 + h];
     };
     auto join_scales = [&]() {
 #pragma unroll
@@ -689,15 +687,16 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void k_tile8(TileArgs8) {
     // The lines of a tile's residual, which the epilogue reads piece by piece, into the L2, a
     // stage before: 8192 x 4096 x 9830 took 337 us without.  The words read go to LDS and are
     // not used.  Not in smaller tiles, where it cost more than it gave (a binary32 result with a
-    // residual 620 us, 633 with it).
+    // residual 620 us, 633 with it), so the residual has 16 bits.
     auto touch = [&](const Tile &q) {
         const Gemm8 &g = args().g;
         if (!g.e.R || args().part.keep) return;
-        const int size = g.e.out_f32 ? 4 : 2, per = NROWS * size / 128;  // lines a row
+        constexpr int size = 2, per = NROWS * size / 128;  // lines a row
         const int rows = (int)min(g.M - q.m0, (int64_t)BM), bytes = (int)min(g.N - q.n0, (int64_t)NROWS) * size;
         const uint64_t at = reinterpret_cast<uint64_t>(g.e.R) + (q.m0 * g.e.ldr + q.n0) * size;
         const uint32_t pitch = (uint32_t)g.e.ldr * (uint32_t)size;
         const i32x4 rs = buffer_at(at & ~(uint64_t)3, uni((int)((uint32_t)(rows - 1) * pitch + (uint32_t)bytes) & ~3));
+#pragma unroll 1  // side by side they would spill
         for (int c = 0; c < BM * per; c += Cfg::NT) {
             const int i = c + tid, row = i / per, in = (i - row * per) * 128;
             dma4<Cfg::touch_at>(rs, row < rows && in < bytes ? (uint32_t)row * pitch + (uint32_t)in & ~3u : kInvalidOffset, 0, lds0);
@@ -885,7 +884,7 @@ struct TileShape8 {
     int bn, bm, slots;                // tile; workgroups that the 256 CUs hold
 };
 constexpr TileShape8 kTileShape8[4] = {{128, 64, 512}, {128, 128, 512}, {256, 128, 256}, {256, 256, 256}};
-constexpr TileModel8 kTileModel8[4][4] = {
+constexpr TileModel8 kTileModel8[3][4] = {
     {{5.21f, 1.33f, 0.381f, 0.633f, 0.966f, 0.0442f, 1.53f, 0.285f, 0.296f},
      {6.74f, 1.23f, 0.698f, 1.07f, 1.13f, 0.0441f, 0.664f, 0.29f, 0.285f},
      {4.86f, 1.54f, 0.404f, 0.671f, 0.668f, 0.0464f, 1.86f, 0.32f, 0.333f},
@@ -898,11 +897,9 @@ constexpr TileModel8 kTileModel8[4][4] = {
      {8.48f, 3.03f, 15.3f, 1.52f, 1.19f, 0.0425f, 0.0f, 0.267f, 0.261f},
      {6.05f, 2.06f, 10.1f, 0.799f, 0.748f, 0.0538f, 2.0f, 0.313f, 0.323f},
      {7.52f, 2.27f, 22.0f, 1.62f, 0.885f, 0.052f, 1.23f, 0.321f, 0.29f}},
-    {{7.66f, 4.73f, 5.79f, 1.37f, 1.0f, 0.0655f, 0.926f, 0.268f, 0.272f},
-     {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f},
-     {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f},
-     {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f}},
 };
+// 256 x 256: plain products by 8-bit instructions only
+constexpr TileModel8 kTileModel256x256 = {7.66f, 4.73f, 5.79f, 1.37f, 1.0f, 0.0655f, 0.926f, 0.268f, 0.272f};
 
 // Do the results of a path go through k_join8?
 bool is_joined(const Gemm8 &g, Path8 path, int split) {
@@ -922,7 +919,7 @@ float rows_time(const Gemm8 &g, int i, int split) {
 }
 
 float tile_time(const Gemm8 &g, int i, int split) {
-    const TileModel8 &m = kTileModel8[i][(g.gated ? 2 : 0) + is_exact(g)];
+    const TileModel8 &m = i < 3 ? kTileModel8[i][(g.gated ? 2 : 0) + is_exact(g)] : kTileModel256x256;
     const TileShape8 &s = kTileShape8[i];
     const int64_t nn = g.N * (g.gated ? 2 : 1);
     const int64_t tiles = ((g.M + s.bm - 1) / s.bm) * ((nn + s.bn - 1) / s.bn) * split, rest = tiles % s.slots;

@@ -1,6 +1,9 @@
 """Which kernel an 8-bit product takes (CPU): the sizes of the parity tests take the kernels
 that they are there for, and those are all kernels that any size takes."""
+import ctypes
+import os
 import random
+import subprocess
 
 import pytest
 
@@ -56,3 +59,18 @@ def test_plan_refuses_what_the_call_refuses():
         with pytest.raises(sa.StructAdmmError):
             sa.product8_plan(*sizes, **kw)
     assert sa.lib().structadmm_linear8_plan(None, None) == -1 and sa.lib().structadmm_glu8_plan(None, None) == -1
+
+
+def test_info_layout_matches_header(tmp_path):
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    names = [n for n, _ in sa.Product8PlanInfo._fields_]
+    lines = ["#include <stdio.h>", "#include <stddef.h>", '#include "structadmm.h"', "int main(void){"]
+    lines += [f'printf("%zu\\n", offsetof(sa_product8_plan_info, {n}));' for n in names]
+    lines += ['printf("%zu\\n", sizeof(sa_product8_plan_info));', "return 0;}"]
+    src, exe = str(tmp_path / "l.c"), str(tmp_path / "l")
+    with open(src, "w") as f:
+        f.write("\n".join(lines))
+    subprocess.check_call(["gcc", "-D__HIP_PLATFORM_AMD__", "-I", os.path.join(root, "include"), "-I", "/opt/rocm/include",
+                           src, "-o", exe])
+    got = [int(v) for v in subprocess.check_output([exe]).decode().split()]
+    assert got == [getattr(sa.Product8PlanInfo, n).offset for n in names] + [ctypes.sizeof(sa.Product8PlanInfo)]
