@@ -710,7 +710,9 @@ int structadmm_glu_bwd(const sa_glu_bwd_desc *desc, hipStream_t stream);
  *
  * Written by these calls, a block has
  *   scale = max(largest |v| / 448, 2^-126), code = v * (1 / scale) to nearest even,
- * of the binary32 values v.  The scale leaves NaN out of account and a NaN has a NaN
+ * of the binary32 values v; the quotient, the reciprocal and the product are rounded to
+ * binary32 (the code of v / scale is another one where a rounding takes v across the middle
+ * of two codes, which is as far from either).  The scale leaves NaN out of account and a NaN has a NaN
  * code; in a block with an infinity the scale is infinite, the infinities' codes are
  * NaN and the others 0, so that a product with the block gives NaN.
  */
@@ -790,9 +792,15 @@ int structadmm_rms_norm_bwd(const sa_rms_norm_bwd_desc *desc, hipStream_t stream
  * NULL).  The row blocks of QT run along X's rows, and so have scales of their own;
  * with square blocks QT holds the codes and scales of Q transposed.
  *
- * A product's gradients are products of such operands: with dY's row blocks Q and QT,
- * the square blocks QT of W and QT of X,
- *   dX = linear8_fwd(dY.Q, W.QT), dW = linear8_fwd(dY.QT, X.QT) (out_type SA_F32).
+ * The gradients of a product z = X W^T are products of such operands: with the row blocks
+ * Q and QT of dz, the square blocks QT of W and QT of X,
+ *   dX = linear8_fwd(dz.Q, W.QT), dW = linear8_fwd(dz.QT, X.QT) (out_type SA_F32).
+ * dz is the gradient that reaches the product: dY where there is no activation.  Past an
+ * activation or a gate it is the caller's to make (dz = dY act'(z); for a gated pair
+ * dg = dH u act'(g), du = dH act(g)); structadmm_linear_bwd and structadmm_glu_bwd keep
+ * theirs in their workspaces and go on in 16 bits, with X and W in 16 bits.  QT of X comes
+ * from X's values in 16 or 32 bits, not from its row blocks: ask the call that makes X in 8
+ * bits for them too (Y beside Q, H beside Q).
  */
 typedef struct sa_quantize8_desc {
     int64_t rows, cols;   /* QT: rows at most SA_MAX_LD */
