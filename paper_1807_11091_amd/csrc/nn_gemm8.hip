@@ -264,11 +264,13 @@ __global__ __launch_bounds__(512, PER) void k_rows8(Gemm8 g, Partial8 q) {
 //
 // Workgroups are persistent and their loads run over the stages of all their tiles.
 //
-// Bound by the matrix cores' power and, in exact products, by issue: 8192 x 4096 x 9830 with
-// 16-bit results takes 284 us (2.3 PFLOP/s; 324 with bias and residual), exact 584 (1.13), of
-// which the widening of the codes and the scaling of the blocks issue 3 vector instructions
-// beside each matrix instruction, which hides 2.  With two stages in flight, and arguments kept
-// in registers that then spilled, exact products took 659.
+// 8192 x 4096 x 9830 with 16-bit results takes 287 us (2.3 PFLOP/s; 318 to 331 with bias and
+// residual): the matrix cores are busy half the time, a third of the wavefronts wait for
+// loads, LDS or the barrier and a third for their turn to issue, at a clock of 2.0 GHz (2.4
+// in a copy without loads).  Exact products take 552 (1.2 PFLOP/s), bound by issue: the
+// widening of the codes and the scaling of the blocks are 3.4 vector instructions beside each
+// matrix instruction, which hides 2.  With two stages in flight, and arguments kept in
+// registers that then spilled, they took 75 more.
 template <bool GATED, int BN, int BM, int WN, int WM, int S>
 struct TileCfg8 {
     static constexpr int NW = WN * WM, NT = NW * 64;
@@ -843,7 +845,7 @@ struct Plan8 {
 };
 
 // 8-bit instructions where every result has 16 bits and the caller leaves the choice
-// (8192 x 4096 x 9830: 284 us, and 584 of exact products).
+// (8192 x 4096 x 9830: 287 us, and 552 of exact products).
 bool is_exact(const Gemm8 &g) { return g.exact || g.q.codes || g.e.out_f32; }
 
 // n of a tile
